@@ -242,6 +242,70 @@ ssgd_status ssgd_debug_batch(uint64_t seed, uint32_t replica, uint32_t worker, u
 ssgd_status ssgd_stream_read_rate(const void *data, int64_t bytes, int32_t passes, void *hip_stream,
                                   double *bytes_per_s);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a low-precision training step, beside the simulated workers: the master's update as
+ * an adaptive one, the norm in front of a product, and the product itself on few bits.  They take no
+ * context: tensors are DEVICE pointers on the HIP device that is current, all work is enqueued on
+ * `hip_stream` (a hipStream_t of that device; NULL = default stream) and nothing is awaited, allocated
+ * or copied to the host unless a call says so.  Arguments are checked before anything is enqueued
+ * (SSGD_EINVAL, text in ssgd_last_error(NULL)).  Rows of a matrix are contiguous and `pitch` elements
+ * apart (pitch >= columns); no buffer has to be aligned beyond its element type unless that is said,
+ * 16-byte aligned ones with pitches that are a multiple of 8 elements are the fast ones.  Inputs and
+ * outputs must not overlap unless that is said.  A result does not depend on the stream, the pitch, the
+ * alignment or on other work on the device: every sum is taken in a fixed order. */
+typedef enum { SSGD_F32 = 0, SSGD_BF16 = 1 } ssgd_dtype;
+
+/* Microscaled matrices: 32 consecutive columns of a row share the scale 2^(byte - 127), and each value is an E2M1 (4 bits: 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 and their negatives; two to a byte, the first in the low nibble) or an E4M3 (8 bits, magnitudes to 448)
+ * multiple of it.  byte - 127 = floor(log2 of the block's largest magnitude) - 2 (E2M1) or - 8 (E4M3), at least -127; a value is
+ * divided by the scale and rounded to the nearest of the format, ties to the even code, and to the largest where it is past it (a
+ * block's largest magnitude is at most 8 / 6 or 512 / 448 of it).  A block of zeros has byte 0.  A block with an infinity or NaN
+ * has byte 255 and zeros as values, and stands for NaN.
+ * Layout, row-major: values rows x ssgd_mx_row_bytes, scales rows x (that row's columns / 32) bytes.  Rows are padded
+ * with zeros (values and scale bytes) to a multiple of 128 columns, since a product contracts 128 at a time; the padding is
+ * written by ssgd_mx_quantize and ssgd_rmsnorm and relied upon by the products.  Both arrays 16-byte aligned. */
+typedef enum { SSGD_MX_FP4 = 0, SSGD_MX_FP8 = 1 } ssgd_mx_format;
+
+/* AdamW over many tensors at once.  For every element, with the gradient g, the update's number t and
+ *   g' = g c,   c = min(1, max_norm / (norm + 1e-6)),   norm = (sum of g^2 over all tensors)^(1/2)
+ *   m  = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^t)  m / ((v / (1 - beta2^t))^(1/2) + eps)
+ * in fp32 (the norm in fp64; max_norm = 0: no clipping, c = 1).  Infinities and NaN follow the formulas.
+ * Moments lie in arrays of ssgd_adamw_state_elements elements, in which tensor k begins behind the tensors before it, each
+ * rounded up to a multiple of 128 elements (the rest of the last 128 stays zero):
+ *   state_bits 32: m, v fp32 (m_scale, v_scale NULL)
+ *   state_bits 8:  m and the square root of v as E4M3 values times an fp32 scale per block of 128 elements, the largest
+ *                  magnitude of the block / 448 (one below 2^-100 makes the block zero).  The update uses the new moments
+ *                  before they are rounded.  Rounding is stochastic: a value between two neighbours goes to the upper one
+ *                  with the probability of its place between them (in 1/65536), so that averages move that a nearest
+ *                  rounding would stop (beta2 = 0.999 changes v by less than half a place).  The random numbers are a hash
+ *                  of (seed, t, place in the state array), so equal arguments give equal results.  The root of a v above zero is never
+ *                  rounded to zero.  A block with an infinity or NaN becomes NaN in the next step. */
+typedef struct ssgd_adamw ssgd_adamw; /* opaque, library-owned */
+typedef struct {
+    double beta1, beta2; /* in [0, 1) */
+    double eps;          /* > 0 */
+    double max_norm;     /* >= 0; 0: no clipping */
+    int32_t state_bits;  /* 32 or 8 */
+    uint64_t seed;       /* of the stochastic rounding */
+} ssgd_adamw_options;
+
+/* Elements of a moment's array for these tensors (sizes >= 0; -1 for an invalid argument). */
+int64_t ssgd_adamw_state_elements(int32_t tensors, const int64_t *sizes);
+/* A handle for these tensors: sizes[k] elements of contiguous fp32 parameters at params[k]; copies (HOST array, nullable, and
+ * its entries too) receive the new parameters in bf16; weight_decay[k] (HOST).  m and v: 16-byte aligned.  The handle keeps
+ * the DEVICE pointers and a work area on the current device (this call allocates and waits). */
+ssgd_status ssgd_adamw_create(int32_t tensors, const int64_t *sizes, float *const *params, void *const *copies,
+                              const double *weight_decay, const ssgd_adamw_options *options, void *m, void *v,
+                              float *m_scale, float *v_scale, ssgd_adamw **out);
+/* Update number t (>= 1) with the gradients grads[k] (HOST array of DEVICE pointers, sizes[k] contiguous elements of grad_dtype, an
+ * ssgd_dtype).  norm_out (DEVICE, nullable, one float): the norm of all gradients, written when max_norm > 0.  Steps of one handle
+ * share its work area and have to be ordered among themselves. */
+ssgd_status ssgd_adamw_step(ssgd_adamw *handle, const void *const *grads, int32_t grad_dtype, double lr, int64_t t,
+                            float *norm_out, void *hip_stream);
+/* Waits for the device and frees the work area. */
+void ssgd_adamw_destroy(ssgd_adamw *handle);
+
 /* Text of the last error of a context (ctx may be NULL: last error of a call
  * that has no context).  Valid until the next call on that context. */
 const char *ssgd_last_error(const ssgd_ctx *ctx);

@@ -1,0 +1,175 @@
+// Shared by the operators of a low-precision training step (adamw.hip, rmsnorm.hip, mx_quantize.hip, mx_matmul.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <exception>
+#include <new>
+#include <string>
+
+#include "../../include/ssgd.h"
+#include "common.hpp"
+
+namespace ssgd {
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+inline ssgd_status op_fail(ssgd_status st, const char* what) {
+    try { set_global_error(what); } catch (...) {}
+    return st;
+}
+inline ssgd_status op_hip(hipError_t e, const char* what) {
+    if (e == hipSuccess) return SSGD_OK;
+    try { set_global_error(std::string(what) + ": " + hipGetErrorString(e)); } catch (...) {}
+    return e == hipErrorOutOfMemory ? SSGD_ENOMEM : SSGD_EDEVICE;
+}
+// Nothing throws across the ABI.
+template <typename F>
+ssgd_status op_entry(F&& body) {
+    try { return body(); }
+    catch (const std::bad_alloc&) { return op_fail(SSGD_ENOMEM, "out of host memory"); }
+    catch (...) { return op_fail(SSGD_EDEVICE, "unexpected error"); }
+}
+inline bool dtype_ok(int32_t t) { return t == SSGD_F32 || t == SSGD_BF16; }
+inline int64_t dtype_bytes(int32_t t) { return t == SSGD_F32 ? 4 : 2; }
+inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+constexpr int kMxBlock = 32;      // columns per scale
+constexpr int kMxPad = 128;       // rows of a quantised matrix are padded to so many columns: what one matrix instruction contracts
+constexpr int64_t mx_padded(int64_t cols) { return (cols + kMxPad - 1) / kMxPad * kMxPad; }
+constexpr int64_t mx_row_bytes(int fmt, int64_t cols) { return fmt == SSGD_MX_FP4 ? mx_padded(cols) / 2 : mx_padded(cols); }
+
+// ---- device ----------------------------------------------------------------------------------------------------------
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef uint16_t bf16_t;          // bits of a bfloat16
+
+__device__ __forceinline__ float bf16_to_f32(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+// Nearest even; NaN stays NaN (one instruction for two values).
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const f32x2 v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ uint32_t f32_to_bf16(float x) { return pack_bf16(x, 0.0f) & 0xFFFFu; }
+
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ float load_one(const bf16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void store_one(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_one(bf16_t* p, float x) { *p = (bf16_t)f32_to_bf16(x); }
+
+// V consecutive values (4 or 8) at p; `left` of them exist, the rest are zero.  wide: p is a multiple of 16 bytes (8 for four bf16).
+template <int V>
+__device__ __forceinline__ void load_vec(const float* p, bool wide, int64_t left, float (&x)[V]) {
+    if (wide && left >= V) {
+#pragma unroll
+        for (int q = 0; q < V; q += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(p + q);
+            x[q] = v.x; x[q + 1] = v.y; x[q + 2] = v.z; x[q + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) x[q] = q < left ? p[q] : 0.0f;
+    }
+}
+template <int V>
+__device__ __forceinline__ void load_vec(const bf16_t* p, bool wide, int64_t left, float (&x)[V]) {
+    if (wide && left >= V) {
+        uint32_t w[V / 2];
+        if constexpr (V == 8) {
+            const words4 v = *reinterpret_cast<const words4*>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const words2 v = *reinterpret_cast<const words2*>(p);
+            w[0] = v.x; w[1] = v.y;
+        }
+#pragma unroll
+        for (int q = 0; q < V / 2; ++q) { x[2 * q] = bf16_to_f32(w[q] & 0xFFFFu); x[2 * q + 1] = __builtin_bit_cast(float, w[q] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) x[q] = q < left ? bf16_to_f32(p[q]) : 0.0f;
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_vec(float* p, bool wide, int64_t left, const float (&x)[V]) {
+    if (wide && left >= V) {
+#pragma unroll
+        for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4*>(p + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) if (q < left) p[q] = x[q];
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_vec(bf16_t* p, bool wide, int64_t left, const float (&x)[V]) {
+    if (wide && left >= V) {
+        if constexpr (V == 8) *reinterpret_cast<words4*>(p) = words4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+        else *reinterpret_cast<words2*>(p) = words2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q) if (q < left) p[q] = (bf16_t)f32_to_bf16(x[q]);
+    }
+}
+
+// Moves within rows of 16 lanes, without LDS.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// Largest of 4 and of 16 adjacent lanes.  On the bits of magnitudes: infinities and NaN are the largest, so they carry.
+__device__ __forceinline__ uint32_t max_of_4(uint32_t x) { x = umax(x, dpp<kXor1>(x)); return umax(x, dpp<kXor2>(x)); }
+__device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
+    x = max_of_4(x);
+    x = umax(x, dpp<kHalfMirror>(x));
+    return umax(x, dpp<kMirror>(x));
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+    return x;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+    return x;
+}
+
+// ---- microscaled formats ---------------------------------------------------------------------------------------------
+// A block of 32 values shares the scale 2^(byte - 127), the exponent of its largest magnitude less that of the format's largest
+// value (E2M1: 6 = 1.5 x 2^2, E4M3: 448 = 1.75 x 2^8), so that the largest value lands in the top binade and saturates in its
+// upper part.  Byte 255 stands for NaN: a block with an infinity or a NaN has no scale.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest) {
+    const uint32_t e = largest >> 23, top = FMT == SSGD_MX_FP4 ? 2u : 8u;
+    return e == 255u ? 255u : (e > top ? e - top : 0u);
+}
+__device__ __forceinline__ float mx_inverse_scale(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }   // byte <= 252
+// Eight values at a scale -> 4 (E2M1, low nibble first) or 8 bytes, nearest, ties to even, saturating.
+__device__ __forceinline__ uint32_t mx_pack_fp4(const float (&x)[8], uint32_t byte) {
+    if (byte == 255u) return 0u;
+    const float inv = mx_inverse_scale(byte);
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0] * inv, x[1] * inv, 1.0f, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2] * inv, x[3] * inv, 1.0f, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4] * inv, x[5] * inv, 1.0f, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6] * inv, x[7] * inv, 1.0f, 3);
+    return r;
+}
+// (the conversion gives NaN past the largest value, so the values are cut off before it)
+__device__ __forceinline__ float clamp448(float x) { return __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f); }
+__device__ __forceinline__ words2 mx_pack_fp8(const float (&x)[8], uint32_t byte) {
+    if (byte == 255u) return words2{0u, 0u};
+    const float inv = mx_inverse_scale(byte);
+    float y[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) y[q] = clamp448(x[q] * inv);
+    int lo = 0, hi = 0;
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], lo, false); lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], hi, false); hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+    return words2{(uint32_t)lo, (uint32_t)hi};
+}
+
+}  // namespace ssgd

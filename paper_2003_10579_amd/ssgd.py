@@ -15,6 +15,7 @@ K_SYNC, K_BATCH_SYNC, K_ASYNC, K_BATCH_ASYNC = 0, 1, 2, 3
 EXP, SHIFTED_EXP, PARETO, TABLE = 0, 1, 2, 3
 OK, EINVAL, ENOMEM, EDEVICE, ESTATE = 0, 1, 2, 3, 4
 _VARIANTS = {"k_sync": K_SYNC, "k_batch_sync": K_BATCH_SYNC, "k_async": K_ASYNC, "k_batch_async": K_BATCH_ASYNC}
+F32, BF16 = 0, 1
 _KINDS = {"lsq": LSQ, "softmax": SOFTMAX, "mlp2": MLP2}
 
 EXPORTS = [
@@ -23,7 +24,7 @@ EXPORTS = [
     "ssgd_get_workers", "ssgd_state_bytes", "ssgd_get_state", "ssgd_set_state", "ssgd_full_loss",
     "ssgd_full_gradient", "ssgd_full_gradient_static",
     "ssgd_runtime_mc", "ssgd_debug_delays", "ssgd_debug_batch", "ssgd_stream_read_rate", "ssgd_last_error",
-    "ssgd_last_kernel_ms",
+    "ssgd_last_kernel_ms", "ssgd_adamw_state_elements", "ssgd_adamw_create", "ssgd_adamw_step", "ssgd_adamw_destroy",
     "ssgd_destroy",
 ]
 
@@ -47,6 +48,11 @@ class ModelDesc(C.Structure):
 class AdaSync(C.Structure):
     _fields_ = [("mode", C.c_int32), ("K0", C.c_int32), ("Kmax", C.c_int32), ("window", C.c_int32),
                 ("rel_tol", C.c_double), ("interval_t", C.c_double)]
+
+
+class AdamWOptions(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("max_norm", C.c_double),
+                ("state_bits", C.c_int32), ("seed", C.c_uint64)]
 
 
 _lib = None
@@ -104,6 +110,11 @@ def lib():
         L.ssgd_last_error.argtypes = [C.c_void_p]
         L.ssgd_last_kernel_ms.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.ssgd_destroy.argtypes = [C.c_void_p]
+        L.ssgd_adamw_state_elements.restype = C.c_int64
+        L.ssgd_adamw_state_elements.argtypes = [C.c_int32, C.c_void_p]
+        L.ssgd_adamw_create.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(AdamWOptions)] + [C.c_void_p] * 5
+        L.ssgd_adamw_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_double, C.c_int64, C.c_void_p, C.c_void_p]
+        L.ssgd_adamw_destroy.argtypes = [C.c_void_p]
         _lib = L
     return _lib
 
@@ -291,3 +302,92 @@ def debug_batch(seed, replica, worker, ordinal, version, m, N):
     out = np.zeros(m, dtype=np.uint32)
     _check(lib().ssgd_debug_batch(seed, replica, worker, ordinal, version, m, N, out.ctypes.data))
     return out
+
+
+# ---- operators of a low-precision training step: on the device and the current stream of their tensors ----------------
+
+def _need(ok, msg):
+    if not ok:
+        raise SsgdError(EINVAL, msg)
+
+
+def _dtype(t):
+    import torch
+    if t == torch.float32:
+        return F32
+    if t == torch.bfloat16:
+        return BF16
+    raise SsgdError(EINVAL, f"float32 or bfloat16 is wanted, not {t}")
+
+
+def _call(entry, device, *args):
+    """One library call on the device and its current stream, which is the last argument of every operator."""
+    import torch
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        _check(entry(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args, stream))
+
+
+class AdamW:
+    """AdamW over many tensors at once (ssgd_adamw_*): fp32 parameters, updated in place; `copies` (a list of bfloat16
+    tensors, entries may be None) receive them rounded.  The moments are `m` and `v`, flat arrays of 32-bit numbers or, with
+    `state_bits=8`, of E4M3 values (of m and of the root of v) with a scale per 128 elements in `m_scale`, `v_scale`; `t`
+    counts the updates.  These five are all that a checkpoint needs.  With `max_norm` gradients are clipped to that norm
+    over all tensors, and `grad_norm` (one element on the device) holds the norm of the last step's."""
+
+    def __init__(self, params, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, max_norm=0.0, state_bits=32, seed=0, copies=None):
+        import torch
+        self.h = None
+        params = list(params)
+        _need(len(params) > 0, "adamw: at least one tensor")
+        dev = params[0].device
+        copies = [None] * len(params) if copies is None else list(copies)
+        decay = [float(weight_decay)] * len(params) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        _need(len(copies) == len(params) and len(decay) == len(params), "adamw: one copy and one weight decay per tensor")
+        for p, c in zip(params, copies):
+            _need(p.is_cuda and p.device == dev and p.dtype == torch.float32 and p.is_contiguous(), "adamw: parameters are contiguous float32 tensors of one GPU")
+            _need(c is None or (c.device == dev and c.dtype == torch.bfloat16 and c.is_contiguous() and c.numel() == p.numel()),
+                  "adamw: copies are contiguous bfloat16 tensors of their parameter's size")
+        n = len(params)
+        self._sizes = [p.numel() for p in params]
+        sizes = (C.c_int64 * n)(*self._sizes)
+        total = lib().ssgd_adamw_state_elements(n, sizes)
+        _need(state_bits in (8, 32), "adamw: state_bits is 8 or 32")
+        self.m = torch.zeros(total, device=dev, dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn)
+        self.v = torch.zeros_like(self.m)
+        self.m_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
+        self.v_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
+        self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
+        self.t = 0
+        self._keep, self._device, self._pointers = (params, copies), dev, C.c_void_p * n
+        o = AdamWOptions(float(betas[0]), float(betas[1]), float(eps), float(max_norm), state_bits, seed)
+        h = C.c_void_p()
+        with torch.cuda.device(dev):
+            _check(lib().ssgd_adamw_create(
+                n, sizes, self._pointers(*[p.data_ptr() for p in params]), self._pointers(*[None if c is None else c.data_ptr() for c in copies]),
+                (C.c_double * n)(*decay), C.byref(o), self.m.data_ptr(), self.v.data_ptr(),
+                None if self.m_scale is None else self.m_scale.data_ptr(), None if self.v_scale is None else self.v_scale.data_ptr(), C.byref(h)))
+        self.h = h
+
+    def step(self, grads, lr):
+        """One update with a list of gradients, contiguous tensors of one type (float32 or bfloat16) and their parameters' sizes."""
+        _need(self.h is not None, "adamw: closed")
+        _need(len(grads) == len(self._sizes), "adamw step: one gradient per tensor")
+        kind = grads[0].dtype
+        for g, n in zip(grads, self._sizes):
+            _need(g.dtype == kind and g.numel() == n and g.device == self._device and g.is_contiguous(),
+                  "adamw step: gradients are contiguous tensors of one type, of their parameters' sizes and device")
+        _call(lib().ssgd_adamw_step, self._device, self.h, self._pointers(*[g.data_ptr() for g in grads]), _dtype(kind), lr, self.t + 1,
+              None if self.grad_norm is None else self.grad_norm.data_ptr())
+        self.t += 1
+
+    def close(self):
+        if getattr(self, "h", None):
+            lib().ssgd_adamw_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        self.close()
