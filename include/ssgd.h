@@ -261,10 +261,36 @@ typedef enum { SSGD_F32 = 0, SSGD_BF16 = 1 } ssgd_dtype;
  * divided by the scale and rounded to the nearest of the format, ties to the even code, and to the largest where it is past it (a
  * block's largest magnitude is at most 8 / 6 or 512 / 448 of it).  A block of zeros has byte 0.  A block with an infinity or NaN
  * has byte 255 and zeros as values, and stands for NaN.
- * Layout, row-major: values rows x ssgd_mx_row_bytes, scales rows x (that row's columns / 32) bytes.  Rows are padded
+ * Layout, row-major: values rows x ssgd_mx_row_bytes(fmt, cols), scales rows x (that row's columns / 32) bytes.  Rows are padded
  * with zeros (values and scale bytes) to a multiple of 128 columns, since a product contracts 128 at a time; the padding is
  * written by ssgd_mx_quantize and ssgd_rmsnorm and relied upon by the products.  Both arrays 16-byte aligned. */
 typedef enum { SSGD_MX_FP4 = 0, SSGD_MX_FP8 = 1 } ssgd_mx_format;
+/* Bytes of a row of values; a row of scales has ceil(cols / 128) * 4.  -1 for an invalid argument. */
+int64_t ssgd_mx_row_bytes(int32_t fmt, int64_t cols);
+/* A matrix of rows x cols, quantised along its rows (values, scales in `fmt`: rows x cols), along its columns (values_t, scales_t in
+ * `fmt_t`: the transposed matrix, cols x rows), or both from one read; the outputs of a direction that is not wanted are NULL. */
+ssgd_status ssgd_mx_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t pitch, int32_t fmt, void *values,
+                             void *scales, int32_t fmt_t, void *values_t, void *scales_t, void *hip_stream);
+/* The values read back (exact in fp32; in bf16 too, but for results outside the normal numbers). */
+ssgd_status ssgd_mx_dequantize(const void *values, const void *scales, int32_t fmt, int64_t rows, int64_t cols, void *out,
+                               int32_t dtype, int64_t pitch, void *hip_stream);
+
+/* Root-mean-square norm of rows of d columns with the residual's addition:
+ *   s = x + residual (rounded to dtype; without a residual s = x),  rstd = (mean of s^2 + eps)^(-1/2),  y = s rstd weight
+ * x, residual, sum and y have `dtype`, weight weight_dtype (d contiguous elements).  sum receives s and may be x or residual itself (same pitch); it
+ * is given exactly when a residual is.  Output: either y, or values and scales (16-byte aligned), the rows quantised to SSGD_MX_FP8 (without
+ * a rounding to dtype in between).  rstd (fp32, one per row) is for the backward pass.  1 <= d < 2^30; sums in fp32 and fp64. */
+ssgd_status ssgd_rmsnorm(const void *x, int64_t x_pitch, const void *residual, int64_t residual_pitch, const void *weight, int32_t dtype,
+                         int32_t weight_dtype, int64_t rows, int64_t d, double eps, void *sum, int64_t sum_pitch, void *y, int64_t y_pitch,
+                         void *values, void *scales, float *rstd, void *hip_stream);
+/* Its gradients, from s and rstd of the forward pass: dx (the gradient of x and of the residual alike) and dweight (fp32, nullable)
+ *   g = dy weight,  dx = rstd (g - s rstd mean(g s rstd)) + dsum,  dweight = sum over rows of dy s rstd
+ * dsum (nullable): the gradient that reaches s past the norm.  dx may be dy, or dsum, itself (same pitch).  An output in 8 bits has the
+ * gradient of the one before rounding.  work: ssgd_rmsnorm_work_floats floats, 16-byte aligned, used when dweight is given. */
+int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d);
+ssgd_status ssgd_rmsnorm_backward(const void *dy, int64_t dy_pitch, const void *s, int64_t s_pitch, const void *weight, int32_t dtype,
+                                  int32_t weight_dtype, const float *rstd, const void *dsum, int64_t dsum_pitch, int64_t rows, int64_t d,
+                                  void *dx, int64_t dx_pitch, float *dweight, float *work, void *hip_stream);
 
 /* AdamW over many tensors at once.  For every element, with the gradient g, the update's number t and
  *   g' = g c,   c = min(1, max_norm / (norm + 1e-6)),   norm = (sum of g^2 over all tensors)^(1/2)

@@ -257,7 +257,7 @@ ssgd_status ssgd_adamw_create(int32_t tensors, const int64_t* sizes, float* cons
             return op_fail(SSGD_EINVAL, "adamw: betas in [0, 1), eps > 0, max_norm >= 0, state_bits 8 or 32");
         if (total > 0 && (!m || !v || !aligned(m, 16) || !aligned(v, 16))) return op_fail(SSGD_EINVAL, "adamw: m and v must be 16-byte aligned device arrays");
         if (total > 0 && o.state_bits == 8 && (!m_scale || !v_scale)) return op_fail(SSGD_EINVAL, "adamw: 8-bit moments need m_scale and v_scale");
-        if (total / kPiece + tensors > INT32_MAX) return op_fail(SSGD_EINVAL, "adamw: too many elements");
+        if (total / kPiece + tensors > kMostBlocks) return op_fail(SSGD_EINVAL, "adamw: too many elements");
         for (int32_t k = 0; k < tensors; ++k) {
             if (sizes[k] > 0 && (!params[k] || !aligned(params[k], 4) || (copies && !aligned(copies[k], 2)))) return op_fail(SSGD_EINVAL, "adamw: a parameter pointer is null or misaligned");
             if (!std::isfinite(weight_decay[k])) return op_fail(SSGD_EINVAL, "adamw: a weight decay is no number");

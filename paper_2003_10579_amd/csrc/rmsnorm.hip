@@ -1,0 +1,372 @@
+// Root-mean-square norm of rows with the residual's addition, output as it is or microscaled in 8 bits, and its gradients.
+//
+//   s = x + residual (rounded to the rows' type: what the stream keeps is what is normalised, forward and backward)
+//   rstd = (mean s^2 + eps)^(-1/2),  y = (s rstd) w
+//   dx = rstd (g - xhat mean(g xhat)) + dsum,  g = dy w,  xhat = s rstd;    dw = sum over rows of dy xhat
+//
+// About 8 operations per element forward, 12 backward: bound by memory.  A row stays in the registers of 64, 256 or 1024 threads, eight
+// or sixteen columns each, between the sum of squares and the output, so it is read once; the threads go on to further rows with
+// their part of w, and backward with their part of dw, kept.  Rows of more than 16384 columns are read a second time instead.
+#include <cmath>
+
+#include "ops.hpp"
+
+using namespace ssgd;
+
+namespace {
+
+constexpr int kMostKept = 16384;      // columns that fit the registers of 1024 threads
+constexpr int kTeams = 1024;          // rows at work at a time, and partial sums of dw
+
+struct Forward {
+    const void *x, *residual, *w;
+    void *sum, *y;
+    uint8_t *values, *scales;
+    float* rstd;
+    int64_t rows, x_pitch, residual_pitch, sum_pitch, y_pitch, row_bytes, scale_bytes;
+    int32_t d, w_bf16, wide_x, wide_residual, wide_sum, wide_y, wide_w;
+    float eps;
+};
+
+struct Backward {
+    const void *dy, *s, *w, *dsum;
+    const float* rstd;
+    void* dx;
+    float* partial;          // [teams][d], nullptr: dw is not wanted
+    int64_t rows, dy_pitch, s_pitch, dsum_pitch, dx_pitch, teams;
+    int32_t d, w_bf16, wide_dy, wide_s, wide_dsum, wide_dx, wide_w;
+};
+
+// Sum over the threads of a row: across lanes in fp64, so that all that is left of the order is a thread's own few terms.
+template <int LANES>
+__device__ __forceinline__ double team_sum(double x, double* part) {
+    x = wave_sum(x);
+    if constexpr (LANES > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0.0;
+#pragma unroll
+        for (int q = 0; q < LANES / 64; ++q) x += part[q];
+        __syncthreads();
+    }
+    return x;
+}
+
+__device__ __forceinline__ void load_weight(const void* w, int bf16, int wide, int col, int d, float (&x)[8]) {
+    if (bf16) load_vec<8>(static_cast<const bf16_t*>(w) + col, wide, d - col, x);
+    else load_vec<8>(static_cast<const float*>(w) + col, wide, d - col, x);
+}
+
+__device__ __forceinline__ float as_stored(const float*, float x) { return x; }
+__device__ __forceinline__ float as_stored(const bf16_t*, float x) { return bf16_to_f32(f32_to_bf16(x)); }
+
+// Eight columns of the stream: the sum, rounded as it is stored, and stored.
+template <typename T>
+__device__ __forceinline__ void take_sum(const Forward& a, int64_t row, int col, float (&s)[8]) {
+    load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.wide_x, a.d - col, s);
+    if (a.residual != nullptr) {
+        float r[8];
+        load_vec<8>(static_cast<const T*>(a.residual) + row * a.residual_pitch + col, a.wide_residual, a.d - col, r);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s[q] = as_stored(static_cast<const T*>(nullptr), s[q] + r[q]);
+        store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.wide_sum, a.d - col, s);
+    }
+}
+
+template <typename T, bool FP8>
+__device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, const float (&s)[8], float rstd, const float (&w)[8]) {
+    float y[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) y[q] = (s[q] * rstd) * w[q];
+    if constexpr (FP8) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(y[q]));
+        const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
+        *reinterpret_cast<words2*>(a.values + row * a.row_bytes + col) = mx_pack_fp8(y, byte);
+        if ((threadIdx.x & 3) == 0) a.scales[row * a.scale_bytes + col / kMxBlock] = (uint8_t)byte;
+    } else {
+        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, a.wide_y, a.d - col, y);
+    }
+}
+
+__device__ __forceinline__ float inverse_root(double sum, const Forward& a) { return 1.0f / sqrtf((float)(sum / a.d) + a.eps); }
+
+template <typename T, bool FP8, int LANES, int NV>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forward a) {
+    constexpr int kRows = LANES == 64 ? 4 : 1;         // teams of a workgroup
+    __shared__ double part[LANES / 64];
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t team = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES, teams = (int64_t)gridDim.x * kRows;
+    const int end = FP8 ? (int)mx_padded(a.d) : a.d;
+    float w[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, a.wide_w, (v * LANES + lane) * 8, a.d, w[v]);
+    for (int64_t row = team; row < a.rows; row += teams) {
+        float s[NV][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            take_sum<T>(a, row, (v * LANES + lane) * 8, s[v]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += s[v][q] * s[v][q];
+        }
+        const float rstd = inverse_root(team_sum<LANES>((double)sum, part), a);
+        if (lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if ((v * LANES + lane) * 8 < end) store_normed<T, FP8>(a, row, (v * LANES + lane) * 8, s[v], rstd, w[v]);
+    }
+}
+
+// Rows that registers do not hold: a second read, of the sum (its own threads have written it) or of x.
+template <typename T, bool FP8>
+__global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
+    __shared__ double part[16];
+    const int64_t end = FP8 ? mx_padded(a.d) : (int64_t)a.d;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        double sum = 0.0;
+        for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
+            float s[8];
+            take_sum<T>(a, row, (int)col, s);
+            float few = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) few += s[q] * s[q];
+            sum += few;
+        }
+        const float rstd = inverse_root(team_sum<1024>(sum, part), a);
+        if (threadIdx.x == 0) a.rstd[row] = rstd;
+        for (int64_t col = threadIdx.x * 8; col < end; col += 8192) {
+            float s[8], w[8];
+            if (a.residual != nullptr) load_vec<8>(static_cast<const T*>(a.sum) + row * a.sum_pitch + col, a.wide_sum, a.d - col, s);
+            else load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.wide_x, a.d - col, s);
+            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+            store_normed<T, FP8>(a, row, (int)col, s, rstd, w);
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_dx(const Backward& a, int64_t row, int64_t col, const float (&dy)[8], const float (&xhat)[8], const float (&w)[8], float rstd,
+                                         float c) {
+    float dx[8], more[8];
+    if (a.dsum != nullptr) load_vec<8>(static_cast<const T*>(a.dsum) + row * a.dsum_pitch + col, a.wide_dsum, a.d - col, more);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        dx[q] = rstd * (dy[q] * w[q] - xhat[q] * c);
+        if (a.dsum != nullptr) dx[q] += more[q];
+    }
+    store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, a.wide_dx, a.d - col, dx);
+}
+
+template <typename T, int LANES, int NV>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Backward a) {
+    constexpr int kRows = LANES == 64 ? 4 : 1;
+    __shared__ double part[LANES / 64];
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t team = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    float w[NV][8], dw[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        load_weight(a.w, a.w_bf16, a.wide_w, (v * LANES + lane) * 8, a.d, w[v]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) dw[v][q] = 0.0f;
+    }
+    for (int64_t row = team; row < a.rows; row += a.teams) {
+        float dy[NV][8], xhat[NV][8];
+        const float rstd = a.rstd[row];
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * LANES + lane) * 8;
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy[v]);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, xhat[v]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                xhat[v][q] *= rstd;
+                sum += dy[v][q] * w[v][q] * xhat[v][q];
+                dw[v][q] += dy[v][q] * xhat[v][q];
+            }
+        }
+        const float c = (float)(team_sum<LANES>((double)sum, part) / a.d);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * LANES + lane) * 8;
+            if (col < a.d) store_dx<T>(a, row, col, dy[v], xhat[v], w[v], rstd, c);
+        }
+    }
+    if (a.partial != nullptr && team < a.teams) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int col = (v * LANES + lane) * 8;
+            store_vec<8>(a.partial + team * a.d + col, a.d % 4 == 0, a.d - col, dw[v]);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
+    __shared__ double part[16];
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < a.rows; row += a.teams) {
+        const float rstd = a.rstd[row];
+        double sum = 0.0;
+        for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
+            float dy[8], s[8], w[8];
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, s);
+            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+            float few = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) few += dy[q] * w[q] * (s[q] * rstd);
+            sum += few;
+        }
+        const float c = (float)(team_sum<1024>(sum, part) / a.d);
+        for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
+            float dy[8], s[8], w[8];
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, s);
+            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q] *= rstd;
+            store_dx<T>(a, row, col, dy, s, w, rstd, c);
+            if (a.partial == nullptr) continue;
+            float* to = a.partial + (int64_t)blockIdx.x * a.d + col;
+            const bool wide = a.d % 4 == 0;
+            float dw[8];
+            if (first) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) dw[q] = 0.0f;
+            } else load_vec<8>(to, wide, a.d - col, dw);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) dw[q] += dy[q] * s[q];
+            store_vec<8>(to, wide, a.d - col, dw);
+        }
+        first = false;
+    }
+}
+
+// dw of 64 columns: sixteen waves add every sixteenth partial sum, in fp64, and the first adds those.
+__global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int64_t teams, int32_t d, float* dw) {
+    __shared__ double part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    double sum = 0.0;
+    if (col < d)
+        for (int64_t t = wave; t < teams; t += 16) sum += (double)partial[t * d + col];
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && col < d) {
+#pragma unroll
+        for (int q = 1; q < 16; ++q) sum += part[q][lane];
+        dw[col] = (float)sum;
+    }
+}
+
+int lanes_for(int64_t d) { return d <= 1024 ? 64 : (d <= 4096 ? 256 : 1024); }
+
+template <typename T, bool FP8>
+void launch_forward(const Forward& a, hipStream_t s) {
+    const int lanes = lanes_for(a.d), rows = lanes == 64 ? 4 : 1;
+    int64_t blocks = (a.rows + rows - 1) / rows;
+    const int64_t most = lanes == 1024 ? 512 : 2048;     // as many as are resident: the next rows find w in registers
+    if (blocks > most) blocks = most;
+    const dim3 grid((unsigned)blocks), group(lanes == 64 ? 256 : lanes);
+    if (a.d > kMostKept) hipLaunchKernelGGL((forward_long_kernel<T, FP8>), grid, dim3(1024), 0, s, a);
+    else if (a.d <= 512) hipLaunchKernelGGL((forward_kernel<T, FP8, 64, 1>), grid, group, 0, s, a);
+    else if (a.d <= 1024) hipLaunchKernelGGL((forward_kernel<T, FP8, 64, 2>), grid, group, 0, s, a);
+    else if (a.d <= 2048) hipLaunchKernelGGL((forward_kernel<T, FP8, 256, 1>), grid, group, 0, s, a);
+    else if (a.d <= 4096) hipLaunchKernelGGL((forward_kernel<T, FP8, 256, 2>), grid, group, 0, s, a);
+    else if (a.d <= 8192) hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 1>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 2>), grid, group, 0, s, a);
+}
+
+// Rows at work at a time: the partial sums of dw are written and read once more, 8 bytes a column each.
+int64_t teams_for(int64_t rows, int64_t d) {
+    const int64_t most = lanes_for(d) == 1024 ? 512 : kTeams;
+    return rows < most ? rows : most;
+}
+
+template <typename T>
+void launch_backward(const Backward& a, hipStream_t s) {
+    const int lanes = lanes_for(a.d), rows = lanes == 64 ? 4 : 1;
+    const dim3 grid((unsigned)((a.teams + rows - 1) / rows)), group(lanes == 64 ? 256 : lanes);
+    if (a.d > kMostKept) hipLaunchKernelGGL((backward_long_kernel<T>), grid, dim3(1024), 0, s, a);
+    else if (a.d <= 512) hipLaunchKernelGGL((backward_kernel<T, 64, 1>), grid, group, 0, s, a);
+    else if (a.d <= 1024) hipLaunchKernelGGL((backward_kernel<T, 64, 2>), grid, group, 0, s, a);
+    else if (a.d <= 2048) hipLaunchKernelGGL((backward_kernel<T, 256, 1>), grid, group, 0, s, a);
+    else if (a.d <= 4096) hipLaunchKernelGGL((backward_kernel<T, 256, 2>), grid, group, 0, s, a);
+    else if (a.d <= 8192) hipLaunchKernelGGL((backward_kernel<T, 1024, 1>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((backward_kernel<T, 1024, 2>), grid, group, 0, s, a);
+}
+
+bool shape_ok(int32_t dtype, int32_t w_dtype, int64_t rows, int64_t d) {
+    return dtype_ok(dtype) && dtype_ok(w_dtype) && rows >= 0 && rows < (int64_t(1) << 40) && d >= 1 && d < (int64_t(1) << 30);
+}
+bool there(const void* p, int32_t dtype) { return p != nullptr && aligned(p, (uintptr_t)dtype_bytes(dtype)); }
+int wide(const void* p, int64_t pitch) { return aligned(p, 16) && pitch % 8 == 0 ? 1 : 0; }
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+ssgd_status ssgd_rmsnorm(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, const void* weight, int32_t dtype, int32_t weight_dtype,
+                         int64_t rows, int64_t d, double eps, void* sum, int64_t sum_pitch, void* y, int64_t y_pitch, void* values, void* scales, float* rstd,
+                         void* hip_stream) {
+    return op_entry([&]() -> ssgd_status {
+        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm: types of the enumeration, rows of zero or more, 1 <= d < 2^30");
+        if (!(eps >= 0) || !std::isfinite(eps)) return op_fail(SSGD_EINVAL, "rmsnorm: eps of zero or more");
+        if (rows == 0) return SSGD_OK;
+        if (!there(x, dtype) || !there(weight, weight_dtype) || !there(rstd, SSGD_F32) || x_pitch < d) return op_fail(SSGD_EINVAL, "rmsnorm: x, weight and rstd, pitch >= d");
+        if ((residual != nullptr) != (sum != nullptr)) return op_fail(SSGD_EINVAL, "rmsnorm: a residual and its sum go together");
+        if (residual != nullptr && (!there(residual, dtype) || !there(sum, dtype) || residual_pitch < d || sum_pitch < d)) return op_fail(SSGD_EINVAL, "rmsnorm: residual and sum, pitch >= d");
+        if ((y != nullptr) == (values != nullptr) || (values != nullptr) != (scales != nullptr)) return op_fail(SSGD_EINVAL, "rmsnorm: either y, or values and scales");
+        if (y != nullptr && (!there(y, dtype) || y_pitch < d)) return op_fail(SSGD_EINVAL, "rmsnorm: y, pitch >= d");
+        if (values != nullptr && (!aligned(values, 16) || !aligned(scales, 16))) return op_fail(SSGD_EINVAL, "rmsnorm: values and scales are 16-byte aligned");
+        Forward a{};
+        a.x = x; a.residual = residual; a.w = weight; a.sum = sum; a.y = y;
+        a.values = static_cast<uint8_t*>(values); a.scales = static_cast<uint8_t*>(scales); a.rstd = rstd;
+        a.rows = rows; a.x_pitch = x_pitch; a.residual_pitch = residual_pitch; a.sum_pitch = sum_pitch; a.y_pitch = y_pitch;
+        a.row_bytes = mx_row_bytes(SSGD_MX_FP8, d); a.scale_bytes = mx_padded(d) / kMxBlock;
+        a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16; a.eps = (float)eps;
+        a.wide_x = wide(x, x_pitch); a.wide_residual = wide(residual, residual_pitch); a.wide_sum = wide(sum, sum_pitch); a.wide_y = wide(y, y_pitch); a.wide_w = wide(weight, 0);
+        const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+        if (dtype == SSGD_F32) { if (values) launch_forward<float, true>(a, s); else launch_forward<float, false>(a, s); }
+        else { if (values) launch_forward<bf16_t, true>(a, s); else launch_forward<bf16_t, false>(a, s); }
+        return op_hip(hipGetLastError(), "rmsnorm");
+    });
+}
+
+int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d) { return shape_ok(SSGD_F32, SSGD_F32, rows, d) ? teams_for(rows, d) * d : -1; }
+
+ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* s, int64_t s_pitch, const void* weight, int32_t dtype, int32_t weight_dtype,
+                                  const float* rstd, const void* dsum, int64_t dsum_pitch, int64_t rows, int64_t d, void* dx, int64_t dx_pitch, float* dweight,
+                                  float* work, void* hip_stream) {
+    return op_entry([&]() -> ssgd_status {
+        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm backward: types of the enumeration, rows of zero or more, 1 <= d < 2^30");
+        if (dweight != nullptr && (!aligned(dweight, 4) || (rows > 0 && (!work || !aligned(work, 16))))) return op_fail(SSGD_EINVAL, "rmsnorm backward: dweight needs a 16-byte aligned work area");
+        if (rows > 0) {
+            if (!there(dy, dtype) || !there(s, dtype) || !there(weight, weight_dtype) || !there(rstd, SSGD_F32) || !there(dx, dtype) || dy_pitch < d || s_pitch < d || dx_pitch < d)
+                return op_fail(SSGD_EINVAL, "rmsnorm backward: dy, s, weight, rstd and dx, pitch >= d");
+            if (dsum != nullptr && (!there(dsum, dtype) || dsum_pitch < d)) return op_fail(SSGD_EINVAL, "rmsnorm backward: dsum, pitch >= d");
+        }
+        Backward a{};
+        a.dy = dy; a.s = s; a.w = weight; a.dsum = dsum; a.rstd = rstd; a.dx = dx; a.partial = dweight ? work : nullptr;
+        a.rows = rows; a.dy_pitch = dy_pitch; a.s_pitch = s_pitch; a.dsum_pitch = dsum_pitch; a.dx_pitch = dx_pitch; a.teams = teams_for(rows, d);
+        a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16;
+        a.wide_dy = wide(dy, dy_pitch); a.wide_s = wide(s, s_pitch); a.wide_dsum = wide(dsum, dsum_pitch); a.wide_dx = wide(dx, dx_pitch); a.wide_w = wide(weight, 0);
+        const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        if (rows > 0) {
+            if (dtype == SSGD_F32) launch_backward<float>(a, stream); else launch_backward<bf16_t>(a, stream);
+        }
+        ssgd_status st = op_hip(hipGetLastError(), "rmsnorm backward");
+        if (st == SSGD_OK && dweight != nullptr) {
+            hipLaunchKernelGGL(weight_kernel, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, stream, work, a.teams, (int32_t)d, dweight);
+            st = op_hip(hipGetLastError(), "rmsnorm backward");
+        }
+        return st;
+    });
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -16,6 +16,8 @@ EXP, SHIFTED_EXP, PARETO, TABLE = 0, 1, 2, 3
 OK, EINVAL, ENOMEM, EDEVICE, ESTATE = 0, 1, 2, 3, 4
 _VARIANTS = {"k_sync": K_SYNC, "k_batch_sync": K_BATCH_SYNC, "k_async": K_ASYNC, "k_batch_async": K_BATCH_ASYNC}
 F32, BF16 = 0, 1
+MX_FP4, MX_FP8 = 0, 1
+_FORMATS = {"fp4": MX_FP4, "fp8": MX_FP8}
 _KINDS = {"lsq": LSQ, "softmax": SOFTMAX, "mlp2": MLP2}
 
 EXPORTS = [
@@ -25,6 +27,8 @@ EXPORTS = [
     "ssgd_full_gradient", "ssgd_full_gradient_static",
     "ssgd_runtime_mc", "ssgd_debug_delays", "ssgd_debug_batch", "ssgd_stream_read_rate", "ssgd_last_error",
     "ssgd_last_kernel_ms", "ssgd_adamw_state_elements", "ssgd_adamw_create", "ssgd_adamw_step", "ssgd_adamw_destroy",
+    "ssgd_mx_row_bytes", "ssgd_mx_quantize", "ssgd_mx_dequantize",
+    "ssgd_rmsnorm", "ssgd_rmsnorm_work_floats", "ssgd_rmsnorm_backward",
     "ssgd_destroy",
 ]
 
@@ -115,6 +119,15 @@ def lib():
         L.ssgd_adamw_create.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(AdamWOptions)] + [C.c_void_p] * 5
         L.ssgd_adamw_step.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_double, C.c_int64, C.c_void_p, C.c_void_p]
         L.ssgd_adamw_destroy.argtypes = [C.c_void_p]
+        i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
+        L.ssgd_mx_row_bytes.restype = i64
+        L.ssgd_mx_row_bytes.argtypes = [i32, i64]
+        L.ssgd_mx_quantize.argtypes = [ptr, i32, i64, i64, i64, i32, ptr, ptr, i32, ptr, ptr, ptr]
+        L.ssgd_mx_dequantize.argtypes = [ptr, ptr, i32, i64, i64, ptr, i32, i64, ptr]
+        L.ssgd_rmsnorm.argtypes = [ptr, i64, ptr, i64, ptr, i32, i32, i64, i64, C.c_double, ptr, i64, ptr, i64, ptr, ptr, ptr, ptr]
+        L.ssgd_rmsnorm_work_floats.restype = i64
+        L.ssgd_rmsnorm_work_floats.argtypes = [i64, i64]
+        L.ssgd_rmsnorm_backward.argtypes = [ptr, i64, ptr, i64, ptr, i32, i32, ptr, ptr, i64, i64, i64, ptr, i64, ptr, ptr, ptr]
         _lib = L
     return _lib
 
@@ -391,3 +404,133 @@ class AdamW:
 
     def __del__(self):
         self.close()
+
+
+def _matrix(x, what):
+    """(device, dtype, rows, cols, pitch) of a matrix with contiguous rows."""
+    _need(x.is_cuda and x.dim() == 2, f"{what}: a matrix on the GPU is wanted")
+    rows, cols = x.shape
+    pitch = x.stride(0) if rows > 1 else cols
+    _need((cols <= 1 or x.stride(1) == 1) and pitch >= cols, f"{what}: rows have to be contiguous")
+    return x.device, _dtype(x.dtype), rows, cols, pitch
+
+
+class MxTensor:
+    """A microscaled matrix: `values` (uint8, rows x bytes; two E2M1 or one E4M3 number to a byte) and `scales` (uint8, 2^(byte - 127) per
+    32 columns), both padded with zeros to a multiple of 128 columns.  `format` is "fp4" or "fp8", `shape` (rows, cols)."""
+
+    __slots__ = ("values", "scales", "format", "shape")
+
+    def __init__(self, values, scales, format, shape):
+        self.values, self.scales, self.format, self.shape = values, scales, format, shape
+
+    @classmethod
+    def empty(cls, rows, cols, format, device):
+        import torch
+        _need(format in _FORMATS, "mx: the format is 'fp4' or 'fp8'")
+        wide = -(-cols // 128) * 128
+        return cls(torch.empty((rows, wide // 2 if format == "fp4" else wide), dtype=torch.uint8, device=device),
+                   torch.empty((rows, wide // 32), dtype=torch.uint8, device=device), format, (rows, cols))
+
+
+def mx_quantize(x, format="fp4"):
+    """The rows of a matrix (float32 or bfloat16) as an MxTensor."""
+    dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize")
+    q = MxTensor.empty(rows, cols, format, dev)
+    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], q.values.data_ptr(), q.scales.data_ptr(),
+          0, None, None)
+    return q
+
+
+def mx_quantize_transposed(x, format="fp4"):
+    """The columns of a matrix as the rows of an MxTensor."""
+    dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize_transposed")
+    q = MxTensor.empty(cols, rows, format, dev)
+    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, 0, None, None, _FORMATS[format], q.values.data_ptr(),
+          q.scales.data_ptr())
+    return q
+
+
+def mx_quantize_both(x, format="fp4", format_transposed="fp4"):
+    """(mx_quantize(x), mx_quantize_transposed(x)) from one read of x."""
+    dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize_both")
+    q, t = MxTensor.empty(rows, cols, format, dev), MxTensor.empty(cols, rows, format_transposed, dev)
+    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], q.values.data_ptr(), q.scales.data_ptr(),
+          _FORMATS[format_transposed], t.values.data_ptr(), t.scales.data_ptr())
+    return q, t
+
+
+def _mx(q, what):
+    """An MxTensor whose arrays are as the library lays them out."""
+    _need(isinstance(q, MxTensor) and q.format in _FORMATS, f"{what}: an MxTensor is wanted")
+    rows, cols = q.shape
+    wide = -(-cols // 128) * 128
+    _need(q.values.is_cuda and q.values.is_contiguous() and q.scales.is_contiguous() and q.scales.device == q.values.device and
+          q.values.element_size() == q.scales.element_size() == 1 and
+          tuple(q.values.shape) == (rows, wide // 2 if q.format == "fp4" else wide) and tuple(q.scales.shape) == (rows, wide // 32),
+          f"{what}: values and scales do not have the layout of {rows} x {cols}")
+    return q.values.device
+
+
+def mx_dequantize(q, dtype=None):
+    """The values of an MxTensor as a matrix of `dtype` (float32 unless it is given, or bfloat16)."""
+    import torch
+    dev = _mx(q, "mx_dequantize")
+    out = torch.empty(q.shape, dtype=dtype or torch.float32, device=dev)
+    _call(lib().ssgd_mx_dequantize, dev, q.values.data_ptr(), q.scales.data_ptr(), _FORMATS[q.format], q.shape[0], q.shape[1], out.data_ptr(),
+          _dtype(out.dtype), q.shape[1])
+    return out
+
+
+def _beside(t, x, what):
+    """(pointer, pitch) of a matrix of the shape, type and device of x, or of none."""
+    if t is None:
+        return None, 0
+    dev, kind, rows, cols, pitch = _matrix(t, what)
+    _need(dev == x.device and t.dtype == x.dtype and t.shape == x.shape, f"{what}: the shape, type and device of the first matrix are wanted")
+    return t.data_ptr(), pitch
+
+
+def _weight(w, x, what):
+    _need(w.dim() == 1 and w.numel() == x.shape[1] and w.is_contiguous() and w.device == x.device, f"{what}: a contiguous weight per column is wanted")
+    return w.data_ptr(), _dtype(w.dtype)
+
+
+def rmsnorm(x, weight, residual=None, eps=1e-6, output=None):
+    """(y, s, rstd) of the root-mean-square norm of the rows of s = x + residual (s = x without one).  y has x's type or, with
+    output="fp8", is an MxTensor for the product behind it; s and rstd are what rmsnorm_backward takes."""
+    import torch
+    dev, kind, rows, d, pitch = _matrix(x, "rmsnorm")
+    _need(output in (None, "fp8"), "rmsnorm: the output is None (x's type) or 'fp8'")
+    w, w_kind = _weight(weight, x, "rmsnorm")
+    r, r_pitch = _beside(residual, x, "rmsnorm")
+    total = x if residual is None else torch.empty((rows, d), dtype=x.dtype, device=dev)
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    if output is None:
+        y = torch.empty((rows, d), dtype=x.dtype, device=dev)
+        to = (y.data_ptr(), d, None, None)
+    else:
+        y = MxTensor.empty(rows, d, "fp8", dev)
+        to = (None, 0, y.values.data_ptr(), y.scales.data_ptr())
+    _call(lib().ssgd_rmsnorm, dev, x.data_ptr(), pitch, r, r_pitch, w, kind, w_kind, rows, d, eps, None if residual is None else total.data_ptr(), d, *to,
+          rstd.data_ptr())
+    return y, total, rstd
+
+
+def rmsnorm_backward(dy, s, weight, rstd, dsum=None):
+    """(dx, dweight) from the gradient dy of the norm's output and, where there is one, dsum that reaches s past it.  dx is the
+    gradient of x and of the residual; dweight is float32."""
+    import torch
+    dev, kind, rows, d, pitch = _matrix(dy, "rmsnorm_backward")
+    w, w_kind = _weight(weight, dy, "rmsnorm_backward")
+    s_at, s_pitch = _beside(s, dy, "rmsnorm_backward")
+    _need(rstd.dtype == torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous() and rstd.device == dev, "rmsnorm_backward: one float32 rstd per row is wanted")
+    more, more_pitch = _beside(dsum, dy, "rmsnorm_backward")
+    dx = torch.empty((rows, d), dtype=dy.dtype, device=dev)
+    dw = torch.empty(d, dtype=torch.float32, device=dev)
+    floats = lib().ssgd_rmsnorm_work_floats(rows, d)
+    _need(floats >= 0, "rmsnorm_backward: 1 <= columns < 2^30")
+    work = torch.empty(floats, dtype=torch.float32, device=dev)
+    _call(lib().ssgd_rmsnorm_backward, dev, dy.data_ptr(), pitch, s_at, s_pitch, w, kind, w_kind, rstd.data_ptr(), more, more_pitch, rows, d, dx.data_ptr(), d,
+          dw.data_ptr(), work.data_ptr())
+    return dx, dw
