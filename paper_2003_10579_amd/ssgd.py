@@ -28,6 +28,7 @@ EXPORTS = [
     "ssgd_runtime_mc", "ssgd_debug_delays", "ssgd_debug_batch", "ssgd_stream_read_rate", "ssgd_last_error",
     "ssgd_last_kernel_ms", "ssgd_adamw_state_elements", "ssgd_adamw_create", "ssgd_adamw_step", "ssgd_adamw_destroy",
     "ssgd_mx_row_bytes", "ssgd_mx_quantize", "ssgd_mx_dequantize",
+    "ssgd_mx_matmul", "ssgd_mx_linear_work_bytes", "ssgd_mx_linear",
     "ssgd_rmsnorm", "ssgd_rmsnorm_work_floats", "ssgd_rmsnorm_backward",
     "ssgd_destroy",
 ]
@@ -124,6 +125,10 @@ def lib():
         L.ssgd_mx_row_bytes.argtypes = [i32, i64]
         L.ssgd_mx_quantize.argtypes = [ptr, i32, i64, i64, i64, i32, ptr, ptr, i32, ptr, ptr, ptr]
         L.ssgd_mx_dequantize.argtypes = [ptr, ptr, i32, i64, i64, ptr, i32, i64, ptr]
+        L.ssgd_mx_matmul.argtypes = [ptr, ptr, i32, i64, ptr, ptr, i64, i64, ptr, i32, i64, ptr]
+        L.ssgd_mx_linear_work_bytes.restype = i64
+        L.ssgd_mx_linear_work_bytes.argtypes = [i32, i64, i64]
+        L.ssgd_mx_linear.argtypes = [ptr, i32, i64, i64, i32, ptr, ptr, i64, i64, ptr, i32, i64, ptr, ptr]
         L.ssgd_rmsnorm.argtypes = [ptr, i64, ptr, i64, ptr, i32, i32, i64, i64, C.c_double, ptr, i64, ptr, i64, ptr, ptr, ptr, ptr]
         L.ssgd_rmsnorm_work_floats.restype = i64
         L.ssgd_rmsnorm_work_floats.argtypes = [i64, i64]
@@ -479,6 +484,34 @@ def mx_dequantize(q, dtype=None):
     out = torch.empty(q.shape, dtype=dtype or torch.float32, device=dev)
     _call(lib().ssgd_mx_dequantize, dev, q.values.data_ptr(), q.scales.data_ptr(), _FORMATS[q.format], q.shape[0], q.shape[1], out.data_ptr(),
           _dtype(out.dtype), q.shape[1])
+    return out
+
+
+def mx_matmul(a, b, dtype=None):
+    """a b^T of two MxTensors with equal numbers of columns, a in either format, b in "fp4", as a matrix of `dtype` (bfloat16 unless
+    it is given, or float32)."""
+    import torch
+    dev = _mx(a, "mx_matmul")
+    _need(_mx(b, "mx_matmul") == dev and b.format == "fp4" and a.shape[1] == b.shape[1], "mx_matmul: b is an 'fp4' MxTensor with a's columns, on its device")
+    (M, K), N = a.shape, b.shape[0]
+    out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=dev)
+    _call(lib().ssgd_mx_matmul, dev, a.values.data_ptr(), a.scales.data_ptr(), _FORMATS[a.format], M, b.values.data_ptr(), b.scales.data_ptr(), N, K,
+          out.data_ptr(), _dtype(out.dtype), N)
+    return out
+
+
+def mx_linear(x, w, format="fp8", dtype=None):
+    """x w^T for rows x (float32 or bfloat16), quantised to `format` on the way, and an "fp4" MxTensor w (outputs x inputs), as a
+    matrix of `dtype` (x's unless it is given)."""
+    import torch
+    dev, kind, M, K, pitch = _matrix(x, "mx_linear")
+    _need(format in _FORMATS, "mx_linear: the format is 'fp4' or 'fp8'")
+    _need(_mx(w, "mx_linear") == dev and w.format == "fp4" and w.shape[1] == K, "mx_linear: w is an 'fp4' MxTensor with x's columns, on its device")
+    N, f = w.shape[0], _FORMATS[format]
+    out = torch.empty((M, N), dtype=dtype or x.dtype, device=dev)
+    work = torch.empty(lib().ssgd_mx_linear_work_bytes(f, M, K), dtype=torch.uint8, device=dev)
+    _call(lib().ssgd_mx_linear, dev, x.data_ptr(), kind, pitch, M, f, w.values.data_ptr(), w.scales.data_ptr(), N, K, out.data_ptr(), _dtype(out.dtype), N,
+          work.data_ptr())
     return out
 
 

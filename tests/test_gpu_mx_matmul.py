@@ -1,0 +1,194 @@
+"""The product of microscaled matrices against the same values in 64 bits, through the public entry points."""
+import numpy as np
+import pytest
+
+import mx_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2003_10579_amd import ssgd
+    assert torch.cuda.is_available(), "this test needs the GPU"
+    ssgd.lib()
+    return torch, ssgd
+
+
+def _host(x):
+    return x.double().cpu().numpy()
+
+
+def _matrix(torch, rows, cols, seed):
+    """Every row at a level of its own, blocks of different sizes along it, a few large values."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * torch.exp(torch.randn(rows, 1, generator=g))
+    x = x * torch.exp(1.5 * torch.randn(1, max(1, -(-cols // 32)), generator=g)).repeat_interleave(32, 1)[:, :cols]
+    return x * (1 + 10 * (torch.rand(rows, cols, generator=g) < 0.01))
+
+
+def _close(got, a, b, fmt, dtype):
+    """a, b: the values that the operands stand for."""
+    want, size = a @ b.T, np.abs(a) @ np.abs(b).T
+    steps = -(-a.shape[1] // 128)
+    # one rounding of the running sum per 128 columns; 4 by 4 bits are exact within an instruction, of 8 by 4 bits it drops of each of 128
+    # products what is below 2^-14 of the largest (a product of 2^-7 beside 448 and -448 is lost, one of 2^-5 is not)
+    bound = (steps + 4) * 2.0 ** -24 * size + 1e-36
+    if fmt == "fp8":
+        for k in range(0, a.shape[1], 128):
+            bound += 128 * 2.0 ** -14 * np.outer(np.abs(a[:, k:k + 128]).max(1), np.abs(b[:, k:k + 128]).max(1))
+        assert np.linalg.norm(got - want) <= (1e-4 if dtype == "float32" else 2.0 ** -8) * np.linalg.norm(want)
+    # then the rounding to the output's type
+    place = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(want) + bound, 1e-38))) - (24 if dtype == "float32" else 8))
+    assert np.all(np.abs(got - want) <= bound + 1.01 * place)
+
+
+# few rows (one, two and four groups of 16, partial ones), tiles of 128 and, from 200 tiles of 256 on, of 256; contractions from one column to
+# many steps of 128, each remainder of the stages; rows of B that are no multiple of anything
+SHAPES = [(1, 1, 1), (1, 3, 5), (1, 16, 128), (1, 17, 4096), (1, 300, 3072), (2, 512, 3071), (15, 33, 129), (16, 100, 640), (17, 100, 512), (32, 40, 2200), (33, 70, 1000),
+          (61, 130, 5000), (64, 64, 8192), (65, 1, 100), (65, 127, 300), (100, 129, 129), (128, 128, 128), (129, 257, 256), (130, 130, 384), (300, 200, 512),
+          (257, 513, 640), (512, 384, 1100), (3500, 3700, 127), (3585, 3600, 300), (3700, 3500, 700), (4000, 3500, 513)]
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_product(env, shape, fmt):
+    torch, ssgd = env
+    M, N, K = shape
+    x, w = _matrix(torch, M, K, M + K), _matrix(torch, N, K, N + K + 1)
+    a, b = ssgd.mx_quantize(x.cuda(), fmt), ssgd.mx_quantize(w.cuda(), "fp4")
+    ah, bh = _host(ssgd.mx_dequantize(a)), _host(ssgd.mx_dequantize(b))
+    if M * K < 1 << 20:
+        assert np.array_equal(ah, ref.rounded(_host(x), fmt).astype(np.float32))
+    for dtype in ("float32", "bfloat16"):
+        out = ssgd.mx_matmul(a, b, getattr(torch, dtype))
+        assert out.shape == (M, N) and out.dtype == getattr(torch, dtype)
+        _close(_host(out), ah, bh, fmt, dtype)
+    assert ssgd.mx_matmul(a, b).dtype == torch.bfloat16
+    assert torch.equal(ssgd.mx_matmul(a, b), ssgd.mx_matmul(a, b))
+    # the rows quantised on the way: the same bits
+    for dtype in (torch.float32, torch.bfloat16):
+        y = x.to(dtype).cuda()
+        assert torch.equal(ssgd.mx_linear(y, b, fmt), ssgd.mx_matmul(ssgd.mx_quantize(y, fmt), b, dtype))
+    assert ssgd.mx_linear(x.cuda(), b, fmt, torch.bfloat16).dtype == torch.bfloat16
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_a_layer_forward_and_backward(env, fmt):
+    """y = x w^T, dx = dy w, dw = dy^T x by quantisation along rows and columns: each against the product of the values that its own
+    operands stand for."""
+    torch, ssgd = env
+    T, N, K = 200, 96, 160
+    x, w, dy = (_matrix(torch, *s, k).cuda() for k, s in enumerate(((T, K), (N, K), (T, N))))
+    (xq, xt), (wq, wt), (dq, dt) = ssgd.mx_quantize_both(x, fmt, "fp4"), ssgd.mx_quantize_both(w, "fp4", "fp4"), ssgd.mx_quantize_both(dy, fmt, fmt)
+    for a, b, left, right in ((xq, wq, x, w), (dq, wt, dy, w.t()), (dt, xt, dy.t(), x.t())):
+        got = _host(ssgd.mx_matmul(a, b, torch.float32))
+        _close(got, ref.rounded(_host(left), a.format), ref.rounded(_host(right), "fp4"), a.format, "float32")
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_gradients_of_a_layer_against_differences(env, fmt):
+    """With values that both formats hold exactly along rows and columns, the layer is the unquantised one: its gradients against central
+    differences of sum(dy * y), which are exact for a function linear in each argument, up to the rounding of the differences."""
+    torch, ssgd = env
+    T, N, K = 70, 40, 100
+    g = torch.Generator().manual_seed(4)
+    pick = lambda *s: torch.tensor(ref.TABLE["fp4"], dtype=torch.float32)[torch.randint(1, 8, s, generator=g)] * torch.randint(0, 2, s, generator=g).mul(2).sub(1)  # noqa: E731
+    x, w, dy = pick(T, K), pick(N, K), pick(T, N)
+    (xq, xt), (wq, wt), (dq, dt) = (ssgd.mx_quantize_both(t.cuda(), f, h) for t, f, h in ((x, fmt, "fp4"), (w, "fp4", "fp4"), (dy, fmt, fmt)))
+    y, dx, dw = (_host(ssgd.mx_matmul(a, b, torch.float32)) for a, b in ((xq, wq), (dq, wt), (dt, xt)))
+    xh, wh, dyh = _host(x), _host(w), _host(dy)
+    assert np.array_equal(y, xh @ wh.T)
+    for i, k in ((0, 0), (33, 99), (69, 50)):
+        e = np.zeros_like(xh); e[i, k] = 0.5
+        assert abs((dyh * ((xh + e) @ wh.T)).sum() - (dyh * ((xh - e) @ wh.T)).sum() - dx[i, k]) < 1e-9
+    for n, k in ((0, 0), (20, 99), (39, 31)):
+        e = np.zeros_like(wh); e[n, k] = 0.5
+        assert abs((dyh * (xh @ (wh + e).T)).sum() - (dyh * (xh @ (wh - e).T)).sum() - dw[n, k]) < 1e-9
+
+
+def test_blocks_that_are_nan_and_large_scales(env):
+    torch, ssgd = env
+    for M, N in ((3, 40), (100, 140), (3600, 3600)):
+        x, w = torch.ones(M, 300), torch.ones(N, 300)
+        x[1, 40] = float("inf")
+        w[5, 299] = float("nan")
+        for fmt in ("fp4", "fp8"):
+            out = ssgd.mx_linear(x.cuda(), ssgd.mx_quantize(w.cuda(), "fp4"), fmt).cpu()
+            assert torch.isnan(out[1]).all() and torch.isnan(out[:, 5]).all()
+            out[1], out[:, 5] = 300, 300
+            assert torch.all(out == 300)
+    # 2^120 times 2^-120, 2^100 times 2^100: finite, and past the range
+    one = torch.ones(70, 128, device="cuda")
+    small, large = ssgd.mx_quantize(one * 2.0 ** -120), ssgd.mx_quantize(one * 2.0 ** 120)
+    assert torch.all(ssgd.mx_matmul(small, large, torch.float32) == 128)
+    huge = ssgd.mx_quantize(one * 2.0 ** 100)
+    assert torch.isinf(ssgd.mx_matmul(huge, huge, torch.float32)).all()
+
+
+def test_strided_and_misaligned_outputs_and_nothing_beside_them(env):
+    """Through the C entry, with room around the rows of the output."""
+    torch, ssgd = env
+    L = ssgd.lib()
+    stream = torch.cuda.current_stream().cuda_stream
+    for M, N, K in ((1, 37, 200), (50, 130, 700), (140, 135, 300), (3500, 3601, 130)):
+        a, b = ssgd.mx_quantize(_matrix(torch, M, K, 1).cuda(), "fp8"), ssgd.mx_quantize(_matrix(torch, N, K, 2).cuda(), "fp4")
+        want = ssgd.mx_matmul(a, b, torch.float32)
+        for pad, offset in ((0, 0), (8, 4), (5, 1)):
+            room = torch.full((M + 2, N + pad), 7.0, device="cuda")
+            assert L.ssgd_mx_matmul(a.values.data_ptr(), a.scales.data_ptr(), 1, M, b.values.data_ptr(), b.scales.data_ptr(), N, K,
+                                    room[1:].data_ptr() + 4 * offset, 0, N + pad, stream) == 0
+            flat = room.reshape(-1)
+            at = N + pad + offset
+            body = flat[at:at + (M - 1) * (N + pad) + N]
+            got = torch.stack([body[i * (N + pad):i * (N + pad) + N] for i in (0, M // 2, M - 1)])
+            assert torch.equal(got, want[[0, M // 2, M - 1]])
+            assert torch.all(flat[:at] == 7) and torch.all(flat[at + (M - 1) * (N + pad) + N:] == 7)
+            assert torch.all(torch.as_strided(flat, (M - 1, pad), (N + pad, 1), at + N) == 7)      # between the rows
+
+
+def test_empty_products(env):
+    torch, ssgd = env
+    e = lambda r, c, f="fp4": ssgd.mx_quantize(torch.zeros(r, c, device="cuda"), f)  # noqa: E731
+    assert ssgd.mx_matmul(e(0, 64), e(5, 64)).shape == (0, 5) and ssgd.mx_matmul(e(5, 64), e(0, 64)).shape == (5, 0)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = ssgd.mx_matmul(e(70, 0), e(90, 0), dtype)
+        assert out.shape == (70, 90) and torch.all(out == 0)
+        assert torch.all(ssgd.mx_linear(torch.zeros(3, 0, device="cuda", dtype=dtype), e(4, 0)) == 0)
+    assert ssgd.mx_linear(torch.zeros(0, 64, device="cuda"), e(4, 64)).shape == (0, 4)
+
+
+def test_another_stream_and_a_replayed_graph_give_the_same(env):
+    torch, ssgd = env
+    x, w = _matrix(torch, 90, 900, 1).cuda().bfloat16(), ssgd.mx_quantize(_matrix(torch, 333, 900, 2).cuda(), "fp4")
+    for rows in (1, 90):
+        want = ssgd.mx_linear(x[:rows], w)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            got = ssgd.mx_linear(x[:rows], w)
+        s.synchronize()
+        assert torch.equal(want, got)
+        graph = torch.cuda.CUDAGraph()
+        y = x[:rows].clone()
+        with torch.cuda.graph(graph):
+            out = ssgd.mx_linear(y, w)
+        for k in range(3):
+            y.copy_(x[:rows] * (k + 1))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, ssgd.mx_linear(y, w))
+
+
+def test_refusals(env):
+    torch, ssgd = env
+    x = torch.zeros(4, 64, device="cuda")
+    a, b, f8 = ssgd.mx_quantize(x), ssgd.mx_quantize(torch.zeros(6, 64, device="cuda")), ssgd.mx_quantize(x, "fp8")
+    other = ssgd.mx_quantize(torch.zeros(6, 65, device="cuda"))
+    for call in (lambda: ssgd.mx_matmul(a, f8), lambda: ssgd.mx_matmul(a, other), lambda: ssgd.mx_matmul(x, b), lambda: ssgd.mx_matmul(a, x),
+                 lambda: ssgd.mx_matmul(a, b, torch.float16), lambda: ssgd.mx_linear(x, f8), lambda: ssgd.mx_linear(x, other), lambda: ssgd.mx_linear(x, b, "int8"),
+                 lambda: ssgd.mx_linear(x.half(), b), lambda: ssgd.mx_linear(x.cpu(), b), lambda: ssgd.mx_linear(x, b, "fp8", torch.float64), lambda: ssgd.mx_linear(x.t(), b)):
+        with pytest.raises(ssgd.SsgdError) as e:
+            call()
+        assert e.value.status == ssgd.EINVAL
