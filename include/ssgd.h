@@ -249,8 +249,7 @@ ssgd_status ssgd_stream_read_rate(const void *data, int64_t bytes, int32_t passe
  * `hip_stream` (a hipStream_t of that device; NULL = default stream) and nothing is awaited, allocated
  * or copied to the host unless a call says so.  Arguments are checked before anything is enqueued
  * (SSGD_EINVAL, text in ssgd_last_error(NULL)).  Rows of a matrix are contiguous and `pitch` elements
- * apart (pitch >= columns); no buffer has to be aligned beyond its element type unless that is said,
- * 16-byte aligned ones with pitches that are a multiple of 8 elements are the fast ones.  Inputs and
+ * apart (pitch >= columns); no buffer has to be aligned beyond its element type unless that is said.  Inputs and
  * outputs must not overlap unless that is said.  A result does not depend on the stream, the pitch, the
  * alignment or on other work on the device: every sum is taken in a fixed order. */
 typedef enum { SSGD_F32 = 0, SSGD_BF16 = 1 } ssgd_dtype;

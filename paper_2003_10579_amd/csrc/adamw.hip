@@ -98,10 +98,9 @@ __global__ __launch_bounds__(kThreads) void square_kernel(const Piece* pieces, i
     for (int c = blockIdx.x; c < n_pieces; c += gridDim.x) {
         const Piece w = pieces[c];
         const G* g = grads.of[w.tensor] + w.first;
-        const bool wide = (reinterpret_cast<uintptr_t>(g) & 15u) == 0;
         for (int i = threadIdx.x * 8; i < w.n; i += kThreads * 8) {
             float x[8];
-            load_vec<8>(g + i, wide, w.n - i, x);
+            load_vec<8>(g + i, w.n - i, x);
 #pragma unroll
             for (int q = 0; q < 8; ++q) sum += (double)x[q] * (double)x[q];
         }
@@ -136,9 +135,6 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, in
     if ((int)blockIdx.x >= n_pieces) return;          // no elements at all: the norm alone
     const Piece w = pieces[blockIdx.x];
     const G* g = grads.of[w.tensor] + w.first;
-    const bool wide_p = (reinterpret_cast<uintptr_t>(w.p) & 15u) == 0;
-    const bool wide_g = (reinterpret_cast<uintptr_t>(g) & (V * sizeof(G) >= 16 ? 15u : 7u)) == 0;
-    const bool wide_c = (reinterpret_cast<uintptr_t>(w.copy) & (V == 8 ? 15u : 7u)) == 0;
     const float keep = 1.0f - rule.lr * w.decay;
     // (whole blocks of the moments: lanes past the end hold zeros)
     const int end = (w.n + kStateBlock - 1) / kStateBlock * kStateBlock;
@@ -146,11 +142,11 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, in
         const int left = w.n - i;
         const int64_t at = w.state + i;
         float p[V], gr[V], m[V], v[V];
-        load_vec<V>(w.p + i, wide_p, left, p);
-        load_vec<V>(g + i, wide_g, left, gr);
+        load_vec<V>(w.p + i, left, p);
+        load_vec<V>(g + i, left, gr);
         if constexpr (BITS == 32) {
-            load_vec<V>(static_cast<const float*>(rule.m) + at, true, V, m);
-            load_vec<V>(static_cast<const float*>(rule.v) + at, true, V, v);
+            load_vec<V>(static_cast<const float*>(rule.m) + at, V, m);
+            load_vec<V>(static_cast<const float*>(rule.v) + at, V, v);
         } else {
             unpack_fp8(*reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.m) + at), rule.m_scale[at / kStateBlock], m);
             unpack_fp8(*reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.v) + at), rule.v_scale[at / kStateBlock], v);
@@ -166,15 +162,15 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, in
             root[q] = sqrtf(v[q]);
             p[q] = p[q] * keep - rule.step * m[q] / (root[q] * rule.root_scale + rule.eps);
         }
-        store_vec<V>(w.p + i, wide_p, left, p);
-        if (w.copy != nullptr) store_vec<V>(w.copy + i, wide_c, left, p);
+        store_vec<V>(w.p + i, left, p);
+        if (w.copy != nullptr) store_vec<V>(w.copy + i, left, p);
         if constexpr (BITS == 32) {
             if (left < V) {
 #pragma unroll
                 for (int q = 0; q < V; ++q) if (q >= left) { m[q] = 0.0f; v[q] = 0.0f; }
             }
-            store_vec<V>(static_cast<float*>(rule.m) + at, true, V, m);
-            store_vec<V>(static_cast<float*>(rule.v) + at, true, V, v);
+            store_vec<V>(static_cast<float*>(rule.m) + at, V, m);
+            store_vec<V>(static_cast<float*>(rule.v) + at, V, v);
         } else {
             uint32_t dm[8], dr[8];
 #pragma unroll

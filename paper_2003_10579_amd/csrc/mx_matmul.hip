@@ -17,7 +17,6 @@ struct Product {
     void* out;
     int64_t pitch;
     int32_t steps;          // of 128 columns
-    int32_t wide;           // four results of a row may be stored at once
     int32_t tiles_m, tiles_n;
 };
 
@@ -35,7 +34,7 @@ template <typename T>
 __device__ __forceinline__ void store_four(const Product& p, int64_t m, int64_t n, const f32x4& c) {
     if (m >= p.a.rows || n >= p.b.rows) return;
     const float x[4] = {c.x, c.y, c.z, c.w};
-    store_vec<4>(static_cast<T*>(p.out) + m * p.pitch + n, p.wide, p.b.rows - n, x);
+    store_vec<4>(static_cast<T*>(p.out) + m * p.pitch + n, p.b.rows - n, x);
 }
 
 // ---- tiles ---------------------------------------------------------------------------------------------------------
@@ -303,7 +302,6 @@ bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
 
 ssgd_status product(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K,
                     void* out, int32_t out_dtype, int64_t out_pitch, hipStream_t stream) {
-    const int64_t mb = dtype_bytes(out_dtype);
     if (K == 0) {
         const dim3 grid(1024);
         if (out_dtype == SSGD_F32) hipLaunchKernelGGL((zero_kernel<float>), grid, dim3(256), 0, stream, static_cast<float*>(out), M, N, out_pitch);
@@ -315,7 +313,6 @@ ssgd_status product(const void* a_values, const void* a_scales, int32_t a_fmt, i
     p.a = {static_cast<const uint8_t*>(a_values), static_cast<const uint8_t*>(a_scales), M, mx_row_bytes(a_fmt, K), scale_bytes};
     p.b = {static_cast<const uint8_t*>(b_values), static_cast<const uint8_t*>(b_scales), N, mx_row_bytes(SSGD_MX_FP4, K), scale_bytes};
     p.out = out; p.pitch = out_pitch; p.steps = (int32_t)(mx_padded(K) / kMxPad);
-    p.wide = aligned(out, (uintptr_t)(4 * mb)) && out_pitch % 4 == 0 ? 1 : 0;
     if (a_fmt == SSGD_MX_FP4) { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP4, float>(p, stream); else launch<SSGD_MX_FP4, bf16_t>(p, stream); }
     else { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP8, float>(p, stream); else launch<SSGD_MX_FP8, bf16_t>(p, stream); }
     return op_hip(hipGetLastError(), "mx product");

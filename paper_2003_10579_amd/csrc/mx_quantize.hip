@@ -13,7 +13,7 @@ namespace {
 constexpr int kTile = 128;
 constexpr int kThreads = 256;
 
-struct Source { const void* x; int64_t rows, cols, pitch; int32_t wide; };
+struct Source { const void* x; int64_t rows, cols, pitch; };
 struct Target { uint8_t *values, *scales; int64_t row_bytes, scale_bytes; };   // values == nullptr: not wanted
 
 // Eight columns of a row (zeros where there are none) -> values and, from the first of four lanes, the scale.
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Source s, Target t, int6
     if (g >= groups) return;                 // (groups is a multiple of 16: whole blocks)
     const int64_t row = g / groups_per_row, col = (g - row * groups_per_row) * 8;
     float x[8];
-    load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, s.wide, s.cols - col, x);
+    load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, s.cols - col, x);
     store_block<FMT>(t, row, col, x);
 }
 
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads) void tile_kernel(Source s, Target t, Targ
         const int r = q * 16 + (threadIdx.x >> 4);
         const int64_t row = r0 + r, col = c0 + lane_col;
         float x[8];
-        load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, s.wide, row < s.rows ? s.cols - col : 0, x);
+        load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0, x);
         if constexpr (ROWS >= 0) { if (row < s.rows) store_block<ROWS>(t, row, col, x); }
         *reinterpret_cast<f32x4*>(&tile[place(r, lane_col)]) = f32x4{x[0], x[1], x[2], x[3]};
         *reinterpret_cast<f32x4*>(&tile[place(r, lane_col + 4)]) = f32x4{x[4], x[5], x[6], x[7]};
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void tile_kernel(Source s, Target t, Targ
 // Eight columns of a row from their values and scale.
 template <int FMT, typename T>
 __global__ __launch_bounds__(kThreads) void back_kernel(const uint8_t* values, const uint8_t* scales, int64_t row_bytes, int64_t scale_bytes, T* out,
-                                                        int64_t cols, int64_t pitch, int32_t wide, int64_t groups, int64_t groups_per_row) {
+                                                        int64_t cols, int64_t pitch, int64_t groups, int64_t groups_per_row) {
     const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (g >= groups) return;
     const int64_t row = g / groups_per_row, col = (g - row * groups_per_row) * 8;
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads) void back_kernel(const uint8_t* values, c
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) x[q] *= scale;
-    store_vec<8>(out + row * pitch + col, wide, cols - col, x);
+    store_vec<8>(out + row * pitch + col, cols - col, x);
 }
 
 bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
@@ -158,7 +158,7 @@ ssgd_status ssgd_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
         if (!x || !aligned(x, (uintptr_t)dtype_bytes(dtype))) return op_fail(SSGD_EINVAL, "mx quantize: the matrix is null or misaligned");
         if (across && rows >= kMostCols) return op_fail(SSGD_EINVAL, "mx quantize: too many rows to be columns");
         if (!fits(across ? mx_padded(cols) / kTile * (mx_padded(rows) / kTile) : rows * (mx_padded(cols) / 8) / kThreads + 1)) return op_fail(SSGD_EINVAL, "mx quantize: too many elements");
-        const Source s{x, rows, cols, pitch, aligned(x, 16) && pitch % 8 == 0 ? 1 : 0};
+        const Source s{x, rows, cols, pitch};
         const Target t{static_cast<uint8_t*>(values), static_cast<uint8_t*>(scales), mx_row_bytes(fmt, cols), mx_padded(cols) / kMxBlock};
         const Target tt{static_cast<uint8_t*>(values_t), static_cast<uint8_t*>(scales_t), mx_row_bytes(fmt_t, rows), mx_padded(rows) / kMxBlock};
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -179,12 +179,11 @@ ssgd_status ssgd_mx_dequantize(const void* values, const void* scales, int32_t f
             return op_fail(SSGD_EINVAL, "mx dequantize: a buffer is null or misaligned");
         const int64_t per_row = (cols + 7) / 8, groups = rows * per_row;
         if (!fits(groups / kThreads + 1)) return op_fail(SSGD_EINVAL, "mx dequantize: too many elements");
-        const int wide = aligned(out, 16) && pitch % 8 == 0 ? 1 : 0;
         const int64_t rb = mx_row_bytes(fmt, cols), sb = mx_padded(cols) / kMxBlock;
         const dim3 grid((unsigned)((groups + kThreads - 1) / kThreads));
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
 #define SSGD_BACK(F, T) hipLaunchKernelGGL((back_kernel<F, T>), grid, dim3(kThreads), 0, stream, static_cast<const uint8_t*>(values), static_cast<const uint8_t*>(scales), \
-                                           rb, sb, static_cast<T*>(out), cols, pitch, wide, groups, per_row)
+                                           rb, sb, static_cast<T*>(out), cols, pitch, groups, per_row)
         if (fmt == SSGD_MX_FP4) { if (dtype == SSGD_F32) SSGD_BACK(SSGD_MX_FP4, float); else SSGD_BACK(SSGD_MX_FP4, bf16_t); }
         else { if (dtype == SSGD_F32) SSGD_BACK(SSGD_MX_FP8, float); else SSGD_BACK(SSGD_MX_FP8, bf16_t); }
 #undef SSGD_BACK

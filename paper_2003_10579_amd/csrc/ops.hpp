@@ -56,18 +56,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t f32_to_bf16(float x) { return pack_bf16(x, 0.0f) & 0xFFFFu; }
 
-__device__ __forceinline__ float load_one(const float* p) { return *p; }
-__device__ __forceinline__ float load_one(const bf16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void store_one(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_one(bf16_t* p, float x) { *p = (bf16_t)f32_to_bf16(x); }
-
-// V consecutive values (4 or 8) at p; `left` of them exist, the rest are zero.  wide: p is a multiple of 16 bytes (8 for four bf16).
+// V consecutive values (4 or 8) at p; `left` of them exist, the rest are zero.  Global loads and stores of 16 bytes need no more alignment
+// than the element's (the types say so, and the compiler then splits nothing), so rows at odd places take the same path.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef words4 words4_any __attribute__((aligned(2)));
+typedef words2 words2_any __attribute__((aligned(2)));
 template <int V>
-__device__ __forceinline__ void load_vec(const float* p, bool wide, int64_t left, float (&x)[V]) {
-    if (wide && left >= V) {
+__device__ __forceinline__ void load_vec(const float* p, int64_t left, float (&x)[V]) {
+    if (left >= V) {
 #pragma unroll
         for (int q = 0; q < V; q += 4) {
-            const f32x4 v = *reinterpret_cast<const f32x4*>(p + q);
+            const f32x4 v = *reinterpret_cast<const f32x4_any*>(p + q);
             x[q] = v.x; x[q + 1] = v.y; x[q + 2] = v.z; x[q + 3] = v.w;
         }
     } else {
@@ -76,14 +75,14 @@ __device__ __forceinline__ void load_vec(const float* p, bool wide, int64_t left
     }
 }
 template <int V>
-__device__ __forceinline__ void load_vec(const bf16_t* p, bool wide, int64_t left, float (&x)[V]) {
-    if (wide && left >= V) {
+__device__ __forceinline__ void load_vec(const bf16_t* p, int64_t left, float (&x)[V]) {
+    if (left >= V) {
         uint32_t w[V / 2];
         if constexpr (V == 8) {
-            const words4 v = *reinterpret_cast<const words4*>(p);
+            const words4 v = *reinterpret_cast<const words4_any*>(p);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
         } else {
-            const words2 v = *reinterpret_cast<const words2*>(p);
+            const words2 v = *reinterpret_cast<const words2_any*>(p);
             w[0] = v.x; w[1] = v.y;
         }
 #pragma unroll
@@ -94,20 +93,20 @@ __device__ __forceinline__ void load_vec(const bf16_t* p, bool wide, int64_t lef
     }
 }
 template <int V>
-__device__ __forceinline__ void store_vec(float* p, bool wide, int64_t left, const float (&x)[V]) {
-    if (wide && left >= V) {
+__device__ __forceinline__ void store_vec(float* p, int64_t left, const float (&x)[V]) {
+    if (left >= V) {
 #pragma unroll
-        for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4*>(p + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
+        for (int q = 0; q < V; q += 4) *reinterpret_cast<f32x4_any*>(p + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
     } else {
 #pragma unroll
         for (int q = 0; q < V; ++q) if (q < left) p[q] = x[q];
     }
 }
 template <int V>
-__device__ __forceinline__ void store_vec(bf16_t* p, bool wide, int64_t left, const float (&x)[V]) {
-    if (wide && left >= V) {
-        if constexpr (V == 8) *reinterpret_cast<words4*>(p) = words4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
-        else *reinterpret_cast<words2*>(p) = words2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+__device__ __forceinline__ void store_vec(bf16_t* p, int64_t left, const float (&x)[V]) {
+    if (left >= V) {
+        if constexpr (V == 8) *reinterpret_cast<words4_any*>(p) = words4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+        else *reinterpret_cast<words2_any*>(p) = words2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
     } else {
 #pragma unroll
         for (int q = 0; q < V; ++q) if (q < left) p[q] = (bf16_t)f32_to_bf16(x[q]);

@@ -24,7 +24,7 @@ struct Forward {
     uint8_t *values, *scales;
     float* rstd;
     int64_t rows, x_pitch, residual_pitch, sum_pitch, y_pitch, row_bytes, scale_bytes;
-    int32_t d, w_bf16, wide_x, wide_residual, wide_sum, wide_y, wide_w;
+    int32_t d, w_bf16;
     float eps;
 };
 
@@ -34,7 +34,7 @@ struct Backward {
     void* dx;
     float* partial;          // [teams][d], nullptr: dw is not wanted
     int64_t rows, dy_pitch, s_pitch, dsum_pitch, dx_pitch, teams;
-    int32_t d, w_bf16, wide_dy, wide_s, wide_dsum, wide_dx, wide_w;
+    int32_t d, w_bf16;
 };
 
 // Sum over the threads of a row: across lanes in fp64, so that all that is left of the order is a thread's own few terms.
@@ -52,9 +52,9 @@ __device__ __forceinline__ double team_sum(double x, double* part) {
     return x;
 }
 
-__device__ __forceinline__ void load_weight(const void* w, int bf16, int wide, int col, int d, float (&x)[8]) {
-    if (bf16) load_vec<8>(static_cast<const bf16_t*>(w) + col, wide, d - col, x);
-    else load_vec<8>(static_cast<const float*>(w) + col, wide, d - col, x);
+__device__ __forceinline__ void load_weight(const void* w, int bf16, int col, int d, float (&x)[8]) {
+    if (bf16) load_vec<8>(static_cast<const bf16_t*>(w) + col, d - col, x);
+    else load_vec<8>(static_cast<const float*>(w) + col, d - col, x);
 }
 
 __device__ __forceinline__ float as_stored(const float*, float x) { return x; }
@@ -63,13 +63,13 @@ __device__ __forceinline__ float as_stored(const bf16_t*, float x) { return bf16
 // Eight columns of the stream: the sum, rounded as it is stored, and stored.
 template <typename T>
 __device__ __forceinline__ void take_sum(const Forward& a, int64_t row, int col, float (&s)[8]) {
-    load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.wide_x, a.d - col, s);
+    load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.d - col, s);
     if (a.residual != nullptr) {
         float r[8];
-        load_vec<8>(static_cast<const T*>(a.residual) + row * a.residual_pitch + col, a.wide_residual, a.d - col, r);
+        load_vec<8>(static_cast<const T*>(a.residual) + row * a.residual_pitch + col, a.d - col, r);
 #pragma unroll
         for (int q = 0; q < 8; ++q) s[q] = as_stored(static_cast<const T*>(nullptr), s[q] + r[q]);
-        store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.wide_sum, a.d - col, s);
+        store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
     }
 }
 
@@ -86,7 +86,7 @@ __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int 
         *reinterpret_cast<words2*>(a.values + row * a.row_bytes + col) = mx_pack_fp8(y, byte);
         if ((threadIdx.x & 3) == 0) a.scales[row * a.scale_bytes + col / kMxBlock] = (uint8_t)byte;
     } else {
-        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, a.wide_y, a.d - col, y);
+        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, a.d - col, y);
     }
 }
 
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
     const int end = FP8 ? (int)mx_padded(a.d) : a.d;
     float w[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, a.wide_w, (v * LANES + lane) * 8, a.d, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, (v * LANES + lane) * 8, a.d, w[v]);
     for (int64_t row = team; row < a.rows; row += teams) {
         float s[NV][8];
         float sum = 0.0f;
@@ -138,9 +138,9 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
         if (threadIdx.x == 0) a.rstd[row] = rstd;
         for (int64_t col = threadIdx.x * 8; col < end; col += 8192) {
             float s[8], w[8];
-            if (a.residual != nullptr) load_vec<8>(static_cast<const T*>(a.sum) + row * a.sum_pitch + col, a.wide_sum, a.d - col, s);
-            else load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.wide_x, a.d - col, s);
-            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+            if (a.residual != nullptr) load_vec<8>(static_cast<const T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
+            else load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.d - col, s);
+            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
             store_normed<T, FP8>(a, row, (int)col, s, rstd, w);
         }
     }
@@ -150,13 +150,13 @@ template <typename T>
 __device__ __forceinline__ void store_dx(const Backward& a, int64_t row, int64_t col, const float (&dy)[8], const float (&xhat)[8], const float (&w)[8], float rstd,
                                          float c) {
     float dx[8], more[8];
-    if (a.dsum != nullptr) load_vec<8>(static_cast<const T*>(a.dsum) + row * a.dsum_pitch + col, a.wide_dsum, a.d - col, more);
+    if (a.dsum != nullptr) load_vec<8>(static_cast<const T*>(a.dsum) + row * a.dsum_pitch + col, a.d - col, more);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         dx[q] = rstd * (dy[q] * w[q] - xhat[q] * c);
         if (a.dsum != nullptr) dx[q] += more[q];
     }
-    store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, a.wide_dx, a.d - col, dx);
+    store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, a.d - col, dx);
 }
 
 template <typename T, int LANES, int NV>
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_weight(a.w, a.w_bf16, a.wide_w, (v * LANES + lane) * 8, a.d, w[v]);
+        load_weight(a.w, a.w_bf16, (v * LANES + lane) * 8, a.d, w[v]);
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[v][q] = 0.0f;
     }
@@ -179,8 +179,8 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int col = (v * LANES + lane) * 8;
-            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy[v]);
-            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, xhat[v]);
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy[v]);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, xhat[v]);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 xhat[v][q] *= rstd;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int col = (v * LANES + lane) * 8;
-            store_vec<8>(a.partial + team * a.d + col, a.d % 4 == 0, a.d - col, dw[v]);
+            store_vec<8>(a.partial + team * a.d + col, a.d - col, dw[v]);
         }
     }
 }
@@ -213,9 +213,9 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
         double sum = 0.0;
         for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
             float dy[8], s[8], w[8];
-            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy);
-            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, s);
-            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, s);
+            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
             float few = 0.0f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) few += dy[q] * w[q] * (s[q] * rstd);
@@ -224,23 +224,22 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
         const float c = (float)(team_sum<1024>(sum, part) / a.d);
         for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
             float dy[8], s[8], w[8];
-            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.wide_dy, a.d - col, dy);
-            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.wide_s, a.d - col, s);
-            load_weight(a.w, a.w_bf16, a.wide_w, (int)col, a.d, w);
+            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy);
+            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, s);
+            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
 #pragma unroll
             for (int q = 0; q < 8; ++q) s[q] *= rstd;
             store_dx<T>(a, row, col, dy, s, w, rstd, c);
             if (a.partial == nullptr) continue;
             float* to = a.partial + (int64_t)blockIdx.x * a.d + col;
-            const bool wide = a.d % 4 == 0;
             float dw[8];
             if (first) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) dw[q] = 0.0f;
-            } else load_vec<8>(to, wide, a.d - col, dw);
+            } else load_vec<8>(to, a.d - col, dw);
 #pragma unroll
             for (int q = 0; q < 8; ++q) dw[q] += dy[q] * s[q];
-            store_vec<8>(to, wide, a.d - col, dw);
+            store_vec<8>(to, a.d - col, dw);
         }
         first = false;
     }
@@ -303,7 +302,6 @@ bool shape_ok(int32_t dtype, int32_t w_dtype, int64_t rows, int64_t d) {
     return dtype_ok(dtype) && dtype_ok(w_dtype) && rows >= 0 && rows < (int64_t(1) << 40) && d >= 1 && d < (int64_t(1) << 30);
 }
 bool there(const void* p, int32_t dtype) { return p != nullptr && aligned(p, (uintptr_t)dtype_bytes(dtype)); }
-int wide(const void* p, int64_t pitch) { return aligned(p, 16) && pitch % 8 == 0 ? 1 : 0; }
 
 }  // namespace
 
@@ -329,7 +327,6 @@ ssgd_status ssgd_rmsnorm(const void* x, int64_t x_pitch, const void* residual, i
         a.rows = rows; a.x_pitch = x_pitch; a.residual_pitch = residual_pitch; a.sum_pitch = sum_pitch; a.y_pitch = y_pitch;
         a.row_bytes = mx_row_bytes(SSGD_MX_FP8, d); a.scale_bytes = mx_padded(d) / kMxBlock;
         a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16; a.eps = (float)eps;
-        a.wide_x = wide(x, x_pitch); a.wide_residual = wide(residual, residual_pitch); a.wide_sum = wide(sum, sum_pitch); a.wide_y = wide(y, y_pitch); a.wide_w = wide(weight, 0);
         const hipStream_t s = static_cast<hipStream_t>(hip_stream);
         if (dtype == SSGD_F32) { if (values) launch_forward<float, true>(a, s); else launch_forward<float, false>(a, s); }
         else { if (values) launch_forward<bf16_t, true>(a, s); else launch_forward<bf16_t, false>(a, s); }
@@ -354,7 +351,6 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
         a.dy = dy; a.s = s; a.w = weight; a.dsum = dsum; a.rstd = rstd; a.dx = dx; a.partial = dweight ? work : nullptr;
         a.rows = rows; a.dy_pitch = dy_pitch; a.s_pitch = s_pitch; a.dsum_pitch = dsum_pitch; a.dx_pitch = dx_pitch; a.teams = teams_for(rows, d);
         a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16;
-        a.wide_dy = wide(dy, dy_pitch); a.wide_s = wide(s, s_pitch); a.wide_dsum = wide(dsum, dsum_pitch); a.wide_dx = wide(dx, dx_pitch); a.wide_w = wide(weight, 0);
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (rows > 0) {
             if (dtype == SSGD_F32) launch_backward<float>(a, stream); else launch_backward<bf16_t>(a, stream);

@@ -323,30 +323,43 @@ def debug_batch(seed, replica, worker, ordinal, version, m, N):
 
 
 # ---- operators of a low-precision training step: on the device and the current stream of their tensors ----------------
+# (A call's host time is what its caller waits for where the kernels are short, so checks build no text unless they fail and
+# outputs share an allocation.)
 
-def _need(ok, msg):
-    if not ok:
-        raise SsgdError(EINVAL, msg)
+_torch = _raw_stream = _device_now = None
+_DTYPES = {}
+
+
+def _load():
+    """torch and what every call needs of it, looked up once."""
+    global _torch, _raw_stream, _device_now
+    import torch
+    lib()
+    _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    _raw_stream, _device_now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    torch.cuda.init()
+    _torch = torch
+
+
+def _refuse(msg):
+    raise SsgdError(EINVAL, msg)
 
 
 def _dtype(t):
-    import torch
-    if t == torch.float32:
-        return F32
-    if t == torch.bfloat16:
-        return BF16
-    raise SsgdError(EINVAL, f"float32 or bfloat16 is wanted, not {t}")
+    kind = _DTYPES.get(t)
+    return _refuse(f"float32 or bfloat16 is wanted, not {t}") if kind is None else kind
 
 
 def _call(entry, device, *args):
     """One library call on the device and its current stream, which is the last argument of every operator."""
-    import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        _check(entry(*args, stream))
+    index = device.index
+    if _device_now() == index:
+        status = entry(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            _check(entry(*args, stream))
+        with _torch.cuda.device(device):
+            status = entry(*args, _raw_stream(index))
+    if status != OK:
+        _check(status)
 
 
 class AdamW:
@@ -357,93 +370,138 @@ class AdamW:
     over all tensors, and `grad_norm` (one element on the device) holds the norm of the last step's."""
 
     def __init__(self, params, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, max_norm=0.0, state_bits=32, seed=0, copies=None):
-        import torch
+        _torch or _load()
+        torch = _torch
         self.h = None
         params = list(params)
-        _need(len(params) > 0, "adamw: at least one tensor")
+        if not params:
+            _refuse("adamw: at least one tensor")
         dev = params[0].device
         copies = [None] * len(params) if copies is None else list(copies)
         decay = [float(weight_decay)] * len(params) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
-        _need(len(copies) == len(params) and len(decay) == len(params), "adamw: one copy and one weight decay per tensor")
+        if len(copies) != len(params) or len(decay) != len(params):
+            _refuse("adamw: one copy and one weight decay per tensor")
         for p, c in zip(params, copies):
-            _need(p.is_cuda and p.device == dev and p.dtype == torch.float32 and p.is_contiguous(), "adamw: parameters are contiguous float32 tensors of one GPU")
-            _need(c is None or (c.device == dev and c.dtype == torch.bfloat16 and c.is_contiguous() and c.numel() == p.numel()),
-                  "adamw: copies are contiguous bfloat16 tensors of their parameter's size")
+            if not (p.is_cuda and p.device == dev and p.dtype == torch.float32 and p.is_contiguous()):
+                _refuse("adamw: parameters are contiguous float32 tensors of one GPU")
+            if not (c is None or (c.device == dev and c.dtype == torch.bfloat16 and c.is_contiguous() and c.numel() == p.numel())):
+                _refuse("adamw: copies are contiguous bfloat16 tensors of their parameter's size")
         n = len(params)
         self._sizes = [p.numel() for p in params]
         sizes = (C.c_int64 * n)(*self._sizes)
         total = lib().ssgd_adamw_state_elements(n, sizes)
-        _need(state_bits in (8, 32), "adamw: state_bits is 8 or 32")
+        if state_bits not in (8, 32):
+            _refuse("adamw: state_bits is 8 or 32")
         self.m = torch.zeros(total, device=dev, dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn)
         self.v = torch.zeros_like(self.m)
         self.m_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
         self.v_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
         self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
         self.t = 0
-        self._keep, self._device, self._pointers = (params, copies), dev, C.c_void_p * n
+        self._keep, self._device, self._grads = (params, copies), dev, (C.c_void_p * n)()
+        pointers = C.c_void_p * n
         o = AdamWOptions(float(betas[0]), float(betas[1]), float(eps), float(max_norm), state_bits, seed)
         h = C.c_void_p()
         with torch.cuda.device(dev):
             _check(lib().ssgd_adamw_create(
-                n, sizes, self._pointers(*[p.data_ptr() for p in params]), self._pointers(*[None if c is None else c.data_ptr() for c in copies]),
+                n, sizes, pointers(*[p.data_ptr() for p in params]), pointers(*[None if c is None else c.data_ptr() for c in copies]),
                 (C.c_double * n)(*decay), C.byref(o), self.m.data_ptr(), self.v.data_ptr(),
                 None if self.m_scale is None else self.m_scale.data_ptr(), None if self.v_scale is None else self.v_scale.data_ptr(), C.byref(h)))
         self.h = h
 
     def step(self, grads, lr):
         """One update with a list of gradients, contiguous tensors of one type (float32 or bfloat16) and their parameters' sizes."""
-        _need(self.h is not None, "adamw: closed")
-        _need(len(grads) == len(self._sizes), "adamw step: one gradient per tensor")
-        kind = grads[0].dtype
-        for g, n in zip(grads, self._sizes):
-            _need(g.dtype == kind and g.numel() == n and g.device == self._device and g.is_contiguous(),
-                  "adamw step: gradients are contiguous tensors of one type, of their parameters' sizes and device")
-        _call(lib().ssgd_adamw_step, self._device, self.h, self._pointers(*[g.data_ptr() for g in grads]), _dtype(kind), lr, self.t + 1,
-              None if self.grad_norm is None else self.grad_norm.data_ptr())
+        if self.h is None:
+            _refuse("adamw: closed")
+        if len(grads) != len(self._sizes):
+            _refuse("adamw step: one gradient per tensor")
+        kind, dev, at = grads[0].dtype, self._device, self._grads
+        for k, (g, n) in enumerate(zip(grads, self._sizes)):
+            if not (g.dtype == kind and g.numel() == n and g.device == dev and g.is_contiguous()):
+                _refuse("adamw step: gradients are contiguous tensors of one type, of their parameters' sizes and device")
+            at[k] = g.data_ptr()
+        _call(_lib.ssgd_adamw_step, dev, self.h, at, _dtype(kind), lr, self.t + 1, None if self.grad_norm is None else self.grad_norm.data_ptr())
         self.t += 1
 
     def close(self):
         if getattr(self, "h", None):
-            lib().ssgd_adamw_destroy(self.h)
+            _lib.ssgd_adamw_destroy(self.h)
             self.h = None
 
     def __del__(self):
-        self.close()
+        if _lib is not None:        # the interpreter may be past it
+            self.close()
 
 
 def _matrix(x, what):
     """(device, dtype, rows, cols, pitch) of a matrix with contiguous rows."""
-    _need(x.is_cuda and x.dim() == 2, f"{what}: a matrix on the GPU is wanted")
+    _torch or _load()
+    if not x.is_cuda or x.dim() != 2:
+        _refuse(f"{what}: a matrix on the GPU is wanted")
     rows, cols = x.shape
-    pitch = x.stride(0) if rows > 1 else cols
-    _need((cols <= 1 or x.stride(1) == 1) and pitch >= cols, f"{what}: rows have to be contiguous")
-    return x.device, _dtype(x.dtype), rows, cols, pitch
+    pitch, step = x.stride()
+    if rows <= 1:
+        pitch = cols
+    if (step != 1 and cols > 1) or pitch < cols:
+        _refuse(f"{what}: rows have to be contiguous")
+    kind = _DTYPES.get(x.dtype)
+    return x.device, _dtype(x.dtype) if kind is None else kind, rows, cols, pitch
 
 
 class MxTensor:
     """A microscaled matrix: `values` (uint8, rows x bytes; two E2M1 or one E4M3 number to a byte) and `scales` (uint8, 2^(byte - 127) per
     32 columns), both padded with zeros to a multiple of 128 columns.  `format` is "fp4" or "fp8", `shape` (rows, cols)."""
 
-    __slots__ = ("values", "scales", "format", "shape")
+    __slots__ = ("format", "shape", "device", "_values", "_scales", "_room", "_at")
 
     def __init__(self, values, scales, format, shape):
-        self.values, self.scales, self.format, self.shape = values, scales, format, shape
+        if format not in _FORMATS:
+            _refuse("mx: the format is 'fp4' or 'fp8'")
+        rows, cols = shape
+        wide = -(-cols // 128) * 128
+        if not (values.is_cuda and values.is_contiguous() and scales.is_contiguous() and scales.device == values.device and
+                values.element_size() == scales.element_size() == 1 and
+                tuple(values.shape) == (rows, wide // 2 if format == "fp4" else wide) and tuple(scales.shape) == (rows, wide // 32)):
+            _refuse(f"mx: values and scales do not have the layout of {rows} x {cols}")
+        self.format, self.shape, self.device, self._room = format, (rows, cols), values.device, None
+        self._values, self._scales, self._at = values, scales, (values.data_ptr(), scales.data_ptr())
 
     @classmethod
     def empty(cls, rows, cols, format, device):
-        import torch
-        _need(format in _FORMATS, "mx: the format is 'fp4' or 'fp8'")
-        wide = -(-cols // 128) * 128
-        return cls(torch.empty((rows, wide // 2 if format == "fp4" else wide), dtype=torch.uint8, device=device),
-                   torch.empty((rows, wide // 32), dtype=torch.uint8, device=device), format, (rows, cols))
+        _torch or _load()
+        if format not in _FORMATS:
+            _refuse("mx: the format is 'fp4' or 'fp8'")
+        q = cls.__new__(cls)
+        wide = (cols + 127) // 128 * 128
+        bytes = rows * (wide // 2 if format == "fp4" else wide)
+        q._room = room = _torch.empty(bytes + rows * (wide // 32), dtype=_torch.uint8, device=device)
+        at = room.data_ptr()
+        q.format, q.shape, q.device, q._values, q._scales, q._at = format, (rows, cols), room.device, None, None, (at, at + bytes)
+        return q
+
+    # (views of one allocation, made when they are asked for)
+    def _view(self, first, width):
+        return self._room.as_strided((self.shape[0], width), (width, 1), first)
+
+    @property
+    def values(self):
+        if self._values is None:
+            wide = (self.shape[1] + 127) // 128 * 128
+            self._values = self._view(0, wide // 2 if self.format == "fp4" else wide)
+        return self._values
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._scales = self._view(self._at[1] - self._at[0], (self.shape[1] + 127) // 128 * 4)
+        return self._scales
 
 
 def mx_quantize(x, format="fp4"):
     """The rows of a matrix (float32 or bfloat16) as an MxTensor."""
     dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize")
     q = MxTensor.empty(rows, cols, format, dev)
-    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], q.values.data_ptr(), q.scales.data_ptr(),
-          0, None, None)
+    _call(_lib.ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], *q._at, 0, None, None)
     return q
 
 
@@ -451,8 +509,7 @@ def mx_quantize_transposed(x, format="fp4"):
     """The columns of a matrix as the rows of an MxTensor."""
     dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize_transposed")
     q = MxTensor.empty(cols, rows, format, dev)
-    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, 0, None, None, _FORMATS[format], q.values.data_ptr(),
-          q.scales.data_ptr())
+    _call(_lib.ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, 0, None, None, _FORMATS[format], *q._at)
     return q
 
 
@@ -460,58 +517,47 @@ def mx_quantize_both(x, format="fp4", format_transposed="fp4"):
     """(mx_quantize(x), mx_quantize_transposed(x)) from one read of x."""
     dev, kind, rows, cols, pitch = _matrix(x, "mx_quantize_both")
     q, t = MxTensor.empty(rows, cols, format, dev), MxTensor.empty(cols, rows, format_transposed, dev)
-    _call(lib().ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], q.values.data_ptr(), q.scales.data_ptr(),
-          _FORMATS[format_transposed], t.values.data_ptr(), t.scales.data_ptr())
+    _call(_lib.ssgd_mx_quantize, dev, x.data_ptr(), kind, rows, cols, pitch, _FORMATS[format], *q._at, _FORMATS[format_transposed], *t._at)
     return q, t
-
-
-def _mx(q, what):
-    """An MxTensor whose arrays are as the library lays them out."""
-    _need(isinstance(q, MxTensor) and q.format in _FORMATS, f"{what}: an MxTensor is wanted")
-    rows, cols = q.shape
-    wide = -(-cols // 128) * 128
-    _need(q.values.is_cuda and q.values.is_contiguous() and q.scales.is_contiguous() and q.scales.device == q.values.device and
-          q.values.element_size() == q.scales.element_size() == 1 and
-          tuple(q.values.shape) == (rows, wide // 2 if q.format == "fp4" else wide) and tuple(q.scales.shape) == (rows, wide // 32),
-          f"{what}: values and scales do not have the layout of {rows} x {cols}")
-    return q.values.device
 
 
 def mx_dequantize(q, dtype=None):
     """The values of an MxTensor as a matrix of `dtype` (float32 unless it is given, or bfloat16)."""
-    import torch
-    dev = _mx(q, "mx_dequantize")
-    out = torch.empty(q.shape, dtype=dtype or torch.float32, device=dev)
-    _call(lib().ssgd_mx_dequantize, dev, q.values.data_ptr(), q.scales.data_ptr(), _FORMATS[q.format], q.shape[0], q.shape[1], out.data_ptr(),
-          _dtype(out.dtype), q.shape[1])
+    if not isinstance(q, MxTensor):
+        _refuse("mx_dequantize: an MxTensor is wanted")
+    rows, cols = q.shape
+    kind = F32 if dtype is None else _dtype(dtype)
+    out = _torch.empty((rows, cols), dtype=dtype, device=q.device) if dtype else _torch.empty((rows, cols), dtype=_torch.float32, device=q.device)
+    _call(_lib.ssgd_mx_dequantize, q.device, *q._at, _FORMATS[q.format], rows, cols, out.data_ptr(), kind, cols)
     return out
 
 
 def mx_matmul(a, b, dtype=None):
     """a b^T of two MxTensors with equal numbers of columns, a in either format, b in "fp4", as a matrix of `dtype` (bfloat16 unless
     it is given, or float32)."""
-    import torch
-    dev = _mx(a, "mx_matmul")
-    _need(_mx(b, "mx_matmul") == dev and b.format == "fp4" and a.shape[1] == b.shape[1], "mx_matmul: b is an 'fp4' MxTensor with a's columns, on its device")
-    (M, K), N = a.shape, b.shape[0]
-    out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=dev)
-    _call(lib().ssgd_mx_matmul, dev, a.values.data_ptr(), a.scales.data_ptr(), _FORMATS[a.format], M, b.values.data_ptr(), b.scales.data_ptr(), N, K,
-          out.data_ptr(), _dtype(out.dtype), N)
+    if not (isinstance(a, MxTensor) and isinstance(b, MxTensor) and b.format == "fp4" and a.shape[1] == b.shape[1] and a.device == b.device):
+        _refuse("mx_matmul: an MxTensor and an 'fp4' MxTensor of as many columns on its device are wanted")
+    (M, K), N, dev = a.shape, b.shape[0], a.device
+    kind = BF16 if dtype is None else _dtype(dtype)
+    out = _torch.empty((M, N), dtype=dtype or _torch.bfloat16, device=dev)
+    _call(_lib.ssgd_mx_matmul, dev, *a._at, _FORMATS[a.format], M, *b._at, N, K, out.data_ptr(), kind, N)
     return out
 
 
 def mx_linear(x, w, format="fp8", dtype=None):
     """x w^T for rows x (float32 or bfloat16), quantised to `format` on the way, and an "fp4" MxTensor w (outputs x inputs), as a
     matrix of `dtype` (x's unless it is given)."""
-    import torch
     dev, kind, M, K, pitch = _matrix(x, "mx_linear")
-    _need(format in _FORMATS, "mx_linear: the format is 'fp4' or 'fp8'")
-    _need(_mx(w, "mx_linear") == dev and w.format == "fp4" and w.shape[1] == K, "mx_linear: w is an 'fp4' MxTensor with x's columns, on its device")
+    if format not in _FORMATS:
+        _refuse("mx_linear: the format is 'fp4' or 'fp8'")
+    if not (isinstance(w, MxTensor) and w.format == "fp4" and w.shape[1] == K and w.device == dev):
+        _refuse("mx_linear: w is an 'fp4' MxTensor with x's columns, on its device")
     N, f = w.shape[0], _FORMATS[format]
-    out = torch.empty((M, N), dtype=dtype or x.dtype, device=dev)
-    work = torch.empty(lib().ssgd_mx_linear_work_bytes(f, M, K), dtype=torch.uint8, device=dev)
-    _call(lib().ssgd_mx_linear, dev, x.data_ptr(), kind, pitch, M, f, w.values.data_ptr(), w.scales.data_ptr(), N, K, out.data_ptr(), _dtype(out.dtype), N,
-          work.data_ptr())
+    out_kind = kind if dtype is None else _dtype(dtype)
+    out = _torch.empty((M, N), dtype=dtype or x.dtype, device=dev)
+    bytes = _lib.ssgd_mx_linear_work_bytes(f, M, K)
+    work = _torch.empty(bytes, dtype=_torch.uint8, device=dev) if bytes > 0 else None
+    _call(_lib.ssgd_mx_linear, dev, x.data_ptr(), kind, pitch, M, f, *w._at, N, K, out.data_ptr(), out_kind, N, None if work is None else work.data_ptr())
     return out
 
 
@@ -519,51 +565,56 @@ def _beside(t, x, what):
     """(pointer, pitch) of a matrix of the shape, type and device of x, or of none."""
     if t is None:
         return None, 0
-    dev, kind, rows, cols, pitch = _matrix(t, what)
-    _need(dev == x.device and t.dtype == x.dtype and t.shape == x.shape, f"{what}: the shape, type and device of the first matrix are wanted")
-    return t.data_ptr(), pitch
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+        _refuse(f"{what}: the shape, type and device of the first matrix are wanted")
+    return t.data_ptr(), _matrix(t, what)[4]
 
 
 def _weight(w, x, what):
-    _need(w.dim() == 1 and w.numel() == x.shape[1] and w.is_contiguous() and w.device == x.device, f"{what}: a contiguous weight per column is wanted")
+    if not (w.dim() == 1 and w.numel() == x.shape[1] and w.is_contiguous() and w.device == x.device):
+        _refuse(f"{what}: a contiguous weight per column is wanted")
     return w.data_ptr(), _dtype(w.dtype)
 
 
 def rmsnorm(x, weight, residual=None, eps=1e-6, output=None):
     """(y, s, rstd) of the root-mean-square norm of the rows of s = x + residual (s = x without one).  y has x's type or, with
     output="fp8", is an MxTensor for the product behind it; s and rstd are what rmsnorm_backward takes."""
-    import torch
     dev, kind, rows, d, pitch = _matrix(x, "rmsnorm")
-    _need(output in (None, "fp8"), "rmsnorm: the output is None (x's type) or 'fp8'")
+    if output is not None and output != "fp8":
+        _refuse("rmsnorm: the output is None (x's type) or 'fp8'")
     w, w_kind = _weight(weight, x, "rmsnorm")
     r, r_pitch = _beside(residual, x, "rmsnorm")
-    total = x if residual is None else torch.empty((rows, d), dtype=x.dtype, device=dev)
-    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    if residual is None:
+        total, total_at = x, None
+    else:
+        total = _torch.empty((rows, d), dtype=x.dtype, device=dev)
+        total_at = total.data_ptr()
+    rstd = _torch.empty(rows, dtype=_torch.float32, device=dev)
     if output is None:
-        y = torch.empty((rows, d), dtype=x.dtype, device=dev)
+        y = _torch.empty((rows, d), dtype=x.dtype, device=dev)
         to = (y.data_ptr(), d, None, None)
     else:
         y = MxTensor.empty(rows, d, "fp8", dev)
-        to = (None, 0, y.values.data_ptr(), y.scales.data_ptr())
-    _call(lib().ssgd_rmsnorm, dev, x.data_ptr(), pitch, r, r_pitch, w, kind, w_kind, rows, d, eps, None if residual is None else total.data_ptr(), d, *to,
-          rstd.data_ptr())
+        to = (None, 0, *y._at)
+    _call(_lib.ssgd_rmsnorm, dev, x.data_ptr(), pitch, r, r_pitch, w, kind, w_kind, rows, d, eps, total_at, d, *to, rstd.data_ptr())
     return y, total, rstd
 
 
 def rmsnorm_backward(dy, s, weight, rstd, dsum=None):
     """(dx, dweight) from the gradient dy of the norm's output and, where there is one, dsum that reaches s past it.  dx is the
     gradient of x and of the residual; dweight is float32."""
-    import torch
     dev, kind, rows, d, pitch = _matrix(dy, "rmsnorm_backward")
     w, w_kind = _weight(weight, dy, "rmsnorm_backward")
     s_at, s_pitch = _beside(s, dy, "rmsnorm_backward")
-    _need(rstd.dtype == torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous() and rstd.device == dev, "rmsnorm_backward: one float32 rstd per row is wanted")
+    if not (rstd.dtype == _torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous() and rstd.device == dev):
+        _refuse("rmsnorm_backward: one float32 rstd per row is wanted")
     more, more_pitch = _beside(dsum, dy, "rmsnorm_backward")
-    dx = torch.empty((rows, d), dtype=dy.dtype, device=dev)
-    dw = torch.empty(d, dtype=torch.float32, device=dev)
-    floats = lib().ssgd_rmsnorm_work_floats(rows, d)
-    _need(floats >= 0, "rmsnorm_backward: 1 <= columns < 2^30")
-    work = torch.empty(floats, dtype=torch.float32, device=dev)
-    _call(lib().ssgd_rmsnorm_backward, dev, dy.data_ptr(), pitch, s_at, s_pitch, w, kind, w_kind, rstd.data_ptr(), more, more_pitch, rows, d, dx.data_ptr(), d,
+    dx = _torch.empty((rows, d), dtype=dy.dtype, device=dev)
+    dw = _torch.empty(d, dtype=_torch.float32, device=dev)
+    floats = _lib.ssgd_rmsnorm_work_floats(rows, d)
+    if floats < 0:
+        _refuse("rmsnorm_backward: 1 <= columns < 2^30")
+    work = _torch.empty(floats, dtype=_torch.float32, device=dev)
+    _call(_lib.ssgd_rmsnorm_backward, dev, dy.data_ptr(), pitch, s_at, s_pitch, w, kind, w_kind, rstd.data_ptr(), more, more_pitch, rows, d, dx.data_ptr(), d,
           dw.data_ptr(), work.data_ptr())
     return dx, dw

@@ -149,6 +149,10 @@ def test_refusals(env):
     q = ssgd.mx_quantize(x)
     with pytest.raises(ssgd.SsgdError):
         ssgd.mx_dequantize(q, torch.float16)
-    q.scales = q.scales[:, :1]
-    with pytest.raises(ssgd.SsgdError):
-        ssgd.mx_dequantize(q)
+    again = ssgd.MxTensor(q.values, q.scales, q.format, q.shape)
+    assert torch.equal(ssgd.mx_dequantize(again), ssgd.mx_dequantize(q))
+    for values, scales, f, shape in ((q.values, q.scales[:, :1], "fp4", (8, 64)), (q.values[:, :32], q.scales, "fp4", (8, 64)), (q.values.cpu(), q.scales, "fp4", (8, 64)),
+                                     (q.values, q.scales, "fp8", (8, 64)), (q.values, q.scales, "fp4", (8, 200)), (q.values, q.scales, "fp4", (7, 64)),
+                                     (q.values, q.scales, "fp6", (8, 64)), (q.values.float(), q.scales, "fp4", (8, 64))):
+        with pytest.raises(ssgd.SsgdError):
+            ssgd.MxTensor(values, scales, f, shape)
