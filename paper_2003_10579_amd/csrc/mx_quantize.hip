@@ -2,8 +2,9 @@
 //
 // A value is read once and half a byte or one (and 1/32 of one for the scale) is written per direction: bound by memory.
 // Along the rows a lane holds eight columns and four lanes a block, whose largest magnitude takes two lane moves.  For the
-// columns a workgroup holds 128 x 128 values in LDS and a lane takes the 32 rows of one block, so the maximum needs no other lane;
-// four lanes side by side take the four blocks of a column, whose bytes are then 64 (4 bits) or 128 next to each other.
+// columns a workgroup of 512 holds 128 x 128 values in LDS, in their own type, and a lane takes the 32 rows of one block, so the maximum
+// needs no other lane; four lanes side by side take the four blocks of a column, whose bytes are then 64 (4 bits) or 128 next to each
+// other.
 #include "ops.hpp"
 
 using namespace ssgd;
@@ -11,7 +12,7 @@ using namespace ssgd;
 namespace {
 
 constexpr int kTile = 128;
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kTileThreads = 512;
 
 struct Source { const void* x; int64_t rows, cols, pitch; };
 struct Target { uint8_t *values, *scales; int64_t row_bytes, scale_bytes; };   // values == nullptr: not wanted
@@ -40,37 +41,39 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Source s, Target t, int6
     store_block<FMT>(t, row, col, x);
 }
 
-// A tile of 128 x 128.  The rows of a column's block begin 16 banks further on than those of the block before, so that four lanes on
+// A tile of 128 x 128.  The rows of a column's block begin 16 columns further on than those of the block before, so that four lanes on
 // one column and sixteen on the next ones meet in no bank.
 __device__ __forceinline__ int place(int row, int col) { return row * kTile + (row >> 5) * 16 + col; }
+__device__ __forceinline__ float read_tile(const float* t) { return *t; }
+__device__ __forceinline__ float read_tile(const bf16_t* t) { return bf16_to_f32(*t); }
 
 template <typename T, int ROWS, int COLS>       // formats; ROWS < 0: columns alone
-__global__ __launch_bounds__(kThreads) void tile_kernel(Source s, Target t, Target tt, int64_t tiles_across) {
-    __shared__ float tile[kTile * kTile + 3 * 16];
+__global__ __launch_bounds__(kTileThreads) void tile_kernel(Source s, Target t, Target tt, int64_t tiles_across) {
+    __shared__ __attribute__((aligned(16))) T tile[kTile * kTile + 3 * 16];
     const int64_t r0 = (int64_t)(blockIdx.x / tiles_across) * kTile, c0 = (int64_t)(blockIdx.x % tiles_across) * kTile;
     const int lane_col = (threadIdx.x & 15) * 8;
+    float x[kTile / 32][8];
 #pragma unroll
-    for (int q = 0; q < kTile / 16; ++q) {
-        const int r = q * 16 + (threadIdx.x >> 4);
-        const int64_t row = r0 + r, col = c0 + lane_col;
-        float x[8];
-        load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0, x);
-        if constexpr (ROWS >= 0) { if (row < s.rows) store_block<ROWS>(t, row, col, x); }
-        *reinterpret_cast<f32x4*>(&tile[place(r, lane_col)]) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4*>(&tile[place(r, lane_col + 4)]) = f32x4{x[4], x[5], x[6], x[7]};
+    for (int q = 0; q < kTile / 32; ++q) {
+        const int64_t row = r0 + q * 32 + (threadIdx.x >> 4), col = c0 + lane_col;
+        load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0, x[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kTile / 32; ++q) {
+        const int r = q * 32 + (threadIdx.x >> 4);
+        store_vec<8>(&tile[place(r, lane_col)], 8, x[q]);
+        if constexpr (ROWS >= 0) { if (r0 + r < s.rows) store_block<ROWS>(t, r0 + r, c0 + lane_col, x[q]); }
     }
     __syncthreads();
     const int block = threadIdx.x & 3;
-#pragma unroll
-    for (int q = 0; q < kTile / 64; ++q) {
-        const int c = q * 64 + (threadIdx.x >> 2);
+    {
+        const int c = threadIdx.x >> 2;
         const int64_t col = c0 + c;
-        if (col >= s.cols) continue;
-        float x[4][8];
+        if (col >= s.cols) return;
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            x[i >> 3][i & 7] = tile[place(block * 32 + i, c)];
+            x[i >> 3][i & 7] = read_tile(&tile[place(block * 32 + i, c)]);
             most = umax(most, magnitude(x[i >> 3][i & 7]));
         }
         const uint32_t byte = mx_scale_byte<COLS>(most);
@@ -128,7 +131,7 @@ template <typename T>
 void launch_tiles(const Source& s, const Target& t, int fmt, const Target& tt, int tfmt, hipStream_t stream) {
     const int64_t across = mx_padded(s.cols) / kTile, tiles = across * (mx_padded(s.rows) / kTile);
     const dim3 grid((unsigned)tiles);
-#define SSGD_TILES(R, C) hipLaunchKernelGGL((tile_kernel<T, R, C>), grid, dim3(kThreads), 0, stream, s, t, tt, across)
+#define SSGD_TILES(R, C) hipLaunchKernelGGL((tile_kernel<T, R, C>), grid, dim3(kTileThreads), 0, stream, s, t, tt, across)
     if (!t.values) { if (tfmt == SSGD_MX_FP4) SSGD_TILES(-1, SSGD_MX_FP4); else SSGD_TILES(-1, SSGD_MX_FP8); }
     else if (fmt == SSGD_MX_FP4) { if (tfmt == SSGD_MX_FP4) SSGD_TILES(SSGD_MX_FP4, SSGD_MX_FP4); else SSGD_TILES(SSGD_MX_FP4, SSGD_MX_FP8); }
     else { if (tfmt == SSGD_MX_FP4) SSGD_TILES(SSGD_MX_FP8, SSGD_MX_FP4); else SSGD_TILES(SSGD_MX_FP8, SSGD_MX_FP8); }

@@ -33,7 +33,7 @@ inline bool dtype_ok(int32_t t) { return t == SSGD_F32 || t == SSGD_BF16; }
 inline int64_t dtype_bytes(int32_t t) { return t == SSGD_F32 ? 4 : 2; }
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;      // workgroups of 256: a launch ends at 2^32 threads
+constexpr int64_t kMostBlocks = (int64_t(1) << 23) - 1;      // workgroups of up to 512: a launch ends at 2^32 threads
 
 constexpr int kMxBlock = 32;      // columns per scale
 constexpr int kMxPad = 128;       // rows of a quantised matrix are padded to so many columns: what one matrix instruction contracts

@@ -245,19 +245,30 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
     }
 }
 
-// dw of 64 columns: sixteen waves add every sixteenth partial sum, in fp64, and the first adds those.
+// dw of 16 columns: the 64 quarter waves of a workgroup take every 64th partial sum, eight loads in flight, and add in fp64.
 __global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int64_t teams, int32_t d, float* dw) {
-    __shared__ double part[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    __shared__ double part[64][17];
+    const int c = threadIdx.x & 15, group = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     double sum = 0.0;
-    if (col < d)
-        for (int64_t t = wave; t < teams; t += 16) sum += (double)partial[t * d + col];
-    part[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && col < d) {
+    if (col < d) {
+        for (int64_t t = group; t < teams; t += 64 * 8) {
+            float x[8];
 #pragma unroll
-        for (int q = 1; q < 16; ++q) sum += part[q][lane];
-        dw[col] = (float)sum;
+            for (int q = 0; q < 8; ++q) x[q] = t + 64 * q < teams ? partial[(t + 64 * q) * d + col] : 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += (double)x[q];
+        }
+    }
+    part[group][c] = sum;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        // sixteen sums a lane, then the four lanes of a column
+        sum = 0.0;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) sum += part[q * 4 + group][c];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (group == 0 && col < d) dw[col] = (float)sum;
     }
 }
 
@@ -357,7 +368,7 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
         }
         ssgd_status st = op_hip(hipGetLastError(), "rmsnorm backward");
         if (st == SSGD_OK && dweight != nullptr) {
-            hipLaunchKernelGGL(weight_kernel, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0, stream, work, a.teams, (int32_t)d, dweight);
+            hipLaunchKernelGGL(weight_kernel, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, stream, work, a.teams, (int32_t)d, dweight);
             st = op_hip(hipGetLastError(), "rmsnorm backward");
         }
         return st;
