@@ -3,6 +3,8 @@
 // One instruction contracts 16 x 16 x 128, each lane with a row (lane % 16), the scale of its block of 32 columns (lane / 16) and, in
 // 4 bits, that block's 16 bytes; in 8 bits bytes 16 g .. 16 g + 15 and the same 64 further on.  B's rows are the instruction's first
 // operand and A's its second, so that a lane's four results are consecutive columns of a row of C.
+#include <type_traits>
+
 #include "ops.hpp"
 
 using namespace ssgd;
@@ -20,9 +22,15 @@ struct Product {
     int32_t tiles_m, tiles_n;
 };
 
-template <int FA>
+// The scales are byte BYTE of their words.
+template <int FA, int BYTE>
 __device__ __forceinline__ f32x4 mfma(const ints8& b, const ints8& a, const f32x4& c, uint32_t scale_b, uint32_t scale_a) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 4, FA == SSGD_MX_FP4 ? 4 : 0, 0, (int)scale_b, 0, (int)scale_a);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 4, FA == SSGD_MX_FP4 ? 4 : 0, BYTE, (int)scale_b, BYTE, (int)scale_a);
+}
+// Byte g of four words, in order: a lane's scales of four steps of 128 columns from 16 bytes of a row of scales.
+__device__ __forceinline__ uint32_t scales_of_four(const words4& w, int g) {
+    const uint32_t pick = (uint32_t)g | (uint32_t)(4 + g) << 8;
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w.w, w.z, pick), __builtin_amdgcn_perm(w.y, w.x, pick), 0x05040100u);
 }
 
 __device__ __forceinline__ ints8 operand(const words4& lo) { return ints8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0}; }
@@ -40,9 +48,8 @@ __device__ __forceinline__ void store_four(const Product& p, int64_t m, int64_t 
 // ---- tiles ---------------------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) uint32_t lds_word;
 typedef const __attribute__((address_space(1))) uint32_t global_word;
-// Global memory to LDS without registers: lane l's bytes go to `to` + 16 l (4 l).
+// Global memory to LDS without registers: lane l's bytes go to `to` + 16 l.
 __device__ __forceinline__ void copy16(const uint8_t* from, uint8_t* to) { __builtin_amdgcn_global_load_lds((global_word*)from, (lds_word*)to, 16, 0, 0); }
-__device__ __forceinline__ void copy4(const uint8_t* from, uint8_t* to) { __builtin_amdgcn_global_load_lds((global_word*)from, (lds_word*)to, 4, 0, 0); }
 
 template <int VM> __device__ __forceinline__ void wait_and_meet() {
     static_assert(VM < 64, "the counter has six bits");
@@ -52,21 +59,24 @@ template <int VM> __device__ __forceinline__ void wait_and_meet() {
     asm volatile("" ::: "memory");
 }
 
-// WM x WN waves, a tile of BM x BN.  A stage is 128 columns: rows of A (64 or 128 bytes), rows of B (64), a word of scales per row.  In
-// LDS the 16-byte parts of a row change places by its number, so that the lanes that read one part of 16 rows meet in no bank.
+// WM x WN waves, a tile of BM x BN.  A step is 128 columns: rows of A (64 or 128 bytes) and rows of B (64) in a stage of LDS, in which the
+// 16-byte parts of a row change places by its number, so that the lanes that read one part of 16 rows meet in no bank.  Scales come for four
+// steps at a time, 16 bytes of a row: four bytes of every row per step would be as many cache lines again as the values take.  They wait in
+// registers from the first of the four steps on, one word per row, so their place in LDS is free for the next four behind the next meeting.
 template <int FA, int BM, int BN, int WM, int WN, int STAGES, typename T>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int kWaves = WM * WN, kRowA = FA == SSGD_MX_FP4 ? 64 : 128, kRowB = 64;
-    constexpr int kA = BM * kRowA, kB = BN * kRowB, kStage = kA + kB + (BM + BN) * 4;
+    constexpr int kA = BM * kRowA, kB = BN * kRowB, kStage = kA + kB;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves, kLoadsS = (BM + BN) / 64 / kWaves;
-    constexpr int kLoads = kLoadsA + kLoadsB + kLoadsS;
-    static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && kLoadsS * 64 * kWaves == BM + BN, "every wave loads the same share");
-    // (arrays of their own: the compiler then sees that loads into one stage do not concern reads of another)
+    constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves, kLoads = kLoadsA + kLoadsB;
+    static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && BM + BN == 64 * kWaves, "every wave loads the same share");
+    static_assert(STAGES == 2 || STAGES == 4, "four steps end at the stage they began with");
+    // (arrays of their own: the compiler then sees that loads into one do not concern reads of another)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage2[STAGES > 2 ? kStage : 16];
-    __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 3 ? kStage : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 2 ? kStage : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t scales[(BM + BN) * 16];
 
     // Workgroups go to the XCDs in turn; each XCD takes tiles that lie together, in groups of 8 rows of tiles, so that its L2 holds what
     // they share.
@@ -79,40 +89,40 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     const int64_t m0 = (group * kGroup + in_group % height) * BM, n0 = in_group / height * BN;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint8_t* from[kLoads];
+    // (offsets from the tile's first row: 256 rows of less than 2^24 bytes)
+    const uint8_t *a_values = p.a.values + m0 * p.a.row_bytes, *b_values = p.b.values + n0 * p.b.row_bytes;
+    const uint32_t rows_a = (uint32_t)(p.a.rows - m0 < BM ? p.a.rows - m0 : BM), rows_b = (uint32_t)(p.b.rows - n0 < BN ? p.b.rows - n0 : BN);
+    uint32_t from[kLoads];
 #pragma unroll
     for (int q = 0; q < kLoadsA; ++q) {
-        const int unit = (q * kWaves + wave) * 64 + lane, per = kRowA / 16, row = unit / per;
-        const int part = (unit % per) ^ (FA == SSGD_MX_FP4 ? (row >> 1) & 3 : row & 7);
-        const int64_t r = m0 + row < p.a.rows ? m0 + row : p.a.rows - 1;
-        from[q] = p.a.values + r * p.a.row_bytes + part * 16;
+        const uint32_t unit = (q * kWaves + wave) * 64 + lane, per = kRowA / 16, row = unit / per;
+        const uint32_t part = (unit % per) ^ (FA == SSGD_MX_FP4 ? (row >> 1) & 3 : row & 7);
+        from[q] = (row < rows_a ? row : rows_a - 1) * (uint32_t)p.a.row_bytes + part * 16;
     }
 #pragma unroll
     for (int q = 0; q < kLoadsB; ++q) {
-        const int unit = (q * kWaves + wave) * 64 + lane, row = unit / 4, part = (unit % 4) ^ ((row >> 1) & 3);
-        const int64_t r = n0 + row < p.b.rows ? n0 + row : p.b.rows - 1;
-        from[kLoadsA + q] = p.b.values + r * p.b.row_bytes + part * 16;
+        const uint32_t unit = (q * kWaves + wave) * 64 + lane, row = unit / 4, part = (unit % 4) ^ ((row >> 1) & 3);
+        from[kLoadsA + q] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.b.row_bytes + part * 16;
     }
-#pragma unroll
-    for (int q = 0; q < kLoadsS; ++q) {
-        const int row = (q * kWaves + wave) * 64 + lane;
-        if (row < BM) {
-            const int64_t r = m0 + row < p.a.rows ? m0 + row : p.a.rows - 1;
-            from[kLoadsA + kLoadsB + q] = p.a.scales + r * p.a.scale_bytes;
-        } else {
-            const int64_t r = n0 + row - BM < p.b.rows ? n0 + row - BM : p.b.rows - 1;
-            from[kLoadsA + kLoadsB + q] = p.b.scales + r * p.b.scale_bytes;
-        }
+    const uint8_t* scales_from;
+    {
+        const uint32_t row = threadIdx.x, in_a = row < rows_a ? row : rows_a - 1, in_b = row - BM < rows_b ? row - BM : rows_b - 1;
+        scales_from = row < BM ? p.a.scales + (m0 + in_a) * p.a.scale_bytes : p.b.scales + (n0 + in_b) * p.b.scale_bytes;
     }
     // Every call issues as many loads, so that they can be counted: past the last step the last one is loaded again, and not used.
     auto issue = [&](uint8_t* stage, int step) {
         const int k = step < p.steps ? step : p.steps - 1;
+        const uint8_t *a = a_values + (int64_t)k * kRowA, *b = b_values + (int64_t)k * kRowB;
 #pragma unroll
-        for (int q = 0; q < kLoadsA; ++q) copy16(from[q] + (int64_t)k * kRowA, stage + (q * kWaves + wave) * 1024);
+        for (int q = 0; q < kLoadsA; ++q) copy16(a + from[q], stage + (q * kWaves + wave) * 1024);
 #pragma unroll
-        for (int q = 0; q < kLoadsB; ++q) copy16(from[kLoadsA + q] + (int64_t)k * kRowB, stage + kA + (q * kWaves + wave) * 1024);
-#pragma unroll
-        for (int q = 0; q < kLoadsS; ++q) copy4(from[kLoadsA + kLoadsB + q] + (int64_t)k * 4, stage + kA + kB + (q * kWaves + wave) * 256);
+        for (int q = 0; q < kLoadsB; ++q) copy16(b + from[kLoadsA + q], stage + kA + (q * kWaves + wave) * 1024);
+    };
+    const int whole = p.steps / 4, rest = p.steps - whole * 4;       // fours, and steps behind them
+    // The last scales of a row come as its last 16 bytes, those of the steps behind the last four at their end.
+    auto issue_scales = [&](int four) {
+        const int at = four * 16 < p.steps * 4 - 16 ? four * 16 : p.steps * 4 - 16;
+        copy16(scales_from + at, scales + wave * 1024);
     };
 
     f32x4 acc[TM][TN];
@@ -125,58 +135,80 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     // (rows 16 further on have the same exchange of parts)
     const int at_a = FA == SSGD_MX_FP4 ? row_a * 64 + (g ^ ((row_a >> 1) & 3)) * 16 : row_a * 128 + (g ^ (row_a & 7)) * 16;
     const int at_b = kA + row_b * 64 + (g ^ ((row_b >> 1) & 3)) * 16;
-    const int at_sa = kA + kB + row_a * 4 + g, at_sb = kA + kB + (BM + row_b) * 4 + g;
 
-    auto contract = [&](const uint8_t* stage) {
-        ints8 a[TM], b[TN];
-        uint32_t sa[TM], sb[TN];
+    uint32_t sa[TM], sb[TN];
+    auto read_scales = [&](int skipped) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            b[j] = operand(*reinterpret_cast<const words4*>(stage + at_b + j * 16 * 64));
-            sb[j] = stage[at_sb + j * 64];
-        }
+        for (int j = 0; j < TN; ++j) sb[j] = scales_of_four(*reinterpret_cast<const words4*>(scales + (BM + row_b + j * 16) * 16), g) >> (8 * skipped);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sa[i] = scales_of_four(*reinterpret_cast<const words4*>(scales + (row_a + i * 16) * 16), g) >> (8 * skipped);
+    };
+    auto contract = [&](const uint8_t* stage, auto byte) {
+        ints8 a[TM], b[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = operand(*reinterpret_cast<const words4*>(stage + at_b + j * 16 * 64));
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             if constexpr (FA == SSGD_MX_FP4) a[i] = operand(*reinterpret_cast<const words4*>(stage + at_a + i * 16 * 64));
             else a[i] = operand(*reinterpret_cast<const words4*>(stage + at_a + i * 16 * 128), *reinterpret_cast<const words4*>(stage + (at_a ^ 64) + i * 16 * 128));
-            sa[i] = stage[at_sa + i * 64];
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mfma<FA>(b[j], a[i], acc[i][j], sb[j], sa[i]);
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma<FA, decltype(byte)::value>(b[j], a[i], acc[i][j], sb[j], sa[i]);
     };
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    constexpr std::integral_constant<int, 2> k2{};
+    constexpr std::integral_constant<int, 3> k3{};
 
+    if (whole > 0) issue_scales(0);
+    else {
+        // rows of one to three words
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = q >= 4 - rest ? *reinterpret_cast<const uint32_t*>(scales_from + (q - 4 + rest) * 4) : 0u;
+        *reinterpret_cast<words4*>(scales + threadIdx.x * 16) = words4{w[0], w[1], w[2], w[3]};
+    }
     issue(stage0, 0);
-    if constexpr (STAGES > 2) issue(stage1, 1);
-    if constexpr (STAGES > 3) issue(stage2, 2);
+    if constexpr (STAGES > 2) { issue(stage1, 1); issue(stage2, 2); }
     // A stage is read when its own loads have arrived in every wave, and loaded again only behind the next meeting, when all have read it.
+    // The counts are those of the loads issued after it: STAGES - 2 steps, and between steps 1 and 3 the scales.
     constexpr int kFlying = kLoads * (STAGES - 2);
-    int k = 0;
-    for (; k + STAGES <= p.steps; k += STAGES) {
+    for (int f = 0; f < whole; ++f) {
         wait_and_meet<kFlying>();
-        issue(STAGES == 2 ? stage1 : (STAGES == 3 ? stage2 : stage3), k + STAGES - 1);
-        contract(stage0);
+        read_scales(0);
+        issue(STAGES > 2 ? stage3 : stage1, f * 4 + STAGES - 1);
+        contract(stage0, k0);
         wait_and_meet<kFlying>();
-        issue(stage0, k + STAGES);
-        contract(stage1);
+        issue(stage0, f * 4 + STAGES);
+        issue_scales(f + 1);
+        contract(stage1, k1);
+        wait_and_meet<kFlying + 1>();
+        issue(stage1, f * 4 + STAGES + 1);
+        contract(STAGES > 2 ? stage2 : stage0, k2);
+        wait_and_meet<kFlying + (STAGES > 2 ? 1 : 0)>();
+        issue(STAGES > 2 ? stage2 : stage0, f * 4 + STAGES + 2);
+        contract(STAGES > 2 ? stage3 : stage1, k3);
+    }
+    wait_and_meet<0>();
+    if (rest > 0) {
+        read_scales(4 - rest);
         if constexpr (STAGES > 2) {
-            wait_and_meet<kFlying>();
-            issue(stage1, k + STAGES + 1);
-            contract(stage2);
-        }
-        if constexpr (STAGES > 3) {
-            wait_and_meet<kFlying>();
-            issue(stage2, k + STAGES + 2);
-            contract(stage3);
+            contract(stage0, k0);
+            if (rest > 1) contract(stage1, k1);
+            if (rest > 2) contract(stage2, k2);
+        } else {
+            issue(stage1, whole * 4 + 1);
+            contract(stage0, k0);
+            wait_and_meet<0>();
+            issue(stage0, whole * 4 + 2);
+            if (rest > 1) contract(stage1, k1);
+            wait_and_meet<0>();
+            if (rest > 2) contract(stage0, k2);
         }
     }
-    // the last STAGES - 1 steps at most: their loads are on the way
-    wait_and_meet<0>();
-    if (k < p.steps) contract(stage0);
-    if constexpr (STAGES > 2) if (k + 1 < p.steps) contract(stage1);
-    if constexpr (STAGES > 3) if (k + 2 < p.steps) contract(stage2);
-    __builtin_amdgcn_s_waitcnt(0);      // nothing may still be on its way into LDS when the workgroup ends
+    // (the last meeting has seen every load arrive: nothing is on its way into LDS when the workgroup ends)
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -231,7 +263,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(Product p) {
                 for (int i = 0; i < TM; ++i) {
                     ints8 op;
                     if constexpr (FA == SSGD_MX_FP4) op = operand(av[i][q]); else op = operand(av[i][q], ah[i][q]);
-                    acc[i] = mfma<FA>(operand(bv[q]), op, acc[i], bs.w[q] >> (8 * g), as[i].w[q] >> (8 * g));
+                    acc[i] = mfma<FA, 0>(operand(bv[q]), op, acc[i], bs.w[q] >> (8 * g), as[i].w[q] >> (8 * g));
                 }
         } else {
             for (int q = k; q < p.steps; ++q) {
@@ -242,7 +274,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(Product p) {
                     ints8 op;
                     if constexpr (FA == SSGD_MX_FP4) op = operand(*reinterpret_cast<const words4*>(a[i] + (int64_t)q * 64));
                     else op = operand(*reinterpret_cast<const words4*>(a[i] + (int64_t)q * 128), *reinterpret_cast<const words4*>(a[i] + (int64_t)q * 128 + 64));
-                    acc[i] = mfma<FA>(operand(bv), op, acc[i], bs, sa[i][(int64_t)q * 4 + g]);
+                    acc[i] = mfma<FA, 0>(operand(bv), op, acc[i], bs, sa[i][(int64_t)q * 4 + g]);
                 }
             }
         }
@@ -293,11 +325,11 @@ void launch(const Product& p, hipStream_t s) {
     if (p.a.rows <= 16) few_rows<FA, 1, T>(p, s);
     else if (p.a.rows <= 32) few_rows<FA, 2, T>(p, s);
     else if (p.a.rows <= 64) few_rows<FA, 4, T>(p, s);
-    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, 4, T>(p, s);
-    else tiles<FA, 256, 256, 2, 4, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
+    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 2, T>(p, s);
+    else tiles<FA, 256, 256, 2, 4, FA == SSGD_MX_FP4 ? 4 : 2, T>(p, s);
 }
 
-constexpr int64_t kMostRows = int64_t(1) << 31, kMostCols = int64_t(1) << 31;
+constexpr int64_t kMostRows = int64_t(1) << 31, kMostCols = (int64_t(1) << 24) - kMxPad;
 bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
 
 ssgd_status product(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K,
@@ -320,7 +352,7 @@ ssgd_status product(const void* a_values, const void* a_scales, int32_t a_fmt, i
 
 const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, const void* out, int32_t out_dtype, int64_t out_pitch) {
     if (!format_ok(a_fmt) || !dtype_ok(out_dtype)) return "mx product: a format and an output type of the enumerations";
-    if (M < 0 || N < 0 || K < 0 || M >= kMostRows || N >= kMostRows || K >= kMostCols || out_pitch < N) return "mx product: M, N, K from zero to 2^31, pitch >= N";
+    if (M < 0 || N < 0 || K < 0 || M >= kMostRows || N >= kMostRows || K > kMostCols || out_pitch < N) return "mx product: M and N from zero to 2^31, K to 2^24 - 128, pitch >= N";
     if (M == 0 || N == 0) return nullptr;
     if ((M + 127) / 128 * ((N + 127) / 128) > kMostBlocks) return "mx product: too many results";
     if (K > 0 && (!b_values || !b_scales || !aligned(b_values, 16) || !aligned(b_scales, 16))) return "mx product: values and scales are 16-byte aligned arrays";
@@ -344,7 +376,7 @@ ssgd_status ssgd_mx_matmul(const void* a_values, const void* a_scales, int32_t a
 }
 
 int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t K) {
-    if (!format_ok(a_fmt) || M < 0 || K < 0 || M >= kMostRows || K >= kMostCols) return -1;
+    if (!format_ok(a_fmt) || M < 0 || K < 0 || M >= kMostRows || K > kMostCols) return -1;
     return M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock);
 }
 
