@@ -60,9 +60,10 @@ template <int VM> __device__ __forceinline__ void wait_and_meet() {
 }
 
 // WM x WN waves, a tile of BM x BN.  A step is 128 columns: rows of A (64 or 128 bytes) and rows of B (64) in a stage of LDS, in which the
-// 16-byte parts of a row change places by its number, so that the lanes that read one part of 16 rows meet in no bank.  Scales come for four
-// steps at a time, 16 bytes of a row: four bytes of every row per step would be as many cache lines again as the values take.  They wait in
-// registers from the first of the four steps on, one word per row, so their place in LDS is free for the next four behind the next meeting.
+// 16-byte parts of a row change places by its number, so that the lanes that read one part of 16 rows meet in no bank.  Scales come for a
+// group of steps at a time (four, with three stages three), 16 bytes of a row: four bytes of every row per step would be as many cache lines
+// again as the values take.  They wait in registers from the first step of the group on, one word per row, so their place in LDS is free for
+// the next ones behind the next meeting.
 template <int FA, int BM, int BN, int WM, int WN, int STAGES, typename T>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int kWaves = WM * WN, kRowA = FA == SSGD_MX_FP4 ? 64 : 128, kRowB = 64;
@@ -70,12 +71,13 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves, kLoads = kLoadsA + kLoadsB;
     static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && BM + BN == 64 * kWaves, "every wave loads the same share");
-    static_assert(STAGES == 2 || STAGES == 4, "four steps end at the stage they began with");
+    constexpr int kGroupSteps = STAGES == 3 ? 3 : 4;
+    static_assert(STAGES >= 2 && STAGES <= 4, "a group ends at the stage it began with");
     // (arrays of their own: the compiler then sees that loads into one do not concern reads of another)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage2[STAGES > 2 ? kStage : 16];
-    __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 2 ? kStage : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 3 ? kStage : 16];
     __shared__ __attribute__((aligned(1024))) uint8_t scales[(BM + BN) * 16];
 
     // Workgroups go to the XCDs in turn; each XCD takes tiles that lie together, in groups of 8 rows of tiles, so that its L2 holds what
@@ -118,11 +120,13 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
 #pragma unroll
         for (int q = 0; q < kLoadsB; ++q) copy16(b + from[kLoadsA + q], stage + kA + (q * kWaves + wave) * 1024);
     };
-    const int whole = p.steps / 4, rest = p.steps - whole * 4;       // fours, and steps behind them
-    // The last scales of a row come as its last 16 bytes, those of the steps behind the last four at their end.
-    auto issue_scales = [&](int four) {
-        const int at = four * 16 < p.steps * 4 - 16 ? four * 16 : p.steps * 4 - 16;
-        copy16(scales_from + at, scales + wave * 1024);
+    const int whole = p.steps / kGroupSteps;       // groups
+    // Where 16 bytes from a group's first scale on would pass the end of the row, its last 16 bytes come instead; `first` is the place of the
+    // group's first scale in them.  Rows of less than 16 bytes are put together at the start.
+    auto first_of = [&](int f) { return f * kGroupSteps + 4 <= p.steps ? 0 : f * kGroupSteps + 4 - p.steps; };
+    auto issue_scales = [&](int f) {
+        const int at = f * kGroupSteps + 4 <= p.steps ? f * kGroupSteps * 4 : p.steps * 4 - 16;
+        copy16(scales_from + (at > 0 ? at : 0), scales + wave * 1024);
     };
 
     f32x4 acc[TM][TN];
@@ -162,50 +166,63 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr std::integral_constant<int, 2> k2{};
     constexpr std::integral_constant<int, 3> k3{};
 
-    if (whole > 0) issue_scales(0);
+    if (p.steps >= 4) issue_scales(0);
     else {
-        // rows of one to three words
         uint32_t w[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = q >= 4 - rest ? *reinterpret_cast<const uint32_t*>(scales_from + (q - 4 + rest) * 4) : 0u;
+        for (int q = 0; q < 4; ++q) w[q] = q >= 4 - p.steps ? *reinterpret_cast<const uint32_t*>(scales_from + (q - 4 + p.steps) * 4) : 0u;
         *reinterpret_cast<words4*>(scales + threadIdx.x * 16) = words4{w[0], w[1], w[2], w[3]};
     }
     issue(stage0, 0);
-    if constexpr (STAGES > 2) { issue(stage1, 1); issue(stage2, 2); }
+    if constexpr (STAGES > 2) issue(stage1, 1);
+    if constexpr (STAGES > 3) issue(stage2, 2);
     // A stage is read when its own loads have arrived in every wave, and loaded again only behind the next meeting, when all have read it.
-    // The counts are those of the loads issued after it: STAGES - 2 steps, and between steps 1 and 3 the scales.
+    // The counts are those of the loads issued after it: STAGES - 2 steps, and from the second step of a group on its successor's scales
+    // until the steps issued with them are read.
     constexpr int kFlying = kLoads * (STAGES - 2);
-    for (int f = 0; f < whole; ++f) {
-        wait_and_meet<kFlying>();
-        read_scales(0);
-        issue(STAGES > 2 ? stage3 : stage1, f * 4 + STAGES - 1);
-        contract(stage0, k0);
-        wait_and_meet<kFlying>();
-        issue(stage0, f * 4 + STAGES);
-        issue_scales(f + 1);
-        contract(stage1, k1);
-        wait_and_meet<kFlying + 1>();
-        issue(stage1, f * 4 + STAGES + 1);
-        contract(STAGES > 2 ? stage2 : stage0, k2);
-        wait_and_meet<kFlying + (STAGES > 2 ? 1 : 0)>();
-        issue(STAGES > 2 ? stage2 : stage0, f * 4 + STAGES + 2);
-        contract(STAGES > 2 ? stage3 : stage1, k3);
+    if (p.steps >= 4) {
+        for (int f = 0; f < whole; ++f) {
+            const int k = f * kGroupSteps;
+            wait_and_meet<kFlying>();
+            read_scales(first_of(f));
+            issue(STAGES == 2 ? stage1 : (STAGES == 3 ? stage2 : stage3), k + STAGES - 1);
+            contract(stage0, k0);
+            wait_and_meet<kFlying>();
+            issue(stage0, k + STAGES);
+            issue_scales(f + 1);
+            contract(stage1, k1);
+            wait_and_meet<kFlying + 1>();
+            issue(stage1, k + STAGES + 1);
+            contract(STAGES > 2 ? stage2 : stage0, k2);
+            if constexpr (STAGES != 3) {
+                wait_and_meet<kFlying + (STAGES > 3 ? 1 : 0)>();
+                issue(STAGES > 3 ? stage2 : stage0, k + STAGES + 2);
+                contract(STAGES > 3 ? stage3 : stage1, k3);
+            }
+        }
     }
+    const int done = p.steps >= 4 ? whole * kGroupSteps : 0, left = p.steps - done;
     wait_and_meet<0>();
-    if (rest > 0) {
-        read_scales(4 - rest);
-        if constexpr (STAGES > 2) {
+    if (left > 0) {
+        read_scales(p.steps >= 4 ? first_of(whole) : 4 - p.steps);
+        if constexpr (STAGES > 3) {
             contract(stage0, k0);
-            if (rest > 1) contract(stage1, k1);
-            if (rest > 2) contract(stage2, k2);
+            if (left > 1) contract(stage1, k1);
+            if (left > 2) contract(stage2, k2);
+        } else if constexpr (STAGES > 2) {
+            issue(stage2, done + 2);
+            contract(stage0, k0);
+            if (left > 1) contract(stage1, k1);
+            wait_and_meet<0>();
+            if (left > 2) contract(stage2, k2);
         } else {
-            issue(stage1, whole * 4 + 1);
+            issue(stage1, done + 1);
             contract(stage0, k0);
             wait_and_meet<0>();
-            issue(stage0, whole * 4 + 2);
-            if (rest > 1) contract(stage1, k1);
+            issue(stage0, done + 2);
+            if (left > 1) contract(stage1, k1);
             wait_and_meet<0>();
-            if (rest > 2) contract(stage0, k2);
+            if (left > 2) contract(stage0, k2);
         }
     }
     // (the last meeting has seen every load arrive: nothing is on its way into LDS when the workgroup ends)
@@ -325,8 +342,12 @@ void launch(const Product& p, hipStream_t s) {
     if (p.a.rows <= 16) few_rows<FA, 1, T>(p, s);
     else if (p.a.rows <= 32) few_rows<FA, 2, T>(p, s);
     else if (p.a.rows <= 64) few_rows<FA, 4, T>(p, s);
-    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 2, T>(p, s);
-    else tiles<FA, 256, 256, 2, 4, FA == SSGD_MX_FP4 ? 4 : 2, T>(p, s);
+    // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 281 us in 4 bits against 410 with tiles of 128; 1000 x 8192 x 8192, 128
+    // tiles: 59 against 55).  Stages: as many as LDS holds, for tiles of 128 of two workgroups per CU (2100 x 1500 x 4001 in 8 bits: 30 us with
+    // two, 22 with three; 4001 x 2100 x 1500 27 and 23, with four and one workgroup per CU 28).
+    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
+    else if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
+    else tiles<FA, 256, 256, 4, 2, 3, T>(p, s);
 }
 
 constexpr int64_t kMostRows = int64_t(1) << 31, kMostCols = (int64_t(1) << 24) - kMxPad;
