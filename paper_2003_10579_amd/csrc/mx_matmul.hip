@@ -45,6 +45,13 @@ __device__ __forceinline__ void store_four(const Product& p, int64_t m, int64_t 
     store_vec<4>(static_cast<T*>(p.out) + m * p.pitch + n, p.b.rows - n, x);
 }
 
+template <typename T>
+__device__ __forceinline__ void store_eight(const Product& p, int64_t m, int64_t n, const f32x4& c, const f32x4& d) {
+    if (m >= p.a.rows || n >= p.b.rows) return;
+    const float x[8] = {c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
+    store_vec<8>(static_cast<T*>(p.out) + m * p.pitch + n, p.b.rows - n, x);
+}
+
 // ---- tiles ---------------------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) uint32_t lds_word;
 typedef const __attribute__((address_space(1))) uint32_t global_word;
@@ -58,7 +65,6 @@ template <int VM> __device__ __forceinline__ void wait_and_meet() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-
 // WM x WN waves, a tile of BM x BN.  A step is 128 columns: rows of A (64 or 128 bytes) and rows of B (64) in a stage of LDS, in which the
 // 16-byte parts of a row change places by its number, so that the lanes that read one part of 16 rows meet in no bank.  Scales come for a
 // group of steps at a time (four, with three stages three), 16 bytes of a row: four bytes of every row per step would be as many cache lines
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     }
 #pragma unroll
     for (int q = 0; q < kLoadsB; ++q) {
-        const uint32_t unit = (q * kWaves + wave) * 64 + lane, row = unit / 4, part = (unit % 4) ^ ((row >> 1) & 3);
+        const uint32_t unit = (q * kWaves + wave) * 64 + lane, row = unit / 4, part = (unit % 4) ^ ((row >> 3) & 3);
         from[kLoadsA + q] = (row < rows_b ? row : rows_b - 1) * (uint32_t)p.b.row_bytes + part * 16;
     }
     const uint8_t* scales_from;
@@ -135,22 +141,25 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int r16 = lane & 15, g = lane >> 4;
-    const int row_a = (wave / WN) * TM * 16 + r16, row_b = (wave % WN) * TN * 16 + r16;
-    // (rows 16 further on have the same exchange of parts)
+    // Rows of B: of two tiles of 16 that lie together, the first takes four of every eight and the second the others, so that a lane's results in both
+    // are eight columns side by side.
+    const int row_a = (wave / WN) * TM * 16 + r16, col = (wave % WN) * TN * 16, row_b = col + (r16 >> 2) * 8 + (r16 & 3);
+    constexpr auto row_of = [](int j) { return j / 2 * 32 + j % 2 * 4; };
+    // (rows of A 16 further on, and rows of B 4 or 32, have the same exchange of parts)
     const int at_a = FA == SSGD_MX_FP4 ? row_a * 64 + (g ^ ((row_a >> 1) & 3)) * 16 : row_a * 128 + (g ^ (row_a & 7)) * 16;
-    const int at_b = kA + row_b * 64 + (g ^ ((row_b >> 1) & 3)) * 16;
+    const int at_b = kA + row_b * 64 + (g ^ ((row_b >> 3) & 3)) * 16;
 
     uint32_t sa[TM], sb[TN];
     auto read_scales = [&](int skipped) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sb[j] = scales_of_four(*reinterpret_cast<const words4*>(scales + (BM + row_b + j * 16) * 16), g) >> (8 * skipped);
+        for (int j = 0; j < TN; ++j) sb[j] = scales_of_four(*reinterpret_cast<const words4*>(scales + (BM + row_b + row_of(j)) * 16), g) >> (8 * skipped);
 #pragma unroll
         for (int i = 0; i < TM; ++i) sa[i] = scales_of_four(*reinterpret_cast<const words4*>(scales + (row_a + i * 16) * 16), g) >> (8 * skipped);
     };
     auto contract = [&](const uint8_t* stage, auto byte) {
         ints8 a[TM], b[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = operand(*reinterpret_cast<const words4*>(stage + at_b + j * 16 * 64));
+        for (int j = 0; j < TN; ++j) b[j] = operand(*reinterpret_cast<const words4*>(stage + at_b + row_of(j) * 64));
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             if constexpr (FA == SSGD_MX_FP4) a[i] = operand(*reinterpret_cast<const words4*>(stage + at_a + i * 16 * 64));
@@ -229,87 +238,156 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-            store_four<T>(p, m0 + row_a + i * 16, n0 + row_b - r16 + j * 16 + g * 4, acc[i][j]);
+        for (int j = 0; j < TN; j += 2) store_eight<T>(p, m0 + row_a + i * 16, n0 + col + j * 16 + g * 8, acc[i][j], acc[i][j + 1]);
 }
 
 // ---- few rows of A ---------------------------------------------------------------------------------------------------
-// Bound by reading B: a workgroup takes 16 rows of B and all of A, its waves take 512 columns in turn, with B and A straight from global
-// memory to registers, and their sums are added through LDS.
-struct __attribute__((packed, aligned(4))) Scales4 { uint32_t w[4]; };
+// A workgroup takes 16 or 32 rows of B and all of A, its waves take four steps of 128 columns in turn, with B and A straight from global memory to
+// registers, and their sums are added through LDS in the waves' order.  Bound by reading B while A is a row or a few (16384 x 4096, one row:
+// 8.1 us, 4.4 TB/s), by A's way from L2 to every workgroup from 16 rows on.
+constexpr int kAhead = 4;
+struct __attribute__((packed, aligned(4))) Scales { uint32_t w[kAhead]; };
 
-template <int FA, int TM, int WAVES, typename T>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(Product p) {
-    __shared__ f32x4 part[WAVES > 1 ? WAVES - 1 : 1][TM][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (TM * 16);
-    const int64_t rb = n0 + r16 < p.b.rows ? n0 + r16 : p.b.rows - 1;
-    const uint8_t *b = p.b.values + rb * p.b.row_bytes + g * 16, *sb = p.b.scales + rb * p.b.scale_bytes;
-    const uint8_t *a[TM], *sa[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t ra = m0 + i * 16 + r16 < p.a.rows ? m0 + i * 16 + r16 : p.a.rows - 1;
-        a[i] = p.a.values + ra * p.a.row_bytes + g * 16;
-        sa[i] = p.a.scales + ra * p.a.scale_bytes;
-    }
-    f32x4 acc[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = wave * 4; k < p.steps; k += WAVES * 4) {
-        if (k + 4 <= p.steps) {
-            words4 bv[4], av[TM][4], ah[TM][4];
-            const Scales4 bs = *reinterpret_cast<const Scales4*>(sb + (int64_t)k * 4);
-            Scales4 as[TM];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) bv[q] = *reinterpret_cast<const words4*>(b + (int64_t)(k + q) * 64);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                as[i] = *reinterpret_cast<const Scales4*>(sa[i] + (int64_t)k * 4);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if constexpr (FA == SSGD_MX_FP4) av[i][q] = *reinterpret_cast<const words4*>(a[i] + (int64_t)(k + q) * 64);
-                    else {
-                        av[i][q] = *reinterpret_cast<const words4*>(a[i] + (int64_t)(k + q) * 128);
-                        ah[i][q] = *reinterpret_cast<const words4*>(a[i] + (int64_t)(k + q) * 128 + 64);
-                    }
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    ints8 op;
-                    if constexpr (FA == SSGD_MX_FP4) op = operand(av[i][q]); else op = operand(av[i][q], ah[i][q]);
-                    acc[i] = mfma<FA, 0>(operand(bv[q]), op, acc[i], bs.w[q] >> (8 * g), as[i].w[q] >> (8 * g));
-                }
-        } else {
-            for (int q = k; q < p.steps; ++q) {
-                const words4 bv = *reinterpret_cast<const words4*>(b + (int64_t)q * 64);
-                const uint32_t bs = sb[(int64_t)q * 4 + g];
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    ints8 op;
-                    if constexpr (FA == SSGD_MX_FP4) op = operand(*reinterpret_cast<const words4*>(a[i] + (int64_t)q * 64));
-                    else op = operand(*reinterpret_cast<const words4*>(a[i] + (int64_t)q * 128), *reinterpret_cast<const words4*>(a[i] + (int64_t)q * 128 + 64));
-                    acc[i] = mfma<FA, 0>(operand(bv), op, acc[i], bs, sa[i][(int64_t)q * 4 + g]);
-                }
-            }
-        }
-    }
+template <int FA>
+__device__ __forceinline__ ints8 operand_at(const uint8_t* a, int64_t step) {
+    if constexpr (FA == SSGD_MX_FP4) return operand(*reinterpret_cast<const words4*>(a + step * 64));
+    else return operand(*reinterpret_cast<const words4*>(a + step * 128), *reinterpret_cast<const words4*>(a + step * 128 + 64));
+}
+
+// The sums of the waves, and the results.
+template <int TM, int TN, int WAVES, typename T>
+__device__ __forceinline__ void join_and_store(const Product& p, f32x4 (&acc)[TM][TN], f32x4 (*part)[TM * TN][64], int wave, int64_t m0, int64_t n0) {
+    const int lane = threadIdx.x & 63;
     if constexpr (WAVES > 1) {
         if (wave > 0) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) part[wave - 1][i][lane] = acc[i];
+            for (int i = 0; i < TM * TN; ++i) part[wave - 1][i][lane] = acc[i / TN][i % TN];
         }
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
         for (int w = 0; w < WAVES - 1; ++w)
 #pragma unroll
-            for (int i = 0; i < TM; ++i) acc[i] += part[w][i][lane];
+            for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] += part[w][i][lane];
     }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) store_four<T>(p, m0 + i * 16 + r16, n0 + g * 4, acc[i]);
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) store_four<T>(p, m0 + i * 16 + (lane & 15), n0 + j * 16 + (lane >> 4) * 4, acc[i][j]);
+}
+
+template <int FA, int TM, int TN, int WAVES, typename T>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(Product p) {
+    __shared__ f32x4 part[WAVES > 1 ? WAVES - 1 : 1][TM * TN][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * (TN * 16), m0 = (int64_t)blockIdx.y * (TM * 16);
+    const uint8_t *a[TM], *sa[TM], *b[TN], *sb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t rb = n0 + j * 16 + r16 < p.b.rows ? n0 + j * 16 + r16 : p.b.rows - 1;
+        b[j] = p.b.values + rb * p.b.row_bytes + g * 16;
+        sb[j] = p.b.scales + rb * p.b.scale_bytes;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t ra = m0 + i * 16 + r16 < p.a.rows ? m0 + i * 16 + r16 : p.a.rows - 1;
+        a[i] = p.a.values + ra * p.a.row_bytes + g * 16;
+        sa[i] = p.a.scales + ra * p.a.scale_bytes;
+    }
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = wave * kAhead; k < p.steps; k += WAVES * kAhead) {
+        if (k + kAhead <= p.steps) {
+            words4 bv[TN][kAhead];
+            ints8 av[TM][kAhead];
+            Scales as[TM], bs[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                bs[j] = *reinterpret_cast<const Scales*>(sb[j] + (int64_t)k * 4);
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) bv[j][q] = *reinterpret_cast<const words4*>(b[j] + (int64_t)(k + q) * 64);
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                as[i] = *reinterpret_cast<const Scales*>(sa[i] + (int64_t)k * 4);
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) av[i][q] = operand_at<FA>(a[i], k + q);
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int i = 0; i < TM * TN; ++i)
+                    acc[i / TN][i % TN] = mfma<FA, 0>(operand(bv[i % TN][q]), av[i / TN][q], acc[i / TN][i % TN], bs[i % TN].w[q] >> (8 * g), as[i / TN].w[q] >> (8 * g));
+        } else {
+            for (int q = k; q < p.steps; ++q) {
+                ints8 bv[TN];
+                uint32_t bs[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) { bv[j] = operand(*reinterpret_cast<const words4*>(b[j] + (int64_t)q * 64)); bs[j] = sb[j][(int64_t)q * 4 + g]; }
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const ints8 av = operand_at<FA>(a[i], q);
+                    const uint32_t as = sa[i][(int64_t)q * 4 + g];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma<FA, 0>(bv[j], av, acc[i][j], bs[j], as);
+                }
+            }
+        }
+    }
+    join_and_store<TM, TN, WAVES, T>(p, acc, part, wave, m0, n0);
+}
+
+// The same for at most two rows that are quantised on the way, by every workgroup for itself, into LDS: as many bytes as its part of B at most,
+// and one launch instead of two.  The first loads of B are on their way meanwhile.
+constexpr int kRoomForRows = 32768;       // bytes of quantised rows and their scales
+struct Rows { const void* x; int64_t pitch, cols; };
+
+template <int FA, int WAVES, typename X, typename T>
+__global__ __launch_bounds__(64 * WAVES) void one_row_kernel(Product p, Rows x) {
+    __shared__ f32x4 part[WAVES - 1][1][64];
+    __shared__ __attribute__((aligned(16))) uint8_t rows[kRoomForRows];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t rb = n0 + r16 < p.b.rows ? n0 + r16 : p.b.rows - 1;
+    const uint8_t *b = p.b.values + rb * p.b.row_bytes + g * 16, *sb = p.b.scales + rb * p.b.scale_bytes;
+    const int many = (int)p.a.rows, row_bytes = (int)p.a.row_bytes, scale_bytes = (int)p.a.scale_bytes;
+    uint8_t* scales = rows + many * row_bytes;
+    words4 bv[kAhead];
+    uint32_t bs[kAhead];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int64_t s = k + q < p.steps ? k + q : p.steps - 1;
+            bv[q] = *reinterpret_cast<const words4*>(b + s * 64);
+            bs[q] = *reinterpret_cast<const uint32_t*>(sb + s * 4);
+        }
+    };
+    load(wave * kAhead);
+    const int per_row = p.steps * 16;                  // groups of eight columns
+    for (int u = threadIdx.x; u < many * per_row; u += 64 * WAVES) {
+        const int row = u / per_row, col = (u - row * per_row) * 8;
+        float v[8];
+        load_vec<8>(static_cast<const X*>(x.x) + row * x.pitch + col, x.cols - col, v);
+        uint32_t most = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(v[q]));
+        const uint32_t byte = mx_scale_byte<FA>(max_of_4(most));
+        if constexpr (FA == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(rows + row * row_bytes + col / 2) = mx_pack_fp4(v, byte);
+        else *reinterpret_cast<words2*>(rows + row * row_bytes + col) = mx_pack_fp8(v, byte);
+        if ((threadIdx.x & 3) == 0) scales[row * scale_bytes + col / kMxBlock] = (uint8_t)byte;
+    }
+    __syncthreads();
+    const int ra = r16 < many ? r16 : many - 1;
+    const uint8_t *a = rows + ra * row_bytes + g * 16, *sa = scales + ra * scale_bytes + g;
+    f32x4 acc[1][1] = {{f32x4{0.0f, 0.0f, 0.0f, 0.0f}}};
+    for (int k = wave * kAhead; k < p.steps; k += WAVES * kAhead) {
+        if (k > wave * kAhead) load(k);
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (k + q < p.steps) acc[0][0] = mfma<FA, 0>(operand(bv[q]), operand_at<FA>(a, k + q), acc[0][0], bs[q] >> (8 * g), sa[(k + q) * 4]);
+    }
+    join_and_store<1, 1, WAVES, T>(p, acc, part, wave, 0, n0);
 }
 
 template <typename T>
@@ -318,15 +396,18 @@ __global__ __launch_bounds__(256) void zero_kernel(T* out, int64_t rows, int64_t
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
-template <int FA, int TM, typename T>
+template <int FA, int TM, int TN, int WAVES, typename T>
 void few_rows(const Product& p, hipStream_t s) {
-    const dim3 grid((unsigned)((p.b.rows + 15) / 16), (unsigned)((p.a.rows + TM * 16 - 1) / (TM * 16)));
-    // about 4096 waves, none without columns
-    const int64_t want = 4096 / ((int64_t)grid.x * grid.y) + 1, most = (p.steps + 3) / 4;
-    if (want >= 16 && most >= 16) hipLaunchKernelGGL((few_rows_kernel<FA, TM, 16, T>), grid, dim3(1024), 0, s, p);
-    else if (want >= 8 && most >= 8) hipLaunchKernelGGL((few_rows_kernel<FA, TM, 8, T>), grid, dim3(512), 0, s, p);
-    else if (most >= 4) hipLaunchKernelGGL((few_rows_kernel<FA, TM, 4, T>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((few_rows_kernel<FA, TM, 1, T>), grid, dim3(64), 0, s, p);
+    const dim3 grid((unsigned)((p.b.rows + TN * 16 - 1) / (TN * 16)), (unsigned)((p.a.rows + TM * 16 - 1) / (TM * 16)));
+    if (p.steps <= kAhead) hipLaunchKernelGGL((few_rows_kernel<FA, TM, TN, 1, T>), grid, dim3(64), 0, s, p);
+    else hipLaunchKernelGGL((few_rows_kernel<FA, TM, TN, WAVES, T>), grid, dim3(64 * WAVES), 0, s, p);
+}
+
+// Waves of a workgroup for one group of 16 rows of A, with and without their quantisation (the sums of the same columns then add up alike).
+constexpr int kRowWaves = 8;
+template <int FA, typename X, typename T>
+void one_row(const Product& p, const Rows& x, hipStream_t s) {
+    hipLaunchKernelGGL((one_row_kernel<FA, kRowWaves, X, T>), dim3((unsigned)((p.b.rows + 15) / 16)), dim3(64 * kRowWaves), 0, s, p, x);
 }
 
 template <int FA, int BM, int BN, int WM, int WN, int STAGES, typename T>
@@ -339,11 +420,14 @@ void tiles(Product p, hipStream_t s) {
 
 template <int FA, typename T>
 void launch(const Product& p, hipStream_t s) {
-    if (p.a.rows <= 16) few_rows<FA, 1, T>(p, s);
-    else if (p.a.rows <= 32) few_rows<FA, 2, T>(p, s);
-    else if (p.a.rows <= 64) few_rows<FA, 4, T>(p, s);
-    // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 281 us in 4 bits against 410 with tiles of 128; 1000 x 8192 x 8192, 128
-    // tiles: 59 against 55).  Stages: as many as LDS holds, for tiles of 128 of two workgroups per CU (2100 x 1500 x 4001 in 8 bits: 30 us with
+    // 16 rows of B to a workgroup, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as often (61 x 6144 x 5000
+    // in 4 bits: 10.9 us against 14.7; 64 x 2048 x 4096: 10.3 against 8.6).
+    const bool pairs = p.b.rows >= 5120;
+    if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
+    else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
+    else if (p.a.rows <= 64) { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
+    // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 279 us in 4 bits against 403 with tiles of 128; 1000 x 8192 x 8192, 128
+    // tiles: 57 against 53).  Stages: as many as LDS holds, for tiles of 128 of two workgroups per CU (2100 x 1500 x 4001 in 8 bits: 30 us with
     // two, 22 with three; 4001 x 2100 x 1500 27 and 23, with four and one workgroup per CU 28).
     else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
     else if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
@@ -353,22 +437,37 @@ void launch(const Product& p, hipStream_t s) {
 constexpr int64_t kMostRows = int64_t(1) << 31, kMostCols = (int64_t(1) << 24) - kMxPad;
 bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
 
-ssgd_status product(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K,
-                    void* out, int32_t out_dtype, int64_t out_pitch, hipStream_t stream) {
-    if (K == 0) {
-        const dim3 grid(1024);
-        if (out_dtype == SSGD_F32) hipLaunchKernelGGL((zero_kernel<float>), grid, dim3(256), 0, stream, static_cast<float*>(out), M, N, out_pitch);
-        else hipLaunchKernelGGL((zero_kernel<bf16_t>), grid, dim3(256), 0, stream, static_cast<bf16_t*>(out), M, N, out_pitch);
-        return op_hip(hipGetLastError(), "mx product");
-    }
+Product product_of(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, void* out,
+                   int64_t out_pitch) {
     Product p{};
     const int64_t scale_bytes = mx_padded(K) / kMxBlock;
     p.a = {static_cast<const uint8_t*>(a_values), static_cast<const uint8_t*>(a_scales), M, mx_row_bytes(a_fmt, K), scale_bytes};
     p.b = {static_cast<const uint8_t*>(b_values), static_cast<const uint8_t*>(b_scales), N, mx_row_bytes(SSGD_MX_FP4, K), scale_bytes};
     p.out = out; p.pitch = out_pitch; p.steps = (int32_t)(mx_padded(K) / kMxPad);
+    return p;
+}
+
+ssgd_status zeros(int64_t M, int64_t N, void* out, int32_t out_dtype, int64_t out_pitch, hipStream_t stream) {
+    const dim3 grid(1024);
+    if (out_dtype == SSGD_F32) hipLaunchKernelGGL((zero_kernel<float>), grid, dim3(256), 0, stream, static_cast<float*>(out), M, N, out_pitch);
+    else hipLaunchKernelGGL((zero_kernel<bf16_t>), grid, dim3(256), 0, stream, static_cast<bf16_t*>(out), M, N, out_pitch);
+    return op_hip(hipGetLastError(), "mx product");
+}
+
+ssgd_status product(const Product& p, int32_t a_fmt, int32_t out_dtype, hipStream_t stream) {
     if (a_fmt == SSGD_MX_FP4) { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP4, float>(p, stream); else launch<SSGD_MX_FP4, bf16_t>(p, stream); }
     else { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP8, float>(p, stream); else launch<SSGD_MX_FP8, bf16_t>(p, stream); }
     return op_hip(hipGetLastError(), "mx product");
+}
+
+// Rows that each workgroup of the product quantises for itself (16384 x 4096: one row 10.1 us, 11 as two launches, and 3 us less for the host; four
+// rows 12.8 and 12).  Contractions of 512 columns and less leave one wave.
+bool quantises_itself(int32_t a_fmt, int64_t M, int64_t K) { return M <= 2 && mx_padded(K) > kAhead * kMxPad && M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock) <= kRoomForRows; }
+
+template <typename X>
+void one_row_of(const Product& p, const Rows& x, int32_t a_fmt, int32_t out_dtype, hipStream_t stream) {
+    if (a_fmt == SSGD_MX_FP4) { if (out_dtype == SSGD_F32) one_row<SSGD_MX_FP4, X, float>(p, x, stream); else one_row<SSGD_MX_FP4, X, bf16_t>(p, x, stream); }
+    else { if (out_dtype == SSGD_F32) one_row<SSGD_MX_FP8, X, float>(p, x, stream); else one_row<SSGD_MX_FP8, X, bf16_t>(p, x, stream); }
 }
 
 const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, const void* out, int32_t out_dtype, int64_t out_pitch) {
@@ -392,13 +491,15 @@ ssgd_status ssgd_mx_matmul(const void* a_values, const void* a_scales, int32_t a
         if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch)) return op_fail(SSGD_EINVAL, why);
         if (M == 0 || N == 0) return SSGD_OK;
         if (K > 0 && (!a_values || !a_scales || !aligned(a_values, 16) || !aligned(a_scales, 16))) return op_fail(SSGD_EINVAL, "mx product: values and scales are 16-byte aligned arrays");
-        return product(a_values, a_scales, a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch, static_cast<hipStream_t>(hip_stream));
+        const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        if (K == 0) return zeros(M, N, out, out_dtype, out_pitch, stream);
+        return product(product_of(a_values, a_scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, stream);
     });
 }
 
 int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t K) {
     if (!format_ok(a_fmt) || M < 0 || K < 0 || M >= kMostRows || K > kMostCols) return -1;
-    return M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock);
+    return quantises_itself(a_fmt, M, K) ? 0 : M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock);
 }
 
 ssgd_status ssgd_mx_linear(const void* x, int32_t dtype, int64_t pitch, int64_t M, int32_t a_fmt, const void* b_values, const void* b_scales, int64_t N, int64_t K,
@@ -406,13 +507,21 @@ ssgd_status ssgd_mx_linear(const void* x, int32_t dtype, int64_t pitch, int64_t 
     return op_entry([&]() -> ssgd_status {
         if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch)) return op_fail(SSGD_EINVAL, why);
         if (M == 0 || N == 0) return SSGD_OK;
-        uint8_t *values = static_cast<uint8_t*>(work), *scales = values + M * mx_row_bytes(a_fmt, K);
-        if (K > 0) {
-            if (!work || !aligned(work, 16)) return op_fail(SSGD_EINVAL, "mx linear: a 16-byte aligned work area");
-            const ssgd_status st = ssgd_mx_quantize(x, dtype, M, K, pitch, a_fmt, values, scales, 0, nullptr, nullptr, hip_stream);
-            if (st != SSGD_OK) return st;
+        const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+        if (K == 0) return zeros(M, N, out, out_dtype, out_pitch, stream);
+        if (quantises_itself(a_fmt, M, K)) {
+            if (!dtype_ok(dtype) || pitch < K) return op_fail(SSGD_EINVAL, "mx linear: a type of the enumeration, pitch >= K");
+            if (!x || !aligned(x, (uintptr_t)dtype_bytes(dtype))) return op_fail(SSGD_EINVAL, "mx linear: the rows are null or misaligned");
+            const Product p = product_of(nullptr, nullptr, a_fmt, M, b_values, b_scales, N, K, out, out_pitch);
+            const Rows rows{x, pitch, K};
+            if (dtype == SSGD_F32) one_row_of<float>(p, rows, a_fmt, out_dtype, stream); else one_row_of<bf16_t>(p, rows, a_fmt, out_dtype, stream);
+            return op_hip(hipGetLastError(), "mx linear");
         }
-        return product(values, scales, a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch, static_cast<hipStream_t>(hip_stream));
+        if (!work || !aligned(work, 16)) return op_fail(SSGD_EINVAL, "mx linear: a 16-byte aligned work area");
+        uint8_t *values = static_cast<uint8_t*>(work), *scales = values + M * mx_row_bytes(a_fmt, K);
+        const ssgd_status st = ssgd_mx_quantize(x, dtype, M, K, pitch, a_fmt, values, scales, 0, nullptr, nullptr, hip_stream);
+        if (st != SSGD_OK) return st;
+        return product(product_of(values, scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, stream);
     });
 }
 

@@ -46,7 +46,7 @@ def _close(got, a, b, fmt, dtype):
 
 # few rows (one, two and four groups of 16, partial ones), tiles of 128 and, from 200 tiles of 256 on, of 256; contractions from one column to
 # many steps of 128, each remainder of the stages; rows of B that are no multiple of anything
-SHAPES = [(1, 1, 1), (1, 3, 5), (1, 16, 128), (1, 17, 4096), (1, 300, 3072), (2, 512, 3071), (15, 33, 129), (16, 100, 640), (17, 100, 512), (32, 40, 2200), (33, 70, 1000),
+SHAPES = [(1, 1, 1), (1, 3, 5), (2, 50, 900), (3, 50, 900), (2, 40, 17000), (1, 5200, 700), (16, 5130, 600), (20, 5121, 513), (50, 5150, 1300), (1, 16, 128), (1, 17, 4096), (1, 300, 3072), (2, 512, 3071), (15, 33, 129), (16, 100, 640), (17, 100, 512), (32, 40, 2200), (33, 70, 1000),
           (61, 130, 5000), (64, 64, 8192), (65, 1, 100), (65, 127, 300), (100, 129, 129), (128, 128, 128), (129, 257, 256), (130, 130, 384), (300, 200, 512),
           (257, 513, 640), (512, 384, 1100), (3500, 3700, 127), (3585, 3600, 300), (3700, 3500, 700), (4000, 3500, 513)]
 
