@@ -243,6 +243,7 @@ int64_t ssgd_adamw_state_elements(int32_t tensors, const int64_t* sizes) {
     for (int32_t k = 0; k < tensors; ++k) {
         if (sizes[k] < 0 || sizes[k] > (int64_t(1) << 48)) return -1;
         total += (sizes[k] + kStateBlock - 1) / kStateBlock * kStateBlock;
+        if (total > (int64_t(1) << 48)) return -1;
     }
     return total;
 }

@@ -138,7 +138,8 @@ void launch_tiles(const Source& s, const Target& t, int fmt, const Target& tt, i
 #undef SSGD_TILES
 }
 
-bool fits(int64_t blocks) { return blocks <= kMostBlocks; }
+// rows x groups of eight columns in one launch (as a quotient: the product may pass 64 bits)
+bool fits(int64_t rows, int64_t per_row) { return rows <= kMostBlocks * kThreads / per_row; }
 
 }  // namespace
 
@@ -160,7 +161,7 @@ ssgd_status ssgd_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
             return op_fail(SSGD_EINVAL, "mx quantize: outputs are 16-byte aligned arrays of values and scales, formats of the enumeration");
         if (!x || !aligned(x, (uintptr_t)dtype_bytes(dtype))) return op_fail(SSGD_EINVAL, "mx quantize: the matrix is null or misaligned");
         if (across && rows >= kMostCols) return op_fail(SSGD_EINVAL, "mx quantize: too many rows to be columns");
-        if (!fits(across ? mx_padded(cols) / kTile * (mx_padded(rows) / kTile) : rows * (mx_padded(cols) / 8) / kThreads + 1)) return op_fail(SSGD_EINVAL, "mx quantize: too many elements");
+        if (across ? mx_padded(cols) / kTile * (mx_padded(rows) / kTile) > kMostBlocks : !fits(rows, mx_padded(cols) / 8)) return op_fail(SSGD_EINVAL, "mx quantize: too many elements");
         const Source s{x, rows, cols, pitch};
         const Target t{static_cast<uint8_t*>(values), static_cast<uint8_t*>(scales), mx_row_bytes(fmt, cols), mx_padded(cols) / kMxBlock};
         const Target tt{static_cast<uint8_t*>(values_t), static_cast<uint8_t*>(scales_t), mx_row_bytes(fmt_t, rows), mx_padded(rows) / kMxBlock};
@@ -180,8 +181,9 @@ ssgd_status ssgd_mx_dequantize(const void* values, const void* scales, int32_t f
         if (rows == 0 || cols == 0) return SSGD_OK;
         if (!values || !scales || !out || !aligned(values, 16) || !aligned(scales, 16) || !aligned(out, (uintptr_t)dtype_bytes(dtype)))
             return op_fail(SSGD_EINVAL, "mx dequantize: a buffer is null or misaligned");
-        const int64_t per_row = (cols + 7) / 8, groups = rows * per_row;
-        if (!fits(groups / kThreads + 1)) return op_fail(SSGD_EINVAL, "mx dequantize: too many elements");
+        const int64_t per_row = (cols + 7) / 8;
+        if (!fits(rows, per_row)) return op_fail(SSGD_EINVAL, "mx dequantize: too many elements");
+        const int64_t groups = rows * per_row;
         const int64_t rb = mx_row_bytes(fmt, cols), sb = mx_padded(cols) / kMxBlock;
         const dim3 grid((unsigned)((groups + kThreads - 1) / kThreads));
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

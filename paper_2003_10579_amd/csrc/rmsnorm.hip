@@ -16,6 +16,7 @@ using namespace ssgd;
 namespace {
 
 constexpr int kMostKept = 16384;      // columns that fit the registers of 1024 threads
+constexpr int64_t kMostColumns = int64_t(1) << 25;     // 16 to a workgroup of 1024 in the sums of dw: a launch ends at 2^32 threads
 constexpr int kTeams = 1024;          // rows at work at a time, and partial sums of dw
 
 struct Forward {
@@ -310,7 +311,7 @@ void launch_backward(const Backward& a, hipStream_t s) {
 }
 
 bool shape_ok(int32_t dtype, int32_t w_dtype, int64_t rows, int64_t d) {
-    return dtype_ok(dtype) && dtype_ok(w_dtype) && rows >= 0 && rows < (int64_t(1) << 40) && d >= 1 && d < (int64_t(1) << 30);
+    return dtype_ok(dtype) && dtype_ok(w_dtype) && rows >= 0 && rows < (int64_t(1) << 40) && d >= 1 && d < kMostColumns;
 }
 bool there(const void* p, int32_t dtype) { return p != nullptr && aligned(p, (uintptr_t)dtype_bytes(dtype)); }
 
@@ -323,7 +324,7 @@ ssgd_status ssgd_rmsnorm(const void* x, int64_t x_pitch, const void* residual, i
                          int64_t rows, int64_t d, double eps, void* sum, int64_t sum_pitch, void* y, int64_t y_pitch, void* values, void* scales, float* rstd,
                          void* hip_stream) {
     return op_entry([&]() -> ssgd_status {
-        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm: types of the enumeration, rows of zero or more, 1 <= d < 2^30");
+        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm: types of the enumeration, rows of zero or more, 1 <= d < 2^25");
         if (!(eps >= 0) || !std::isfinite(eps)) return op_fail(SSGD_EINVAL, "rmsnorm: eps of zero or more");
         if (rows == 0) return SSGD_OK;
         if (!there(x, dtype) || !there(weight, weight_dtype) || !there(rstd, SSGD_F32) || x_pitch < d) return op_fail(SSGD_EINVAL, "rmsnorm: x, weight and rstd, pitch >= d");
@@ -351,7 +352,7 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
                                   const float* rstd, const void* dsum, int64_t dsum_pitch, int64_t rows, int64_t d, void* dx, int64_t dx_pitch, float* dweight,
                                   float* work, void* hip_stream) {
     return op_entry([&]() -> ssgd_status {
-        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm backward: types of the enumeration, rows of zero or more, 1 <= d < 2^30");
+        if (!shape_ok(dtype, weight_dtype, rows, d)) return op_fail(SSGD_EINVAL, "rmsnorm backward: types of the enumeration, rows of zero or more, 1 <= d < 2^25");
         if (dweight != nullptr && (!aligned(dweight, 4) || (rows > 0 && (!work || !aligned(work, 16))))) return op_fail(SSGD_EINVAL, "rmsnorm backward: dweight needs a 16-byte aligned work area");
         if (rows > 0) {
             if (!there(dy, dtype) || !there(s, dtype) || !there(weight, weight_dtype) || !there(rstd, SSGD_F32) || !there(dx, dtype) || dy_pitch < d || s_pitch < d || dx_pitch < d)

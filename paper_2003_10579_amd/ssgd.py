@@ -613,7 +613,7 @@ def rmsnorm_backward(dy, s, weight, rstd, dsum=None):
     dw = _torch.empty(d, dtype=_torch.float32, device=dev)
     floats = _lib.ssgd_rmsnorm_work_floats(rows, d)
     if floats < 0:
-        _refuse("rmsnorm_backward: 1 <= columns < 2^30")
+        _refuse("rmsnorm_backward: 1 <= columns < 2^25")
     work = _torch.empty(floats, dtype=_torch.float32, device=dev)
     _call(_lib.ssgd_rmsnorm_backward, dev, dy.data_ptr(), pitch, s_at, s_pitch, w, kind, w_kind, rstd.data_ptr(), more, more_pitch, rows, d, dx.data_ptr(), d,
           dw.data_ptr(), work.data_ptr())
