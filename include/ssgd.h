@@ -277,13 +277,15 @@ ssgd_status ssgd_mx_dequantize(const void *values, const void *scales, int32_t f
 /* The product out[m][n] = sum over k of A[m][k] B[n][k] of microscaled matrices, A (M x K) in a_fmt, B (N x K) in SSGD_MX_FP4, both as
  * ssgd_mx_quantize lays them out; out M x N in out_dtype, rows out_pitch elements apart.  Accumulated in fp32 in a fixed order and
  * rounded once.  (The matrix unit adds 4-bit products exactly; of products of 8 by 4 bits it drops what is below about 2^-17 of the
- * largest of 128, an error of 4e-6 of a typical result.)  A block that is NaN makes the results that use it NaN.  K = 0 gives zeros; K is at most 2^24 - 128. */
+ * largest of 128, an error of 4e-6 of a typical result.)  A block that is NaN makes the results that use it NaN.  K = 0 gives zeros; K is at most 2^24 - 128.
+ * work: ssgd_mx_matmul_work_bytes bytes, 16-byte aligned (zero for most shapes: it holds the parts of a long contraction with few results). */
+int64_t ssgd_mx_matmul_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K);
 ssgd_status ssgd_mx_matmul(const void *a_values, const void *a_scales, int32_t a_fmt, int64_t M, const void *b_values,
                            const void *b_scales, int64_t N, int64_t K, void *out, int32_t out_dtype, int64_t out_pitch,
-                           void *hip_stream);
+                           void *work, void *hip_stream);
 /* The same for rows x (M x K, `dtype`) that are quantised to a_fmt on the way, the results those of ssgd_mx_quantize and
  * ssgd_mx_matmul.  work: ssgd_mx_linear_work_bytes bytes, 16-byte aligned. */
-int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t K);
+int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K);
 ssgd_status ssgd_mx_linear(const void *x, int32_t dtype, int64_t pitch, int64_t M, int32_t a_fmt, const void *b_values,
                            const void *b_scales, int64_t N, int64_t K, void *out, int32_t out_dtype, int64_t out_pitch, void *work,
                            void *hip_stream);

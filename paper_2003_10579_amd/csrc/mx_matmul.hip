@@ -20,6 +20,8 @@ struct Product {
     int64_t pitch;
     int32_t steps;          // of 128 columns
     int32_t tiles_m, tiles_n;
+    int32_t part_steps;     // tiles: steps of a part of the contraction (blockIdx.y), `steps` where it is not split
+    int64_t part_stride;    // elements between the results of two parts
 };
 
 // The scales are byte BYTE of their words.
@@ -86,19 +88,21 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 3 ? kStage : 16];
     __shared__ __attribute__((aligned(1024))) uint8_t scales[(BM + BN) * 16];
 
-    // Workgroups go to the XCDs in turn; each XCD takes tiles that lie together, in groups of 8 rows of tiles, so that its L2 holds what
+    // Workgroups go to the XCDs in turn; each XCD takes tiles that lie together, in groups of 4 rows of tiles, so that its L2 holds what
     // they share.
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, per_xcd = (tiles + kXcds - 1) / kXcds;
     const int64_t id = (int64_t)(blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
     if (blockIdx.x / kXcds >= per_xcd || id >= tiles) return;
-    constexpr int kGroup = 8;
+    constexpr int kGroup = 4;
     const int64_t group = id / (kGroup * (int64_t)p.tiles_n), in_group = id - group * kGroup * p.tiles_n;
     const int64_t height = p.tiles_m - group * kGroup < kGroup ? p.tiles_m - group * kGroup : kGroup;
     const int64_t m0 = (group * kGroup + in_group % height) * BM, n0 = in_group / height * BN;
 
+    const int begin = (int)blockIdx.y * p.part_steps, steps = p.steps - begin < p.part_steps ? p.steps - begin : p.part_steps;
+    p.out = static_cast<T*>(p.out) + blockIdx.y * p.part_stride;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (offsets from the tile's first row: 256 rows of less than 2^24 bytes)
-    const uint8_t *a_values = p.a.values + m0 * p.a.row_bytes, *b_values = p.b.values + n0 * p.b.row_bytes;
+    const uint8_t *a_values = p.a.values + m0 * p.a.row_bytes + (int64_t)begin * kRowA, *b_values = p.b.values + n0 * p.b.row_bytes + (int64_t)begin * kRowB;
     const uint32_t rows_a = (uint32_t)(p.a.rows - m0 < BM ? p.a.rows - m0 : BM), rows_b = (uint32_t)(p.b.rows - n0 < BN ? p.b.rows - n0 : BN);
     uint32_t from[kLoads];
 #pragma unroll
@@ -115,23 +119,23 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     const uint8_t* scales_from;
     {
         const uint32_t row = threadIdx.x, in_a = row < rows_a ? row : rows_a - 1, in_b = row - BM < rows_b ? row - BM : rows_b - 1;
-        scales_from = row < BM ? p.a.scales + (m0 + in_a) * p.a.scale_bytes : p.b.scales + (n0 + in_b) * p.b.scale_bytes;
+        scales_from = row < BM ? p.a.scales + (m0 + in_a) * p.a.scale_bytes + (int64_t)begin * 4 : p.b.scales + (n0 + in_b) * p.b.scale_bytes + (int64_t)begin * 4;
     }
     // Every call issues as many loads, so that they can be counted: past the last step the last one is loaded again, and not used.
     auto issue = [&](uint8_t* stage, int step) {
-        const int k = step < p.steps ? step : p.steps - 1;
+        const int k = step < steps ? step : steps - 1;
         const uint8_t *a = a_values + (int64_t)k * kRowA, *b = b_values + (int64_t)k * kRowB;
 #pragma unroll
         for (int q = 0; q < kLoadsA; ++q) copy16(a + from[q], stage + (q * kWaves + wave) * 1024);
 #pragma unroll
         for (int q = 0; q < kLoadsB; ++q) copy16(b + from[kLoadsA + q], stage + kA + (q * kWaves + wave) * 1024);
     };
-    const int whole = p.steps / kGroupSteps;       // groups
+    const int whole = steps / kGroupSteps;       // groups
     // Where 16 bytes from a group's first scale on would pass the end of the row, its last 16 bytes come instead; `first` is the place of the
     // group's first scale in them.  Rows of less than 16 bytes are put together at the start.
-    auto first_of = [&](int f) { return f * kGroupSteps + 4 <= p.steps ? 0 : f * kGroupSteps + 4 - p.steps; };
+    auto first_of = [&](int f) { return f * kGroupSteps + 4 <= steps ? 0 : f * kGroupSteps + 4 - steps; };
     auto issue_scales = [&](int f) {
-        const int at = f * kGroupSteps + 4 <= p.steps ? f * kGroupSteps * 4 : p.steps * 4 - 16;
+        const int at = f * kGroupSteps + 4 <= steps ? f * kGroupSteps * 4 : steps * 4 - 16;
         copy16(scales_from + (at > 0 ? at : 0), scales + wave * 1024);
     };
 
@@ -175,11 +179,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr std::integral_constant<int, 2> k2{};
     constexpr std::integral_constant<int, 3> k3{};
 
-    if (p.steps >= 4) issue_scales(0);
+    if (steps >= 4) issue_scales(0);
     else {
         uint32_t w[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = q >= 4 - p.steps ? *reinterpret_cast<const uint32_t*>(scales_from + (q - 4 + p.steps) * 4) : 0u;
+        for (int q = 0; q < 4; ++q) w[q] = q >= 4 - steps ? *reinterpret_cast<const uint32_t*>(scales_from + (q - 4 + steps) * 4) : 0u;
         *reinterpret_cast<words4*>(scales + threadIdx.x * 16) = words4{w[0], w[1], w[2], w[3]};
     }
     issue(stage0, 0);
@@ -189,7 +193,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     // The counts are those of the loads issued after it: STAGES - 2 steps, and from the second step of a group on its successor's scales
     // until the steps issued with them are read.
     constexpr int kFlying = kLoads * (STAGES - 2);
-    if (p.steps >= 4) {
+    if (steps >= 4) {
         for (int f = 0; f < whole; ++f) {
             const int k = f * kGroupSteps;
             wait_and_meet<kFlying>();
@@ -210,10 +214,10 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
             }
         }
     }
-    const int done = p.steps >= 4 ? whole * kGroupSteps : 0, left = p.steps - done;
+    const int done = steps >= 4 ? whole * kGroupSteps : 0, left = steps - done;
     wait_and_meet<0>();
     if (left > 0) {
-        read_scales(p.steps >= 4 ? first_of(whole) : 4 - p.steps);
+        read_scales(steps >= 4 ? first_of(whole) : 4 - steps);
         if constexpr (STAGES > 3) {
             contract(stage0, k0);
             if (left > 1) contract(stage1, k1);
@@ -395,7 +399,28 @@ __global__ __launch_bounds__(256) void zero_kernel(T* out, int64_t rows, int64_t
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < rows * cols; q += (int64_t)gridDim.x * 256) out[q / cols * pitch + q % cols] = (T)0;
 }
 
+// The parts of a split contraction, added in order: four results a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float* parts, int32_t n, int64_t stride, T* out, int64_t rows, int64_t cols, int64_t pitch, int64_t per_row) {
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / per_row, col = (u - row * per_row) * 4;
+    if (row >= rows) return;
+    float sum[4], x[8][4];
+    const float* at = parts + row * cols + col;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < n) load_vec<4>(at + q * stride, cols - col, x[q]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        sum[c] = x[0][c];
+#pragma unroll
+        for (int q = 1; q < 8; ++q) if (q < n) sum[c] += x[q][c];
+    }
+    store_vec<4>(out + row * pitch + col, cols - col, sum);
+}
+
 // ---- host --------------------------------------------------------------------------------------------------------------
+constexpr int64_t kFewRows = 64;
+
 template <int FA, int TM, int TN, int WAVES, typename T>
 void few_rows(const Product& p, hipStream_t s) {
     const dim3 grid((unsigned)((p.b.rows + TN * 16 - 1) / (TN * 16)), (unsigned)((p.a.rows + TM * 16 - 1) / (TM * 16)));
@@ -415,21 +440,53 @@ void tiles(Product p, hipStream_t s) {
     p.tiles_m = (int32_t)((p.a.rows + BM - 1) / BM);
     p.tiles_n = (int32_t)((p.b.rows + BN - 1) / BN);
     const int64_t all = (int64_t)p.tiles_m * p.tiles_n;
-    hipLaunchKernelGGL((tile_kernel<FA, BM, BN, WM, WN, STAGES, T>), dim3((unsigned)((all + kXcds - 1) / kXcds * kXcds)), dim3(64 * WM * WN), 0, s, p);
+    const unsigned parts = (unsigned)((p.steps + p.part_steps - 1) / p.part_steps);
+    hipLaunchKernelGGL((tile_kernel<FA, BM, BN, WM, WN, STAGES, T>), dim3((unsigned)((all + kXcds - 1) / kXcds * kXcds), parts), dim3(64 * WM * WN), 0, s, p);
+}
+
+// Parts that a contraction is split into where tiles of 128 are too few to keep the CUs busy: the one with the least time, 0.40 us a step of a
+// tile (0.52 in 8 bits) and what the join costs, its launch and the parts written and read.  (128 x 8192 x 8192: 26.7 us whole and 19.7 in four
+// parts in 4 bits, 37 and 22.9 in 8.)
+int parts_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
+    const int64_t tiles = (M + 127) / 128 * ((N + 127) / 128);
+    if (M <= kFewRows || tiles > 128) return 1;
+    const double step = a_fmt == SSGD_MX_FP4 ? 0.40 : 0.52, join = 4.0, results = (double)M * (double)N * 8.0 / 5.0e6;
+    int best = 1;
+    double least = step * (double)steps;
+    for (int n = 2; n <= 8 && n * tiles <= 512 && n * 4 <= steps; ++n) {
+        const double t = step * (double)((steps + n - 1) / n) + join + results * n;
+        if (t < least) { least = t; best = n; }
+    }
+    return best;
+}
+int64_t parts_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
+    const int n = parts_of(a_fmt, M, N, mx_padded(K) / kMxPad);
+    return n > 1 ? n * M * N * 4 : 0;
 }
 
 template <int FA, typename T>
-void launch(const Product& p, hipStream_t s) {
+void launch(Product p, void* work, hipStream_t s) {
     // 16 rows of B to a workgroup, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as often (61 x 6144 x 5000
     // in 4 bits: 10.9 us against 14.7; 64 x 2048 x 4096: 10.3 against 8.6).
     const bool pairs = p.b.rows >= 5120;
     if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
     else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
-    else if (p.a.rows <= 64) { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
+    else if (p.a.rows <= kFewRows) { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
     // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 279 us in 4 bits against 403 with tiles of 128; 1000 x 8192 x 8192, 128
     // tiles: 57 against 53).  Stages: as many as LDS holds, for tiles of 128 of two workgroups per CU (2100 x 1500 x 4001 in 8 bits: 30 us with
     // two, 22 with three; 4001 x 2100 x 1500 27 and 23, with four and one workgroup per CU 28).
-    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
+    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) {
+        constexpr int kStages = FA == SSGD_MX_FP4 ? 4 : 3;
+        const int parts = parts_of(FA, p.a.rows, p.b.rows, p.steps);
+        if (parts == 1) { tiles<FA, 128, 128, 2, 2, kStages, T>(p, s); return; }
+        Product q = p;
+        q.out = work; q.pitch = p.b.rows; q.part_stride = p.a.rows * p.b.rows;
+        q.part_steps = (p.steps + parts - 1) / parts;
+        tiles<FA, 128, 128, 2, 2, kStages, float>(q, s);
+        const int64_t per_row = (p.b.rows + 3) / 4, groups = p.a.rows * per_row;
+        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(work), (p.steps + q.part_steps - 1) / q.part_steps,
+                           q.part_stride, static_cast<T*>(p.out), p.a.rows, p.b.rows, p.pitch, per_row);
+    }
     else if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
     else tiles<FA, 256, 256, 4, 2, 3, T>(p, s);
 }
@@ -443,7 +500,7 @@ Product product_of(const void* a_values, const void* a_scales, int32_t a_fmt, in
     const int64_t scale_bytes = mx_padded(K) / kMxBlock;
     p.a = {static_cast<const uint8_t*>(a_values), static_cast<const uint8_t*>(a_scales), M, mx_row_bytes(a_fmt, K), scale_bytes};
     p.b = {static_cast<const uint8_t*>(b_values), static_cast<const uint8_t*>(b_scales), N, mx_row_bytes(SSGD_MX_FP4, K), scale_bytes};
-    p.out = out; p.pitch = out_pitch; p.steps = (int32_t)(mx_padded(K) / kMxPad);
+    p.out = out; p.pitch = out_pitch; p.steps = p.part_steps = (int32_t)(mx_padded(K) / kMxPad);
     return p;
 }
 
@@ -454,9 +511,9 @@ ssgd_status zeros(int64_t M, int64_t N, void* out, int32_t out_dtype, int64_t ou
     return op_hip(hipGetLastError(), "mx product");
 }
 
-ssgd_status product(const Product& p, int32_t a_fmt, int32_t out_dtype, hipStream_t stream) {
-    if (a_fmt == SSGD_MX_FP4) { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP4, float>(p, stream); else launch<SSGD_MX_FP4, bf16_t>(p, stream); }
-    else { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP8, float>(p, stream); else launch<SSGD_MX_FP8, bf16_t>(p, stream); }
+ssgd_status product(const Product& p, int32_t a_fmt, int32_t out_dtype, void* work, hipStream_t stream) {
+    if (a_fmt == SSGD_MX_FP4) { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP4, float>(p, work, stream); else launch<SSGD_MX_FP4, bf16_t>(p, work, stream); }
+    else { if (out_dtype == SSGD_F32) launch<SSGD_MX_FP8, float>(p, work, stream); else launch<SSGD_MX_FP8, bf16_t>(p, work, stream); }
     return op_hip(hipGetLastError(), "mx product");
 }
 
@@ -470,9 +527,13 @@ void one_row_of(const Product& p, const Rows& x, int32_t a_fmt, int32_t out_dtyp
     else { if (out_dtype == SSGD_F32) one_row<SSGD_MX_FP8, X, float>(p, x, stream); else one_row<SSGD_MX_FP8, X, bf16_t>(p, x, stream); }
 }
 
+bool sizes_ok(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
+    return format_ok(a_fmt) && M >= 0 && N >= 0 && K >= 0 && M < kMostRows && N < kMostRows && K <= kMostCols;
+}
+
 const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, const void* out, int32_t out_dtype, int64_t out_pitch) {
     if (!format_ok(a_fmt) || !dtype_ok(out_dtype)) return "mx product: a format and an output type of the enumerations";
-    if (M < 0 || N < 0 || K < 0 || M >= kMostRows || N >= kMostRows || K > kMostCols || out_pitch < N) return "mx product: M and N from zero to 2^31, K to 2^24 - 128, pitch >= N";
+    if (!sizes_ok(a_fmt, M, N, K) || out_pitch < N) return "mx product: M and N from zero to 2^31, K to 2^24 - 128, pitch >= N";
     if (M == 0 || N == 0) return nullptr;
     if ((M + 127) / 128 * ((N + 127) / 128) > kMostBlocks) return "mx product: too many results";
     if (K > 0 && (!b_values || !b_scales || !aligned(b_values, 16) || !aligned(b_scales, 16))) return "mx product: values and scales are 16-byte aligned arrays";
@@ -485,21 +546,24 @@ const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* 
 #pragma GCC visibility push(default)
 extern "C" {
 
+int64_t ssgd_mx_matmul_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) { return sizes_ok(a_fmt, M, N, K) ? parts_bytes(a_fmt, M, N, K) : -1; }
+
 ssgd_status ssgd_mx_matmul(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K,
-                           void* out, int32_t out_dtype, int64_t out_pitch, void* hip_stream) {
+                           void* out, int32_t out_dtype, int64_t out_pitch, void* work, void* hip_stream) {
     return op_entry([&]() -> ssgd_status {
         if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch)) return op_fail(SSGD_EINVAL, why);
         if (M == 0 || N == 0) return SSGD_OK;
         if (K > 0 && (!a_values || !a_scales || !aligned(a_values, 16) || !aligned(a_scales, 16))) return op_fail(SSGD_EINVAL, "mx product: values and scales are 16-byte aligned arrays");
+        if ((!work || !aligned(work, 16)) && parts_bytes(a_fmt, M, N, K) > 0) return op_fail(SSGD_EINVAL, "mx product: a 16-byte aligned work area");
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (K == 0) return zeros(M, N, out, out_dtype, out_pitch, stream);
-        return product(product_of(a_values, a_scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, stream);
+        return product(product_of(a_values, a_scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, work, stream);
     });
 }
 
-int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t K) {
-    if (!format_ok(a_fmt) || M < 0 || K < 0 || M >= kMostRows || K > kMostCols) return -1;
-    return quantises_itself(a_fmt, M, K) ? 0 : M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock);
+int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
+    if (!sizes_ok(a_fmt, M, N, K)) return -1;
+    return quantises_itself(a_fmt, M, K) ? 0 : parts_bytes(a_fmt, M, N, K) + (M * (mx_row_bytes(a_fmt, K) + mx_padded(K) / kMxBlock) + 15) / 16 * 16;
 }
 
 ssgd_status ssgd_mx_linear(const void* x, int32_t dtype, int64_t pitch, int64_t M, int32_t a_fmt, const void* b_values, const void* b_scales, int64_t N, int64_t K,
@@ -518,10 +582,12 @@ ssgd_status ssgd_mx_linear(const void* x, int32_t dtype, int64_t pitch, int64_t 
             return op_hip(hipGetLastError(), "mx linear");
         }
         if (!work || !aligned(work, 16)) return op_fail(SSGD_EINVAL, "mx linear: a 16-byte aligned work area");
-        uint8_t *values = static_cast<uint8_t*>(work), *scales = values + M * mx_row_bytes(a_fmt, K);
+        // values and scales in front (whole multiples of 16 bytes in all), then the parts
+        const int64_t value_bytes = M * mx_row_bytes(a_fmt, K), all = (value_bytes + M * (mx_padded(K) / kMxBlock) + 15) / 16 * 16;
+        uint8_t *values = static_cast<uint8_t*>(work), *scales = values + value_bytes;
         const ssgd_status st = ssgd_mx_quantize(x, dtype, M, K, pitch, a_fmt, values, scales, 0, nullptr, nullptr, hip_stream);
         if (st != SSGD_OK) return st;
-        return product(product_of(values, scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, stream);
+        return product(product_of(values, scales, a_fmt, M, b_values, b_scales, N, K, out, out_pitch), a_fmt, out_dtype, values + all, stream);
     });
 }
 

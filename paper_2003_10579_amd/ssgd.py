@@ -28,7 +28,7 @@ EXPORTS = [
     "ssgd_runtime_mc", "ssgd_debug_delays", "ssgd_debug_batch", "ssgd_stream_read_rate", "ssgd_last_error",
     "ssgd_last_kernel_ms", "ssgd_adamw_state_elements", "ssgd_adamw_create", "ssgd_adamw_step", "ssgd_adamw_destroy",
     "ssgd_mx_row_bytes", "ssgd_mx_quantize", "ssgd_mx_dequantize",
-    "ssgd_mx_matmul", "ssgd_mx_linear_work_bytes", "ssgd_mx_linear",
+    "ssgd_mx_matmul_work_bytes", "ssgd_mx_matmul", "ssgd_mx_linear_work_bytes", "ssgd_mx_linear",
     "ssgd_rmsnorm", "ssgd_rmsnorm_work_floats", "ssgd_rmsnorm_backward",
     "ssgd_destroy",
 ]
@@ -125,9 +125,11 @@ def lib():
         L.ssgd_mx_row_bytes.argtypes = [i32, i64]
         L.ssgd_mx_quantize.argtypes = [ptr, i32, i64, i64, i64, i32, ptr, ptr, i32, ptr, ptr, ptr]
         L.ssgd_mx_dequantize.argtypes = [ptr, ptr, i32, i64, i64, ptr, i32, i64, ptr]
-        L.ssgd_mx_matmul.argtypes = [ptr, ptr, i32, i64, ptr, ptr, i64, i64, ptr, i32, i64, ptr]
+        L.ssgd_mx_matmul_work_bytes.restype = i64
+        L.ssgd_mx_matmul_work_bytes.argtypes = [i32, i64, i64, i64]
+        L.ssgd_mx_matmul.argtypes = [ptr, ptr, i32, i64, ptr, ptr, i64, i64, ptr, i32, i64, ptr, ptr]
         L.ssgd_mx_linear_work_bytes.restype = i64
-        L.ssgd_mx_linear_work_bytes.argtypes = [i32, i64, i64]
+        L.ssgd_mx_linear_work_bytes.argtypes = [i32, i64, i64, i64]
         L.ssgd_mx_linear.argtypes = [ptr, i32, i64, i64, i32, ptr, ptr, i64, i64, ptr, i32, i64, ptr, ptr]
         L.ssgd_rmsnorm.argtypes = [ptr, i64, ptr, i64, ptr, i32, i32, i64, i64, C.c_double, ptr, i64, ptr, i64, ptr, ptr, ptr, ptr]
         L.ssgd_rmsnorm_work_floats.restype = i64
@@ -527,9 +529,13 @@ def mx_dequantize(q, dtype=None):
         _refuse("mx_dequantize: an MxTensor is wanted")
     rows, cols = q.shape
     kind = F32 if dtype is None else _dtype(dtype)
-    out = _torch.empty((rows, cols), dtype=dtype, device=q.device) if dtype else _torch.empty((rows, cols), dtype=_torch.float32, device=q.device)
+    out = _torch.empty(rows, cols, dtype=dtype or _torch.float32, device=q.device)
     _call(_lib.ssgd_mx_dequantize, q.device, *q._at, _FORMATS[q.format], rows, cols, out.data_ptr(), kind, cols)
     return out
+
+
+def _work(bytes, device):
+    return _torch.empty(bytes, dtype=_torch.uint8, device=device) if bytes > 0 else None
 
 
 def mx_matmul(a, b, dtype=None):
@@ -539,8 +545,10 @@ def mx_matmul(a, b, dtype=None):
         _refuse("mx_matmul: an MxTensor and an 'fp4' MxTensor of as many columns on its device are wanted")
     (M, K), N, dev = a.shape, b.shape[0], a.device
     kind = BF16 if dtype is None else _dtype(dtype)
-    out = _torch.empty((M, N), dtype=dtype or _torch.bfloat16, device=dev)
-    _call(_lib.ssgd_mx_matmul, dev, *a._at, _FORMATS[a.format], M, *b._at, N, K, out.data_ptr(), kind, N)
+    out = _torch.empty(M, N, dtype=dtype or _torch.bfloat16, device=dev)
+    f = _FORMATS[a.format]
+    work = _work(_lib.ssgd_mx_matmul_work_bytes(f, M, N, K), dev)
+    _call(_lib.ssgd_mx_matmul, dev, *a._at, f, M, *b._at, N, K, out.data_ptr(), kind, N, None if work is None else work.data_ptr())
     return out
 
 
@@ -554,9 +562,8 @@ def mx_linear(x, w, format="fp8", dtype=None):
         _refuse("mx_linear: w is an 'fp4' MxTensor with x's columns, on its device")
     N, f = w.shape[0], _FORMATS[format]
     out_kind = kind if dtype is None else _dtype(dtype)
-    out = _torch.empty((M, N), dtype=dtype or x.dtype, device=dev)
-    bytes = _lib.ssgd_mx_linear_work_bytes(f, M, K)
-    work = _torch.empty(bytes, dtype=_torch.uint8, device=dev) if bytes > 0 else None
+    out = _torch.empty(M, N, dtype=dtype or x.dtype, device=dev)
+    work = _work(_lib.ssgd_mx_linear_work_bytes(f, M, N, K), dev)
     _call(_lib.ssgd_mx_linear, dev, x.data_ptr(), kind, pitch, M, f, *w._at, N, K, out.data_ptr(), out_kind, N, None if work is None else work.data_ptr())
     return out
 
@@ -587,11 +594,11 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, output=None):
     if residual is None:
         total, total_at = x, None
     else:
-        total = _torch.empty((rows, d), dtype=x.dtype, device=dev)
+        total = _torch.empty(rows, d, dtype=x.dtype, device=dev)
         total_at = total.data_ptr()
     rstd = _torch.empty(rows, dtype=_torch.float32, device=dev)
     if output is None:
-        y = _torch.empty((rows, d), dtype=x.dtype, device=dev)
+        y = _torch.empty(rows, d, dtype=x.dtype, device=dev)
         to = (y.data_ptr(), d, None, None)
     else:
         y = MxTensor.empty(rows, d, "fp8", dev)
@@ -609,7 +616,7 @@ def rmsnorm_backward(dy, s, weight, rstd, dsum=None):
     if not (rstd.dtype == _torch.float32 and rstd.shape == (rows,) and rstd.is_contiguous() and rstd.device == dev):
         _refuse("rmsnorm_backward: one float32 rstd per row is wanted")
     more, more_pitch = _beside(dsum, dy, "rmsnorm_backward")
-    dx = _torch.empty((rows, d), dtype=dy.dtype, device=dev)
+    dx = _torch.empty(rows, d, dtype=dy.dtype, device=dev)
     dw = _torch.empty(d, dtype=_torch.float32, device=dev)
     floats = _lib.ssgd_rmsnorm_work_floats(rows, d)
     if floats < 0:

@@ -47,7 +47,7 @@ def _close(got, a, b, fmt, dtype):
 # few rows (one, two and four groups of 16, partial ones), tiles of 128 and, from 200 tiles of 256 on, of 256; contractions from one column to
 # many steps of 128, each remainder of the stages; rows of B that are no multiple of anything
 SHAPES = [(1, 1, 1), (1, 3, 5), (2, 50, 900), (3, 50, 900), (2, 40, 17000), (1, 5200, 700), (16, 5130, 600), (20, 5121, 513), (50, 5150, 1300), (1, 16, 128), (1, 17, 4096), (1, 300, 3072), (2, 512, 3071), (15, 33, 129), (16, 100, 640), (17, 100, 512), (32, 40, 2200), (33, 70, 1000),
-          (61, 130, 5000), (64, 64, 8192), (65, 1, 100), (65, 127, 300), (100, 129, 129), (128, 128, 128), (129, 257, 256), (130, 130, 384), (300, 200, 512),
+          (61, 130, 5000), (64, 64, 8192), (65, 1, 100), (65, 127, 300), (100, 129, 129), (65, 70, 5000), (128, 300, 9000), (200, 129, 3200), (256, 1000, 4225), (128, 128, 128), (129, 257, 256), (130, 130, 384), (300, 200, 512),
           (257, 513, 640), (512, 384, 1100), (3500, 3700, 127), (3585, 3600, 300), (3700, 3500, 700), (4000, 3500, 513)]
 
 
@@ -132,13 +132,14 @@ def test_strided_and_misaligned_outputs_and_nothing_beside_them(env):
     torch, ssgd = env
     L = ssgd.lib()
     stream = torch.cuda.current_stream().cuda_stream
-    for M, N, K in ((1, 37, 200), (50, 130, 700), (140, 135, 300), (3500, 3601, 130)):
+    for M, N, K in ((1, 37, 200), (50, 130, 700), (140, 135, 300), (140, 135, 5000), (3500, 3601, 130)):
         a, b = ssgd.mx_quantize(_matrix(torch, M, K, 1).cuda(), "fp8"), ssgd.mx_quantize(_matrix(torch, N, K, 2).cuda(), "fp4")
         want = ssgd.mx_matmul(a, b, torch.float32)
+        work = torch.full((L.ssgd_mx_matmul_work_bytes(1, M, N, K) // 4 + 8,), float("nan"), device="cuda")
         for pad, offset in ((0, 0), (8, 4), (5, 1)):
             room = torch.full((M + 2, N + pad), 7.0, device="cuda")
             assert L.ssgd_mx_matmul(a.values.data_ptr(), a.scales.data_ptr(), 1, M, b.values.data_ptr(), b.scales.data_ptr(), N, K,
-                                    room[1:].data_ptr() + 4 * offset, 0, N + pad, stream) == 0
+                                    room[1:].data_ptr() + 4 * offset, 0, N + pad, work.data_ptr(), stream) == 0
             flat = room.reshape(-1)
             at = N + pad + offset
             body = flat[at:at + (M - 1) * (N + pad) + N]
@@ -161,8 +162,8 @@ def test_empty_products(env):
 
 def test_another_stream_and_a_replayed_graph_give_the_same(env):
     torch, ssgd = env
-    x, w = _matrix(torch, 90, 900, 1).cuda().bfloat16(), ssgd.mx_quantize(_matrix(torch, 333, 900, 2).cuda(), "fp4")
-    for rows in (1, 90):
+    x, w = _matrix(torch, 90, 9000, 1).cuda().bfloat16(), ssgd.mx_quantize(_matrix(torch, 333, 9000, 2).cuda(), "fp4")
+    for rows in (1, 90):          # (90 rows: quantised, split and joined)
         want = ssgd.mx_linear(x[:rows], w)
         torch.cuda.synchronize()
         s = torch.cuda.Stream()

@@ -87,7 +87,7 @@ def test_mx_dequantize_refuses(L, bad):
                                  dict(K=1 << 24), dict(M=(1 << 31) - 1, N=(1 << 31) - 1, pitch=1 << 31)])
 def test_mx_products_refuse(L, bad):
     g = lambda k, d: bad.get(k, d)  # noqa: E731
-    _refused(L, L.ssgd_mx_matmul(g("a", A), g("sa", A), g("fmt", 0), g("M", 10), g("b", A), g("sb", A), g("N", 20), g("K", 100), g("out", A), g("dtype", 0), g("pitch", 20), None), b"mx")
+    _refused(L, L.ssgd_mx_matmul(g("a", A), g("sa", A), g("fmt", 0), g("M", 10), g("b", A), g("sb", A), g("N", 20), g("K", 100), g("out", A), g("dtype", 0), g("pitch", 20), A, None), b"mx")
     if not {"a", "sa"} & set(bad):
         for rows in (1, 10):
             M = g("M", rows)
@@ -98,15 +98,23 @@ def test_mx_products_refuse(L, bad):
 @pytest.mark.parametrize("rows", [1, 10])
 def test_mx_linear_refuses(L, bad, rows):
     if rows == 1 and "work" in bad:
-        assert L.ssgd_mx_linear_work_bytes(1, 1, 1000) == 0            # one row needs none
+        assert L.ssgd_mx_linear_work_bytes(1, 1, 20, 1000) == 0            # one row needs none
         return
     g = lambda k, d: bad.get(k, d)  # noqa: E731
     _refused(L, L.ssgd_mx_linear(g("x", A), g("kind", 0), g("pitch", 1000), rows, 1, A, A, 20, 1000, A, 0, 20, g("work", A), None), b"mx")
 
 
-def test_mx_linear_work_bytes(L):
-    assert L.ssgd_mx_linear_work_bytes(1, 10, 1000) == 10 * (1024 + 32) and L.ssgd_mx_linear_work_bytes(0, 10, 1000) == 10 * (512 + 32)
-    assert L.ssgd_mx_linear_work_bytes(2, 10, 1000) == -1 and L.ssgd_mx_linear_work_bytes(0, -1, 1000) == -1 and L.ssgd_mx_linear_work_bytes(0, 1, 1 << 24) == -1
+def test_mx_work_bytes(L):
+    linear, matmul = L.ssgd_mx_linear_work_bytes, L.ssgd_mx_matmul_work_bytes
+    assert linear(1, 10, 50, 1000) == 10 * (1024 + 32) and linear(0, 9, 50, 1000) == 9 * (512 + 32)
+    # a long contraction with few results is split, one with many is not
+    assert matmul(0, 128, 8192, 8192) >= 2 * 128 * 8192 * 4 and matmul(0, 128, 8192, 8192) % (128 * 8192 * 4) == 0
+    assert linear(0, 128, 8192, 8192) == matmul(0, 128, 8192, 8192) + 128 * (4096 + 256)
+    assert matmul(0, 128, 8192, 128) == 0 and matmul(0, 8192, 8192, 8192) == 0 and matmul(1, 64, 8192, 8192) == 0 and matmul(1, 300, 300, 0) == 0
+    for f in (linear, matmul):
+        assert f(2, 10, 50, 1000) == -1 and f(0, -1, 50, 10) == -1 and f(0, 1, -1, 10) == -1 and f(0, 1, 50, 1 << 24) == -1
+    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 8192, 8192, A, 0, 8192, None, None), b"work")
+    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 8192, 8192, A, 0, 8192, A + 8, None), b"work")
 
 
 @pytest.mark.parametrize("bad", [
