@@ -371,14 +371,11 @@ __global__ __launch_bounds__(64 * WAVES) void one_row_kernel(Product p, Rows x) 
     const int per_row = p.steps * 16;                  // groups of eight columns
     for (int u = threadIdx.x; u < many * per_row; u += 64 * WAVES) {
         const int row = u / per_row, col = (u - row * per_row) * 8;
-        float v[8];
-        load_vec<8>(static_cast<const X*>(x.x) + row * x.pitch + col, x.cols - col, v);
-        uint32_t most = 0;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(v[q]));
-        const uint32_t byte = mx_scale_byte<FA>(max_of_4(most));
-        if constexpr (FA == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(rows + row * row_bytes + col / 2) = mx_pack_fp4(v, byte);
-        else *reinterpret_cast<words2*>(rows + row * row_bytes + col) = mx_pack_fp8(v, byte);
+        Eight<X> v;
+        v.load(static_cast<const X*>(x.x) + row * x.pitch + col, x.cols - col);
+        const uint32_t byte = mx_scale_byte<FA>(max_of_4(v.largest()));
+        if constexpr (FA == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(rows + row * row_bytes + col / 2) = mx_pack_fp4(v.values(), byte);
+        else *reinterpret_cast<words2*>(rows + row * row_bytes + col) = mx_pack_fp8(v.values(), byte);
         if ((threadIdx.x & 3) == 0) scales[row * scale_bytes + col / kMxBlock] = (uint8_t)byte;
     }
     __syncthreads();

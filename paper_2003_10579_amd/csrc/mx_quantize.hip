@@ -18,15 +18,12 @@ struct Source { const void* x; int64_t rows, cols, pitch; };
 struct Target { uint8_t *values, *scales; int64_t row_bytes, scale_bytes; };   // values == nullptr: not wanted
 
 // Eight columns of a row (zeros where there are none) -> values and, from the first of four lanes, the scale.
-template <int FMT>
-__device__ __forceinline__ void store_block(const Target& t, int64_t row, int64_t col, const float (&x)[8]) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-    const uint32_t byte = mx_scale_byte<FMT>(max_of_4(most));
+template <int FMT, typename T>
+__device__ __forceinline__ void store_block(const Target& t, int64_t row, int64_t col, const Eight<T>& x) {
+    const uint32_t byte = mx_scale_byte<FMT>(max_of_4(x.largest()));
     uint8_t* to = t.values + row * t.row_bytes;
-    if constexpr (FMT == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(to + col / 2) = mx_pack_fp4(x, byte);
-    else *reinterpret_cast<words2*>(to + col) = mx_pack_fp8(x, byte);
+    if constexpr (FMT == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(to + col / 2) = mx_pack_fp4(x.values(), byte);
+    else *reinterpret_cast<words2*>(to + col) = mx_pack_fp8(x.values(), byte);
     if ((threadIdx.x & 3) == 0) t.scales[row * t.scale_bytes + col / kMxBlock] = (uint8_t)byte;
 }
 
@@ -36,57 +33,65 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Source s, Target t, int6
     const int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (g >= groups) return;                 // (groups is a multiple of 16: whole blocks)
     const int64_t row = g / groups_per_row, col = (g - row * groups_per_row) * 8;
-    float x[8];
-    load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, s.cols - col, x);
+    Eight<T> x;
+    x.load(static_cast<const T*>(s.x) + row * s.pitch + col, s.cols - col);
     store_block<FMT>(t, row, col, x);
 }
 
 // A tile of 128 x 128.  The rows of a column's block begin 16 columns further on than those of the block before, so that four lanes on
 // one column and sixteen on the next ones meet in no bank.
 __device__ __forceinline__ int place(int row, int col) { return row * kTile + (row >> 5) * 16 + col; }
-__device__ __forceinline__ float read_tile(const float* t) { return *t; }
-__device__ __forceinline__ float read_tile(const bf16_t* t) { return bf16_to_f32(*t); }
+__device__ __forceinline__ void put(float* t, const Eight<float>& x) {
+    *reinterpret_cast<f32x4*>(t) = f32x4{x.x[0], x.x[1], x.x[2], x.x[3]};
+    *reinterpret_cast<f32x4*>(t + 4) = f32x4{x.x[4], x.x[5], x.x[6], x.x[7]};
+}
+__device__ __forceinline__ void put(bf16_t* t, const Eight<bf16_t>& x) { *reinterpret_cast<words4*>(t) = x.w; }
+// Eight rows of a column.
+__device__ __forceinline__ void take(const float* t, Eight<float>& x) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x.x[q] = t[q * kTile];
+}
+__device__ __forceinline__ void take(const bf16_t* t, Eight<bf16_t>& x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = t[2 * q * kTile] | (uint32_t)t[(2 * q + 1) * kTile] << 16;
+    x.w = words4{w[0], w[1], w[2], w[3]};
+}
 
 template <typename T, int ROWS, int COLS>       // formats; ROWS < 0: columns alone
 __global__ __launch_bounds__(kTileThreads) void tile_kernel(Source s, Target t, Target tt, int64_t tiles_across) {
     __shared__ __attribute__((aligned(16))) T tile[kTile * kTile + 3 * 16];
     const int64_t r0 = (int64_t)(blockIdx.x / tiles_across) * kTile, c0 = (int64_t)(blockIdx.x % tiles_across) * kTile;
     const int lane_col = (threadIdx.x & 15) * 8;
-    float x[kTile / 32][8];
+    Eight<T> x[kTile / 32];
 #pragma unroll
     for (int q = 0; q < kTile / 32; ++q) {
         const int64_t row = r0 + q * 32 + (threadIdx.x >> 4), col = c0 + lane_col;
-        load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0, x[q]);
+        x[q].load(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0);
     }
 #pragma unroll
     for (int q = 0; q < kTile / 32; ++q) {
         const int r = q * 32 + (threadIdx.x >> 4);
-        store_vec<8>(&tile[place(r, lane_col)], 8, x[q]);
+        put(&tile[place(r, lane_col)], x[q]);
         if constexpr (ROWS >= 0) { if (r0 + r < s.rows) store_block<ROWS>(t, r0 + r, c0 + lane_col, x[q]); }
     }
     __syncthreads();
-    const int block = threadIdx.x & 3;
-    {
-        const int c = threadIdx.x >> 2;
-        const int64_t col = c0 + c;
-        if (col >= s.cols) return;
-        uint32_t most = 0;
+    const int block = threadIdx.x & 3, c = threadIdx.x >> 2;
+    const int64_t col = c0 + c;
+    if (col >= s.cols) return;
+    uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            x[i >> 3][i & 7] = read_tile(&tile[place(block * 32 + i, c)]);
-            most = umax(most, magnitude(x[i >> 3][i & 7]));
-        }
-        const uint32_t byte = mx_scale_byte<COLS>(most);
-        uint8_t* to = tt.values + col * tt.row_bytes + (r0 + block * 32) * (COLS == SSGD_MX_FP4 ? 1 : 2) / 2;
-        if constexpr (COLS == SSGD_MX_FP4) {
-            *reinterpret_cast<words4*>(to) = words4{mx_pack_fp4(x[0], byte), mx_pack_fp4(x[1], byte), mx_pack_fp4(x[2], byte), mx_pack_fp4(x[3], byte)};
-        } else {
-            const words2 a = mx_pack_fp8(x[0], byte), b = mx_pack_fp8(x[1], byte), c2 = mx_pack_fp8(x[2], byte), d = mx_pack_fp8(x[3], byte);
-            *reinterpret_cast<words4*>(to) = words4{a.x, a.y, b.x, b.y};
-            *reinterpret_cast<words4*>(to + 16) = words4{c2.x, c2.y, d.x, d.y};
-        }
-        tt.scales[col * tt.scale_bytes + r0 / kMxBlock + block] = (uint8_t)byte;
+    for (int q = 0; q < 4; ++q) { take(&tile[place(block * 32 + q * 8, c)], x[q]); most = umax(most, x[q].largest()); }
+    const uint32_t byte = mx_scale_byte<COLS>(most);
+    uint8_t* to = tt.values + col * tt.row_bytes + (r0 + block * 32) * (COLS == SSGD_MX_FP4 ? 1 : 2) / 2;
+    if constexpr (COLS == SSGD_MX_FP4) {
+        *reinterpret_cast<words4*>(to) = words4{mx_pack_fp4(x[0].values(), byte), mx_pack_fp4(x[1].values(), byte), mx_pack_fp4(x[2].values(), byte), mx_pack_fp4(x[3].values(), byte)};
+    } else {
+        const words2 a = mx_pack_fp8(x[0].values(), byte), b = mx_pack_fp8(x[1].values(), byte), d = mx_pack_fp8(x[2].values(), byte), e = mx_pack_fp8(x[3].values(), byte);
+        *reinterpret_cast<words4*>(to) = words4{a.x, a.y, b.x, b.y};
+        *reinterpret_cast<words4*>(to + 16) = words4{d.x, d.y, e.x, e.y};
     }
+    tt.scales[col * tt.scale_bytes + r0 / kMxBlock + block] = (uint8_t)byte;
 }
 
 // Eight columns of a row from their values and scale.

@@ -147,30 +147,88 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest) {
     const uint32_t e = largest >> 23, top = FMT == SSGD_MX_FP4 ? 2u : 8u;
     return e == 255u ? 255u : (e > top ? e - top : 0u);
 }
-__device__ __forceinline__ float mx_inverse_scale(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }   // byte <= 252
-// Eight values at a scale -> 4 (E2M1, low nibble first) or 8 bytes, nearest, ties to even, saturating.
+// Eight values at a scale -> 4 (E2M1, low nibble first) or 8 bytes, nearest, ties to even, saturating.  The conversions divide by a scale
+// themselves, whose exponent field is the byte; past E4M3's largest value they give NaN, so those values are cut off before: at 448 times the
+// scale, 1.75 x 2^(byte + 8 - 127), which bfloat16 holds as well.  (The byte is 246 at most in 8 bits, and 252 in 4.)
+typedef short shorts2 __attribute__((ext_vector_type(2)));
+typedef uint16_t half2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float mx_scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+__device__ __forceinline__ uint32_t mx_limit(uint32_t byte) { return ((byte + 8u) << 23) | 0x600000u; }
 __device__ __forceinline__ uint32_t mx_pack_fp4(const float (&x)[8], uint32_t byte) {
-    if (byte == 255u) return 0u;
-    const float inv = mx_inverse_scale(byte);
+    const float s = mx_scale_of(byte);
     uint32_t r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0] * inv, x[1] * inv, 1.0f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2] * inv, x[3] * inv, 1.0f, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4] * inv, x[5] * inv, 1.0f, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6] * inv, x[7] * inv, 1.0f, 3);
-    return r;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0], x[1], s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2], x[3], s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4], x[5], s, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6], x[7], s, 3);
+    return byte == 255u ? 0u : r;
 }
-// (the conversion gives NaN past the largest value, so the values are cut off before it)
-__device__ __forceinline__ float clamp448(float x) { return __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f); }
 __device__ __forceinline__ words2 mx_pack_fp8(const float (&x)[8], uint32_t byte) {
-    if (byte == 255u) return words2{0u, 0u};
-    const float inv = mx_inverse_scale(byte);
+    const float s = mx_scale_of(byte), most = __builtin_bit_cast(float, mx_limit(byte));
     float y[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) y[q] = clamp448(x[q] * inv);
-    int lo = 0, hi = 0;
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], lo, false); lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], hi, false); hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
-    return words2{(uint32_t)lo, (uint32_t)hi};
+    for (int q = 0; q < 8; ++q) y[q] = __builtin_amdgcn_fmed3f(x[q], -most, most);
+    shorts2 lo = {0, 0}, hi = {0, 0};
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[0], y[1], s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[2], y[3], s, true);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[4], y[5], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[6], y[7], s, true);
+    return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
+// The same from eight bfloat16, two to a word, as they are.
+// (A bit cast of a vector's element reads its first one: copies are taken.)
+__device__ __forceinline__ bf16x2 as_pair(uint32_t w) { return __builtin_bit_cast(bf16x2, w); }
+__device__ __forceinline__ half2 as_halves(uint32_t w) { return __builtin_bit_cast(half2, w); }
+__device__ __forceinline__ uint32_t mx_pack_fp4(const words4& w, uint32_t byte) {
+    const float s = mx_scale_of(byte);
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_pair(w.x), s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_pair(w.y), s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_pair(w.z), s, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_pair(w.w), s, 3);
+    return byte == 255u ? 0u : r;
+}
+__device__ __forceinline__ bf16x2 cut_off(uint32_t w, uint32_t limit) {       // magnitudes as whole numbers
+    const half2 m = __builtin_elementwise_min(as_halves(w & 0x7FFF7FFFu), as_halves(limit));
+    return __builtin_bit_cast(bf16x2, __builtin_bit_cast(uint32_t, m) | (w & 0x80008000u));
+}
+__device__ __forceinline__ words2 mx_pack_fp8(const words4& w, uint32_t byte) {
+    const float s = mx_scale_of(byte);
+    const uint32_t half = mx_limit(byte) >> 16, limit = half | half << 16;
+    shorts2 lo = {0, 0}, hi = {0, 0};
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, cut_off(w.x, limit), s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, cut_off(w.y, limit), s, true);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, cut_off(w.z, limit), s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, cut_off(w.w, limit), s, true);
+    return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+// Eight values in a row, in their own type, as quantisation takes them: their largest magnitude as the bits of an fp32 number.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    float x[8];
+    __device__ __forceinline__ void load(const float* p, int64_t left) { load_vec<8>(p, left, x); }
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t most = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
+        return most;
+    }
+    __device__ __forceinline__ const float (&values() const)[8] { return x; }
+};
+template <> struct Eight<bf16_t> {
+    words4 w;
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t left) {
+        if (left >= 8) { w = *reinterpret_cast<const words4_any*>(p); return; }
+        uint32_t v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (2 * q < left ? p[2 * q] : 0u) | (2 * q + 1 < left ? (uint32_t)p[2 * q + 1] << 16 : 0u);
+        w = words4{v[0], v[1], v[2], v[3]};
+    }
+    __device__ __forceinline__ uint32_t largest() const {
+        constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;
+        const half2 a = __builtin_elementwise_max(as_halves(w.x & kMagnitudes), as_halves(w.y & kMagnitudes));
+        const half2 b = __builtin_elementwise_max(as_halves(w.z & kMagnitudes), as_halves(w.w & kMagnitudes));
+        const half2 m = __builtin_elementwise_max(a, b);
+        return (uint32_t)(m.x > m.y ? m.x : m.y) << 16;
+    }
+    __device__ __forceinline__ const words4& values() const { return w; }
+};
 
 }  // namespace ssgd
