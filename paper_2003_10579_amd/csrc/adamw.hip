@@ -92,7 +92,8 @@ __device__ __forceinline__ void unpack_fp8(words2 w, float scale, float (&x)[8])
     x[4] = c.x * scale; x[5] = c.y * scale; x[6] = d.x * scale; x[7] = d.y * scale;
 }
 
-// Sum of squares of the pieces of a launch, in fp64 (fp32 squares overflow from 1.8e19 on), one number per workgroup.
+// Sum of squares of the pieces of a launch, in fp64 (fp32 squares overflow from 1.8e19 on), one number per workgroup.  Bound by memory: 268 M bf16
+// gradients 144 us, 3.7 TB/s, behind an update that left the caches full of lines to be written back.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void square_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, double* partials) {
     __shared__ double part[kThreads / 64];
@@ -131,6 +132,8 @@ __device__ __forceinline__ float clip_factor(const Rule& rule, double* part) {
     return c > 1.0f ? 1.0f : c;           // (a NaN stays)
 }
 
+// The update.  268 M parameters with bf16 gradients and copy: 1421 us with 32-bit moments (4.9 TB/s), 940 us with 8-bit ones (4.6 TB/s).  Four elements
+// a thread at a time with 32-bit moments, so that a wave's accesses are whole lines; eight with 8-bit ones, so that sixteen lanes hold a block.
 template <int BITS, typename G>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, Rule rule) {
     constexpr int V = BITS == 8 ? 8 : 4;

@@ -211,6 +211,10 @@ template <> struct Eight<float> {
         return most;
     }
     __device__ __forceinline__ const float (&values() const)[8] { return x; }
+    __device__ __forceinline__ void numbers(float (&y)[8]) const {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y[q] = x[q];
+    }
 };
 template <> struct Eight<bf16_t> {
     words4 w;
@@ -229,6 +233,11 @@ template <> struct Eight<bf16_t> {
         return (uint32_t)(m.x > m.y ? m.x : m.y) << 16;
     }
     __device__ __forceinline__ const words4& values() const { return w; }
+    __device__ __forceinline__ void numbers(float (&y)[8]) const {
+        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) { y[2 * q] = bf16_to_f32(v[q] & 0xFFFFu); y[2 * q + 1] = __builtin_bit_cast(float, v[q] & 0xFFFF0000u); }
+    }
 };
 
 }  // namespace ssgd

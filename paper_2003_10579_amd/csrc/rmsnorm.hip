@@ -4,7 +4,8 @@
 //   rstd = (mean s^2 + eps)^(-1/2),  y = (s rstd) w
 //   dx = rstd (g - xhat mean(g xhat)) + dsum,  g = dy w,  xhat = s rstd;    dw = sum over rows of dy xhat
 //
-// About 8 operations per element forward, 12 backward: bound by memory.  A row stays in the registers of 64, 256 or 1024 threads, eight
+// About 8 operations per element forward, 12 backward: bound by memory (16384 x 4096 in bf16: forward with 8-bit output 100 us, 4.7 TB/s; backward
+// 107 us with its sums over rows, 5.0 TB/s).  A row stays in the registers of 64, 256 or 1024 threads, eight
 // or sixteen columns each, between the sum of squares and the output, so it is read once; the threads go on to further rows with
 // their part of w, and backward with their part of dw, kept.  Rows of more than 16384 columns are read a second time instead.
 #include <cmath>
@@ -17,7 +18,6 @@ namespace {
 
 constexpr int kMostKept = 16384;      // columns that fit the registers of 1024 threads
 constexpr int64_t kMostColumns = int64_t(1) << 25;     // 16 to a workgroup of 1024 in the sums of dw: a launch ends at 2^32 threads
-constexpr int kTeams = 1024;          // rows at work at a time, and partial sums of dw
 
 struct Forward {
     const void *x, *residual, *w;
@@ -33,8 +33,8 @@ struct Backward {
     const void *dy, *s, *w, *dsum;
     const float* rstd;
     void* dx;
-    float* partial;          // [teams][d], nullptr: dw is not wanted
-    int64_t rows, dy_pitch, s_pitch, dsum_pitch, dx_pitch, teams;
+    float* partial;          // [groups][d], nullptr: dw is not wanted
+    int64_t rows, dy_pitch, s_pitch, dsum_pitch, dx_pitch, groups;
     int32_t d, w_bf16;
 };
 
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
     }
 }
 
-// Rows that registers do not hold: a second read, of the sum (its own threads have written it) or of x.
+// Rows that registers do not hold: a second read, of the sum (its own threads have written it) or of x (2048 x 20000 in bf16: 79 us, 3.6 TB/s).
 template <typename T, bool FP8>
 __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
     __shared__ double part[16];
@@ -164,8 +164,8 @@ template <typename T, int LANES, int NV>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Backward a) {
     constexpr int kRows = LANES == 64 ? 4 : 1;
     __shared__ double part[LANES / 64];
-    const int lane = threadIdx.x & (LANES - 1);
-    const int64_t team = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    __shared__ float dw_of[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? LANES * NV * 8 : 1];
+    const int lane = threadIdx.x & (LANES - 1), team = threadIdx.x / LANES;
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -173,15 +173,36 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[v][q] = 0.0f;
     }
-    for (int64_t row = team; row < a.rows; row += a.teams) {
-        float dy[NV][8], xhat[NV][8];
-        const float rstd = a.rstd[row];
-        float sum = 0.0f;
+    // The next row's dy and s are on their way while a row's sum is taken (16384 x 1500: 60 us instead of 74; threads of 1024 have no registers
+    // for it, 4000 x 16000: 126 us instead of 119).
+    constexpr bool kAhead = LANES < 1024;
+    Eight<T> next_dy[NV], next_s[NV];
+    float next_rstd = 0.0f;
+    auto load = [&](int64_t row) {
+        if (row >= a.rows) return;
+        next_rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int col = (v * LANES + lane) * 8;
-            load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy[v]);
-            load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, xhat[v]);
+            next_dy[v].load(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col);
+            next_s[v].load(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col);
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * kRows + team, step = a.groups * kRows;
+    if constexpr (kAhead) load(first);
+    for (int64_t row = first; row < a.rows; row += step) {
+        if constexpr (!kAhead) load(row);
+        float dy[NV][8], xhat[NV][8];
+        const float rstd = next_rstd;
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            next_dy[v].numbers(dy[v]);
+            next_s[v].numbers(xhat[v]);
+        }
+        if constexpr (kAhead) load(row + step);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 xhat[v][q] *= rstd;
@@ -196,20 +217,39 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
             if (col < a.d) store_dx<T>(a, row, col, dy[v], xhat[v], w[v], rstd, c);
         }
     }
-    if (a.partial != nullptr && team < a.teams) {
+    if (a.partial == nullptr) return;
+    if constexpr (kRows > 1) {
+        // the rows of a workgroup's waves first, in their order
+        if (team > 0) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int col = (v * LANES + lane) * 8;
-            store_vec<8>(a.partial + team * a.d + col, a.d - col, dw[v]);
+            for (int v = 0; v < NV; ++v) store_vec<8>(&dw_of[team - 1][(v * LANES + lane) * 8], 8, dw[v]);
         }
+        __syncthreads();
+        if (team > 0) return;
+#pragma unroll
+        for (int t = 0; t < kRows - 1; ++t)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float x[8];
+                load_vec<8>(&dw_of[t][(v * LANES + lane) * 8], 8, x);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) dw[v][q] += x[q];
+            }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int col = (v * LANES + lane) * 8;
+        store_vec<8>(a.partial + (int64_t)blockIdx.x * a.d + col, a.d - col, dw[v]);
     }
 }
 
+// The same backward: dy and s twice, and the workgroup's partial sum of dw read and written for every row (2048 x 20000 in bf16: 153 us, 2.1 TB/s of
+// what has to be moved).
 template <typename T>
 __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
     __shared__ double part[16];
     bool first = true;
-    for (int64_t row = blockIdx.x; row < a.rows; row += a.teams) {
+    for (int64_t row = blockIdx.x; row < a.rows; row += a.groups) {
         const float rstd = a.rstd[row];
         double sum = 0.0;
         for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
@@ -246,16 +286,17 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
     }
 }
 
-// dw of 16 columns: the 64 quarter waves of a workgroup take every 64th partial sum, eight loads in flight, and add in fp64.
-__global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int64_t teams, int32_t d, float* dw) {
+// dw of 16 columns: the 64 quarter waves of a workgroup take every 64th partial sum, eight loads in flight, and add in fp64 (768 sums of
+// 4096 columns: 8 us; with 64 columns and whole cache lines to a workgroup no faster).
+__global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int64_t groups, int32_t d, float* dw) {
     __shared__ double part[64][17];
     const int c = threadIdx.x & 15, group = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     double sum = 0.0;
     if (col < d) {
-        for (int64_t t = group; t < teams; t += 64 * 8) {
+        for (int64_t t = group; t < groups; t += 64 * 8) {
             float x[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[q] = t + 64 * q < teams ? partial[(t + 64 * q) * d + col] : 0.0f;
+            for (int q = 0; q < 8; ++q) x[q] = t + 64 * q < groups ? partial[(t + 64 * q) * d + col] : 0.0f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) sum += (double)x[q];
         }
@@ -291,16 +332,19 @@ void launch_forward(const Forward& a, hipStream_t s) {
     else hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 2>), grid, group, 0, s, a);
 }
 
-// Rows at work at a time: the partial sums of dw are written and read once more, 8 bytes a column each.
-int64_t teams_for(int64_t rows, int64_t d) {
-    const int64_t most = lanes_for(d) == 1024 ? 512 : kTeams;
-    return rows < most ? rows : most;
+// Workgroups, each with a partial sum of dw that is written and read once more: as many as are resident.  (16384 x 4096: 107 us with 768, 113 with
+// 512, 128 with 1024; 16384 x 1500: 60 with 1024, 69 with 768; 4000 x 16000: 119 with 256, 125 with 512.)
+int64_t groups_for(int64_t rows, int64_t d) {
+    const int lanes = lanes_for(d);
+    const bool two = (d > 512 && d <= 1024) || (d > 2048 && d <= 4096);      // sixteen columns a thread
+    const int64_t rows_each = lanes == 64 ? 4 : 1, most = lanes == 1024 ? 256 : (two ? 768 : 1024), groups = (rows + rows_each - 1) / rows_each;
+    return groups < most ? groups : most;
 }
 
 template <typename T>
 void launch_backward(const Backward& a, hipStream_t s) {
-    const int lanes = lanes_for(a.d), rows = lanes == 64 ? 4 : 1;
-    const dim3 grid((unsigned)((a.teams + rows - 1) / rows)), group(lanes == 64 ? 256 : lanes);
+    const int lanes = lanes_for(a.d);
+    const dim3 grid((unsigned)a.groups), group(lanes == 64 ? 256 : lanes);
     if (a.d > kMostKept) hipLaunchKernelGGL((backward_long_kernel<T>), grid, dim3(1024), 0, s, a);
     else if (a.d <= 512) hipLaunchKernelGGL((backward_kernel<T, 64, 1>), grid, group, 0, s, a);
     else if (a.d <= 1024) hipLaunchKernelGGL((backward_kernel<T, 64, 2>), grid, group, 0, s, a);
@@ -346,7 +390,7 @@ ssgd_status ssgd_rmsnorm(const void* x, int64_t x_pitch, const void* residual, i
     });
 }
 
-int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d) { return shape_ok(SSGD_F32, SSGD_F32, rows, d) ? teams_for(rows, d) * d : -1; }
+int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d) { return shape_ok(SSGD_F32, SSGD_F32, rows, d) ? groups_for(rows, d) * d : -1; }
 
 ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* s, int64_t s_pitch, const void* weight, int32_t dtype, int32_t weight_dtype,
                                   const float* rstd, const void* dsum, int64_t dsum_pitch, int64_t rows, int64_t d, void* dx, int64_t dx_pitch, float* dweight,
@@ -361,7 +405,7 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
         }
         Backward a{};
         a.dy = dy; a.s = s; a.w = weight; a.dsum = dsum; a.rstd = rstd; a.dx = dx; a.partial = dweight ? work : nullptr;
-        a.rows = rows; a.dy_pitch = dy_pitch; a.s_pitch = s_pitch; a.dsum_pitch = dsum_pitch; a.dx_pitch = dx_pitch; a.teams = teams_for(rows, d);
+        a.rows = rows; a.dy_pitch = dy_pitch; a.s_pitch = s_pitch; a.dsum_pitch = dsum_pitch; a.dx_pitch = dx_pitch; a.groups = groups_for(rows, d);
         a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (rows > 0) {
@@ -369,7 +413,7 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
         }
         ssgd_status st = op_hip(hipGetLastError(), "rmsnorm backward");
         if (st == SSGD_OK && dweight != nullptr) {
-            hipLaunchKernelGGL(weight_kernel, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, stream, work, a.teams, (int32_t)d, dweight);
+            hipLaunchKernelGGL(weight_kernel, dim3((unsigned)((d + 15) / 16)), dim3(1024), 0, stream, work, a.groups, (int32_t)d, dweight);
             st = op_hip(hipGetLastError(), "rmsnorm backward");
         }
         return st;
