@@ -132,7 +132,7 @@ __device__ __forceinline__ float clip_factor(const Rule& rule, double* part) {
     return c > 1.0f ? 1.0f : c;           // (a NaN stays)
 }
 
-// The update.  268 M parameters with bf16 gradients and copy: 1421 us with 32-bit moments (4.9 TB/s), 940 us with 8-bit ones (4.6 TB/s).  Four elements
+// The update.  268 M parameters with bf16 gradients and copy: 1421 us with 32-bit moments (5.3 TB/s), 940 us with 8-bit ones (4.6 TB/s).  Four elements
 // a thread at a time with 32-bit moments, so that a wave's accesses are whole lines; eight with 8-bit ones, so that sixteen lanes hold a block.
 template <int BITS, typename G>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, Rule rule) {
