@@ -140,6 +140,8 @@ def test_rmsnorm_backward_refuses(L, bad):
 
 
 def test_rmsnorm_work_floats(L):
-    assert L.ssgd_rmsnorm_work_floats(0, 100) == 0 and L.ssgd_rmsnorm_work_floats(3, 100) == 300
-    assert L.ssgd_rmsnorm_work_floats(1 << 20, 100) > 0
+    assert L.ssgd_rmsnorm_work_floats(0, 100) == 0
+    for rows, d in ((1, 1), (3, 100), (1 << 20, 100), (1 << 20, 3000), (500, 20000)):       # a sum per workgroup
+        floats = L.ssgd_rmsnorm_work_floats(rows, d)
+        assert floats % d == 0 and 1 <= floats // d <= min(rows, 1024)
     assert L.ssgd_rmsnorm_work_floats(-1, 100) == -1 and L.ssgd_rmsnorm_work_floats(1, 0) == -1
