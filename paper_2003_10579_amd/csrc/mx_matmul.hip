@@ -375,7 +375,8 @@ __global__ __launch_bounds__(64 * WAVES) void one_row_kernel(Product p, Rows x) 
     for (int u = threadIdx.x; u < many * per_row; u += 64 * WAVES) {
         const int row = u / per_row, col = (u - row * per_row) * 8;
         Eight<X> v;
-        v.load(static_cast<const X*>(x.x) + row * x.pitch + col, x.cols - col);
+        v.load(static_cast<const X*>(x.x) + row * x.pitch, col, x.cols);     // (more than 512 columns)
+        v.settle(col, x.cols);
         const uint32_t byte = mx_scale_byte<FA>(max_of_4(v.largest()));
         if constexpr (FA == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(rows + row * row_bytes + col / 2) = mx_pack_fp4(v.values(), byte);
         else *reinterpret_cast<words2*>(rows + row * row_bytes + col) = mx_pack_fp8(v.values(), byte);

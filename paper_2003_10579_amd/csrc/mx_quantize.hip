@@ -34,7 +34,9 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Source s, Target t, int6
     if (g >= groups) return;                 // (groups is a multiple of 16: whole blocks)
     const int64_t row = g / groups_per_row, col = (g - row * groups_per_row) * 8;
     Eight<T> x;
-    x.load(static_cast<const T*>(s.x) + row * s.pitch + col, s.cols - col);
+    const T* from = static_cast<const T*>(s.x) + row * s.pitch;
+    if (s.cols >= 8) { x.load(from, col, s.cols); x.settle(col, s.cols); }
+    else x.load_few(from, col, s.cols);
     store_block<FMT>(t, row, col, x);
 }
 
@@ -67,12 +69,20 @@ __global__ __launch_bounds__(kTileThreads) void tile_kernel(Source s, Target t, 
     Eight<T> x[kTile / 32];
 #pragma unroll
     for (int q = 0; q < kTile / 32; ++q) {
-        const int64_t row = r0 + q * 32 + (threadIdx.x >> 4), col = c0 + lane_col;
-        x[q].load(static_cast<const T*>(s.x) + row * s.pitch + col, row < s.rows ? s.cols - col : 0);
+        const int64_t row = r0 + q * 32 + (threadIdx.x >> 4);
+        if constexpr (sizeof(T) == 4) {
+            load_vec<8>(static_cast<const T*>(s.x) + row * s.pitch + c0 + lane_col, row < s.rows ? s.cols - c0 - lane_col : 0, x[q].x);
+        } else {
+            const T* from = static_cast<const T*>(s.x) + (row < s.rows ? row : s.rows - 1) * s.pitch;
+            const int64_t col = row < s.rows ? c0 + lane_col : s.cols;       // (past the last row: zeros)
+            if (s.cols >= 8) x[q].load(from, col, s.cols);
+            else x[q].load_few(from, col, s.cols);
+        }
     }
 #pragma unroll
     for (int q = 0; q < kTile / 32; ++q) {
         const int r = q * 32 + (threadIdx.x >> 4);
+        if (sizeof(T) == 2 && s.cols >= 8) x[q].settle(r0 + r < s.rows ? c0 + lane_col : s.cols, s.cols);
         put(&tile[place(r, lane_col)], x[q]);
         if constexpr (ROWS >= 0) { if (r0 + r < s.rows) store_block<ROWS>(t, r0 + r, c0 + lane_col, x[q]); }
     }

@@ -199,11 +199,18 @@ __device__ __forceinline__ words2 mx_pack_fp8(const words4& w, uint32_t byte) {
     return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-// Eight values in a row, in their own type, as quantisation takes them: their largest magnitude as the bits of an fp32 number.
+// Eight columns of a row, in their own type: what quantisation and the norm take.  `load` reads the row's last eight where fewer are left, so it
+// has no branch and nothing waits between the loads of several places; `settle`, when they have arrived, moves them to the front and puts zeros
+// behind the row's end.  (In fp32 the loads at a row's end do not wait for each other by themselves.)  Rows of less than eight columns: `load_few`.
+// `load_own` reads no other columns than the eight, and settles itself; AT_ONCE: loads past the end read the last column, since one that is left
+// out would wait for those before.  `largest`: the largest magnitude as the bits of an fp32 number.
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     float x[8];
-    __device__ __forceinline__ void load(const float* p, int64_t left) { load_vec<8>(p, left, x); }
+    __device__ __forceinline__ void load(const float* row, int64_t col, int64_t cols) { load_vec<8>(row + col, cols - col, x); }
+    __device__ __forceinline__ void load_few(const float* row, int64_t col, int64_t cols) { load(row, col, cols); }
+    template <bool> __device__ __forceinline__ void load_own(const float* row, int64_t col, int64_t cols) { load(row, col, cols); }
+    __device__ __forceinline__ void settle(int64_t, int64_t) {}
     __device__ __forceinline__ uint32_t largest() const {
         uint32_t most = 0;
 #pragma unroll
@@ -218,12 +225,35 @@ template <> struct Eight<float> {
 };
 template <> struct Eight<bf16_t> {
     words4 w;
-    __device__ __forceinline__ void load(const bf16_t* p, int64_t left) {
-        if (left >= 8) { w = *reinterpret_cast<const words4_any*>(p); return; }
+    __device__ __forceinline__ void load(const bf16_t* row, int64_t col, int64_t cols) {
+        w = *reinterpret_cast<const words4_any*>(row + (col < cols - 8 ? col : cols - 8));
+    }
+    __device__ __forceinline__ void load_few(const bf16_t* row, int64_t col, int64_t cols) {
         uint32_t v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (2 * q < left ? p[2 * q] : 0u) | (2 * q + 1 < left ? (uint32_t)p[2 * q + 1] << 16 : 0u);
+        for (int q = 0; q < 4; ++q) v[q] = (col + 2 * q < cols ? row[col + 2 * q] : 0u) | (col + 2 * q + 1 < cols ? (uint32_t)row[col + 2 * q + 1] << 16 : 0u);
         w = words4{v[0], v[1], v[2], v[3]};
+    }
+    template <bool AT_ONCE> __device__ __forceinline__ void load_own(const bf16_t* row, int64_t col, int64_t cols) {
+        const int64_t left = cols - col;
+        if (left >= 8) { w = *reinterpret_cast<const words4_any*>(row + col); return; }
+        if constexpr (!AT_ONCE) { load_few(row, col, cols); return; }
+        w = words4{0u, 0u, 0u, 0u};
+        if (left <= 0) return;
+        uint32_t v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = row[q < left ? col + q : cols - 1];
+#pragma unroll
+        for (int q = 1; q < 8; ++q) if (q >= left) v[q] = 0u;
+        w = words4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+    }
+    __device__ __forceinline__ void settle(int64_t col, int64_t cols) {
+        if (col + 8 <= cols) return;
+        const int gone = col < cols ? (int)(col + 8 - cols) : 8;
+        if (gone & 4) w = words4{w.z, w.w, 0u, 0u};
+        if (gone & 2) w = words4{w.y, w.z, w.w, 0u};
+        if (gone & 1) w = words4{w.x >> 16 | w.y << 16, w.y >> 16 | w.z << 16, w.z >> 16 | w.w << 16, w.w >> 16};
+        if (gone == 8) w = words4{0u, 0u, 0u, 0u};
     }
     __device__ __forceinline__ uint32_t largest() const {
         constexpr uint32_t kMagnitudes = 0x7FFF7FFFu;

@@ -4,8 +4,8 @@
 //   rstd = (mean s^2 + eps)^(-1/2),  y = (s rstd) w
 //   dx = rstd (g - xhat mean(g xhat)) + dsum,  g = dy w,  xhat = s rstd;    dw = sum over rows of dy xhat
 //
-// About 8 operations per element forward, 12 backward: bound by memory (16384 x 4096 in bf16: forward with 8-bit output 100 us, 4.7 TB/s; backward
-// 107 us with its sums over rows, 5.0 TB/s).  A row stays in the registers of 64, 256 or 1024 threads, eight
+// About 8 operations per element forward, 12 backward: bound by memory (16384 x 4096 in bf16: forward with 8-bit output 89 us, 5.3 TB/s; backward
+// 105 us with its sums over rows, 5.1 TB/s; rows of 999, 8192 of them, 12.8 and 18.8 us).  A row stays in the registers of 64, 256 or 1024 threads, eight
 // or sixteen columns each, between the sum of squares and the output, so it is read once; the threads go on to further rows with
 // their part of w, and backward with their part of dw, kept.  Rows of more than 16384 columns are read a second time instead.
 #include <cmath>
@@ -75,7 +75,7 @@ __device__ __forceinline__ void take_sum(const Forward& a, int64_t row, int col,
 }
 
 template <typename T, bool FP8>
-__device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, const float (&s)[8], float rstd, const float (&w)[8]) {
+__device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, int end, const float (&s)[8], float rstd, const float (&w)[8]) {
     float y[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) y[q] = (s[q] * rstd) * w[q];
@@ -87,36 +87,81 @@ __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int 
         *reinterpret_cast<words2*>(a.values + row * a.row_bytes + col) = mx_pack_fp8(y, byte);
         if ((threadIdx.x & 3) == 0) a.scales[row * a.scale_bytes + col / kMxBlock] = (uint8_t)byte;
     } else {
-        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, a.d - col, y);
+        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, end - col, y);
     }
 }
 
 __device__ __forceinline__ float inverse_root(double sum, const Forward& a) { return 1.0f / sqrtf((float)(sum / a.d) + a.eps); }
 
+// Eight columns of a row up to `end`, read and, when they have arrived, as numbers; SHORT: rows of less than eight columns are among them.
+template <bool SHORT, typename T>
+__device__ __forceinline__ void read(Eight<T>& to, const void* rows, int64_t row, int64_t pitch, int col, int end, int d) {
+    const T* from = static_cast<const T*>(rows) + row * pitch;
+    if (!SHORT || d >= 8) to.load(from, col, end);
+    else to.load_few(from, col, end);
+}
+template <bool SHORT, typename T>
+__device__ __forceinline__ void numbers(Eight<T>& x, int col, int end, int d, float (&to)[8]) {
+    if (!SHORT || d >= 8) x.settle(col, end);
+    x.numbers(to);
+}
+
 template <typename T, bool FP8, int LANES, int NV>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forward a) {
     constexpr int kRows = LANES == 64 ? 4 : 1;         // teams of a workgroup
+    constexpr bool kShort = LANES == 64 && NV == 1;
     __shared__ double part[LANES / 64];
     const int lane = threadIdx.x & (LANES - 1);
     const int64_t team = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES, teams = (int64_t)gridDim.x * kRows;
     const int end = FP8 ? (int)mx_padded(a.d) : a.d;
+    // Threads whose columns are not the row's last ones know that there are eight (kernels with NV > 1 have rows that long).
+    auto col_of = [&](int v) { return (v * LANES + lane) * 8; };
+    auto end_of = [&](int v) { return v < NV - 1 ? col_of(v) + 8 : a.d; };
+    Eight<T> next_x[NV], next_r[NV];
+    auto load = [&](int64_t row) {
+        if (row >= a.rows) return;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) read<kShort>(next_x[v], a.x, row, a.x_pitch, col_of(v), end_of(v), a.d);
+        if (a.residual != nullptr) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) read<kShort>(next_r[v], a.residual, row, a.residual_pitch, col_of(v), end_of(v), a.d);
+        }
+    };
+    // (the next row's, while a row's sum is taken: fp32 16384 x 4096 197 us instead of 200; threads of 1024 have no registers for it)
+    constexpr bool kAhead = LANES < 1024;
+    if constexpr (kAhead) load(team);
     float w[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, (v * LANES + lane) * 8, a.d, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, col_of(v), end_of(v), w[v]);
     for (int64_t row = team; row < a.rows; row += teams) {
+        if constexpr (!kAhead) load(row);
         float s[NV][8];
         float sum = 0.0f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            take_sum<T>(a, row, (v * LANES + lane) * 8, s[v]);
+        for (int v = 0; v < NV; ++v) numbers<kShort>(next_x[v], col_of(v), end_of(v), a.d, s[v]);
+        if (a.residual != nullptr) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) sum += s[v][q] * s[v][q];
+            for (int v = 0; v < NV; ++v) {
+                float r[8];
+                numbers<kShort>(next_r[v], col_of(v), end_of(v), a.d, r);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s[v][q] = as_stored(static_cast<const T*>(nullptr), s[v][q] + r[q]);
+            }
         }
-        const float rstd = inverse_root(team_sum<LANES>((double)sum, part), a);
-        if (lane == 0) a.rstd[row] = rstd;
+        if constexpr (kAhead) load(row + teams);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
-            if ((v * LANES + lane) * 8 < end) store_normed<T, FP8>(a, row, (v * LANES + lane) * 8, s[v], rstd, w[v]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += s[v][q] * s[v][q];
+        const float rstd = inverse_root(team_sum<LANES>((double)sum, part), a);
+        if (lane == 0) a.rstd[row] = rstd;
+        // (s may go where x or the residual were: the threads have read theirs, each the row's last columns too, before they met for the sum)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int col = col_of(v);
+            if (a.residual != nullptr) store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, end_of(v) - col, s[v]);
+            if (v < NV - 1 || col < end) store_normed<T, FP8>(a, row, col, end_of(v), s[v], rstd, w[v]);
+        }
     }
 }
 
@@ -142,22 +187,27 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
             if (a.residual != nullptr) load_vec<8>(static_cast<const T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
             else load_vec<8>(static_cast<const T*>(a.x) + row * a.x_pitch + col, a.d - col, s);
             load_weight(a.w, a.w_bf16, (int)col, a.d, w);
-            store_normed<T, FP8>(a, row, (int)col, s, rstd, w);
+            store_normed<T, FP8>(a, row, (int)col, a.d, s, rstd, w);
         }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void store_dx(const Backward& a, int64_t row, int64_t col, const float (&dy)[8], const float (&xhat)[8], const float (&w)[8], float rstd,
+template <typename T, bool AT_ONCE>
+__device__ __forceinline__ void store_dx(const Backward& a, int64_t row, int64_t col, int64_t end, const float (&dy)[8], const float (&xhat)[8], const float (&w)[8], float rstd,
                                          float c) {
     float dx[8], more[8];
-    if (a.dsum != nullptr) load_vec<8>(static_cast<const T*>(a.dsum) + row * a.dsum_pitch + col, a.d - col, more);
+    if (a.dsum != nullptr) {
+        Eight<T> x;        // (dx may go where dsum was: a thread reads no more than it writes)
+        const T* from = static_cast<const T*>(a.dsum) + row * a.dsum_pitch;
+        x.template load_own<AT_ONCE>(from, col, end);
+        x.numbers(more);
+    }
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         dx[q] = rstd * (dy[q] * w[q] - xhat[q] * c);
         if (a.dsum != nullptr) dx[q] += more[q];
     }
-    store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, a.d - col, dx);
+    store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, end - col, dx);
 }
 
 template <typename T, int LANES, int NV>
@@ -166,15 +216,22 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     __shared__ double part[LANES / 64];
     __shared__ float dw_of[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? LANES * NV * 8 : 1];
     const int lane = threadIdx.x & (LANES - 1), team = threadIdx.x / LANES;
+    constexpr bool kShort = LANES == 64 && NV == 1;
+    // Sixteen columns to each of 1024 threads fill their registers: they read as load_own does, one place after the other (4000 x 16000 in bf16: 116 us;
+    // as the others do, 171).
+    constexpr bool kWide = LANES < 1024 || NV == 1;
+    // Threads whose columns are not the row's last ones know that there are eight (kernels with NV > 1 have rows that long).
+    auto col_of = [&](int v) { return (v * LANES + lane) * 8; };
+    auto end_of = [&](int v) { return v < NV - 1 && kWide ? col_of(v) + 8 : a.d; };
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_weight(a.w, a.w_bf16, (v * LANES + lane) * 8, a.d, w[v]);
+        load_weight(a.w, a.w_bf16, col_of(v), end_of(v), w[v]);
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[v][q] = 0.0f;
     }
     // The next row's dy and s are on their way while a row's sum is taken (16384 x 1500: 60 us instead of 74; threads of 1024 have no registers
-    // for it, 4000 x 16000: 126 us instead of 119).
+    // for it, 4000 x 16000: 126 us instead of 119).  (dx may go where dy was, as s in the forward pass.)
     constexpr bool kAhead = LANES < 1024;
     Eight<T> next_dy[NV], next_s[NV];
     float next_rstd = 0.0f;
@@ -183,9 +240,13 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
         next_rstd = a.rstd[row];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int col = (v * LANES + lane) * 8;
-            next_dy[v].load(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col);
-            next_s[v].load(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col);
+            if constexpr (kWide) {
+                read<kShort>(next_dy[v], a.dy, row, a.dy_pitch, col_of(v), end_of(v), a.d);
+                read<kShort>(next_s[v], a.s, row, a.s_pitch, col_of(v), end_of(v), a.d);
+            } else {
+                next_dy[v].template load_own<false>(static_cast<const T*>(a.dy) + row * a.dy_pitch, col_of(v), a.d);
+                next_s[v].template load_own<false>(static_cast<const T*>(a.s) + row * a.s_pitch, col_of(v), a.d);
+            }
         }
     };
     const int64_t first = (int64_t)blockIdx.x * kRows + team, step = a.groups * kRows;
@@ -197,8 +258,13 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            next_dy[v].numbers(dy[v]);
-            next_s[v].numbers(xhat[v]);
+            if constexpr (kWide) {
+                numbers<kShort>(next_dy[v], col_of(v), end_of(v), a.d, dy[v]);
+                numbers<kShort>(next_s[v], col_of(v), end_of(v), a.d, xhat[v]);
+            } else {
+                next_dy[v].numbers(dy[v]);
+                next_s[v].numbers(xhat[v]);
+            }
         }
         if constexpr (kAhead) load(row + step);
 #pragma unroll
@@ -213,8 +279,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
         const float c = (float)(team_sum<LANES>((double)sum, part) / a.d);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int col = (v * LANES + lane) * 8;
-            if (col < a.d) store_dx<T>(a, row, col, dy[v], xhat[v], w[v], rstd, c);
+            if ((v < NV - 1 && kWide) || col_of(v) < a.d) store_dx<T, kWide>(a, row, col_of(v), end_of(v), dy[v], xhat[v], w[v], rstd, c);
         }
     }
     if (a.partial == nullptr) return;
@@ -238,8 +303,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int col = (v * LANES + lane) * 8;
-        store_vec<8>(a.partial + (int64_t)blockIdx.x * a.d + col, a.d - col, dw[v]);
+        store_vec<8>(a.partial + (int64_t)blockIdx.x * a.d + col_of(v), end_of(v) - col_of(v), dw[v]);
     }
 }
 
@@ -270,7 +334,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             load_weight(a.w, a.w_bf16, (int)col, a.d, w);
 #pragma unroll
             for (int q = 0; q < 8; ++q) s[q] *= rstd;
-            store_dx<T>(a, row, col, dy, s, w, rstd, c);
+            store_dx<T, false>(a, row, col, a.d, dy, s, w, rstd, c);
             if (a.partial == nullptr) continue;
             float* to = a.partial + (int64_t)blockIdx.x * a.d + col;
             float dw[8];
@@ -286,8 +350,9 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
     }
 }
 
-// dw of 16 columns: the 64 quarter waves of a workgroup take every 64th partial sum, eight loads in flight, and add in fp64 (768 sums of
-// 4096 columns: 8 us; with 64 columns and whole cache lines to a workgroup no faster).
+// dw of 16 columns: the 64 quarter waves of a workgroup take every 64th partial sum, eight loads in flight (a load that is left out would
+// wait for those before: past the end the last sum is read again), and add in fp64 (768 sums of 4096 columns: 6.0 us, 512 of 1537 4.3 us; with 64 columns
+// and whole cache lines to a workgroup no faster).
 __global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int64_t groups, int32_t d, float* dw) {
     __shared__ double part[64][17];
     const int c = threadIdx.x & 15, group = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
@@ -296,9 +361,9 @@ __global__ __launch_bounds__(1024) void weight_kernel(const float* partial, int6
         for (int64_t t = group; t < groups; t += 64 * 8) {
             float x[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[q] = t + 64 * q < groups ? partial[(t + 64 * q) * d + col] : 0.0f;
+            for (int q = 0; q < 8; ++q) x[q] = partial[(t + 64 * q < groups ? t + 64 * q : groups - 1) * d + col];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) sum += (double)x[q];
+            for (int q = 0; q < 8; ++q) sum += t + 64 * q < groups ? (double)x[q] : 0.0;
         }
     }
     part[group][c] = sum;

@@ -77,6 +77,23 @@ def test_strides_and_misaligned_matrices(env, dtype, fmt):
         assert back.shape == view.shape and np.array_equal(_host(back), ref.rounded(_host(view), fmt))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_every_row_end(env, dtype):
+    """Whatever lies around a matrix, and wherever in a thread's eight columns its rows end, the result is that of the matrix alone."""
+    torch, ssgd = env
+    for cols in [*range(1, 42), *range(120, 138), 520, 643]:
+        x = _values(torch, 37, cols, getattr(torch, dtype), cols).cuda()
+        room = torch.full((39, cols + 9), float("nan"), dtype=x.dtype, device="cuda")
+        room[1:38, 3:3 + cols] = x
+        inside = room[1:38, 3:3 + cols]
+        for f in ("fp4", "fp8"):
+            pairs = list(zip(ssgd.mx_quantize_both(x, f, f), ssgd.mx_quantize_both(inside, f, f)))
+            pairs.append((pairs[0][0], ssgd.mx_quantize(inside, f)))
+            pairs.append((pairs[1][0], ssgd.mx_quantize_transposed(inside, f)))
+            assert all(torch.equal(a.values, b.values) and torch.equal(a.scales, b.scales) for a, b in pairs), cols
+            assert not torch.any(pairs[0][0].scales == 255), cols
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_the_whole_range_of_fp32(env, fmt):
     """Every exponent, from the numbers below the normal ones to the largest, alone and beside small ones."""

@@ -176,6 +176,48 @@ def test_nothing_is_written_beside_the_outputs(env):
         assert torch.equal(g.reshape(-1), dx[32:32 + rows * d])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_every_row_end(env, dtype):
+    """Whatever lies around the rows, and wherever in a thread's eight columns they end, the results are those of the rows alone."""
+    torch, ssgd = env
+    for d in [*range(1, 42), *range(504, 522), 1030, 1537, 4103, 8197]:
+        x, r, w, dy, dsum = _inputs(torch, 3, d, getattr(torch, dtype), d)
+        y, s, rstd = ssgd.rmsnorm(x, w, residual=r)
+        want = (y, s, rstd) + ssgd.rmsnorm_backward(dy, s, w, rstd, dsum=dsum)
+        def within(t):
+            room = torch.full((5, d + 9), float("nan"), dtype=t.dtype, device="cuda")
+            room[1:4, 3:3 + d] = t
+            return room[1:4, 3:3 + d]
+        y2, s2, rstd2 = ssgd.rmsnorm(within(x), w, residual=within(r))
+        got = (y2, s2, rstd2) + ssgd.rmsnorm_backward(within(dy), within(s2), w, rstd2, dsum=within(dsum))
+        assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(want, got)), d
+        q, q2 = ssgd.rmsnorm(x, w, residual=r, output="fp8")[0], ssgd.rmsnorm(within(x), w, residual=within(r), output="fp8")[0]
+        assert torch.equal(q.values, q2.values) and torch.equal(q.scales, q2.scales), d
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("d", [7, 50, 513, 1000, 1537, 2055, 4000, 6001, 8200, 17001])
+def test_in_place(env, d, dtype):
+    """The sum over x or over the residual, the gradient over dy or over dsum: as into arrays of their own."""
+    torch, ssgd = env
+    L, dt, kind, rows = ssgd.lib(), getattr(torch, dtype), 0 if dtype == "float32" else 1, 2500 if d < 5000 else 700
+    x, r, w, dy, dsum = _inputs(torch, rows, d, dt, d)
+    y, s, rstd = ssgd.rmsnorm(x, w, residual=r)
+    dx, _ = ssgd.rmsnorm_backward(dy, s, w, rstd, dsum=dsum)
+    stream = torch.cuda.current_stream().cuda_stream
+    for over_x in (True, False):
+        a, b, y2, rstd2 = x.clone(), r.clone(), torch.empty_like(x), torch.empty_like(rstd)
+        to = a if over_x else b
+        assert L.ssgd_rmsnorm(a.data_ptr(), d, b.data_ptr(), d, w.data_ptr(), kind, 0, rows, d, 1e-6, to.data_ptr(), d, y2.data_ptr(), d, None, None,
+                              rstd2.data_ptr(), stream) == 0
+        assert torch.equal(to, s) and torch.equal(y2, y) and torch.equal(rstd2, rstd)
+        a, b = dy.clone(), dsum.clone()
+        to = a if over_x else b
+        assert L.ssgd_rmsnorm_backward(a.data_ptr(), d, s.data_ptr(), d, w.data_ptr(), kind, 0, rstd.data_ptr(), b.data_ptr(), d, rows, d, to.data_ptr(), d,
+                                       None, None, stream) == 0
+        assert torch.equal(to, dx)
+
+
 def test_another_stream_gives_the_same(env):
     torch, ssgd = env
     x, r, w, dy, dsum = _inputs(torch, 700, 3000, torch.bfloat16, 1)
