@@ -93,7 +93,7 @@ __device__ __forceinline__ void unpack_fp8(words2 w, float scale, float (&x)[8])
 }
 
 // Sum of squares of the pieces of a launch, in fp64 (fp32 squares overflow from 1.8e19 on), one number per workgroup.  Bound by memory: 268 M bf16
-// gradients 144 us, 3.7 TB/s, behind an update that left the caches full of lines to be written back.
+// gradients 139 us, 3.9 TB/s, behind an update that left the caches full of lines to be written back.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void square_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, double* partials) {
     __shared__ double part[kThreads / 64];
@@ -102,13 +102,16 @@ __global__ __launch_bounds__(kThreads) void square_kernel(const Piece* pieces, i
         const Piece w = pieces[c];
         const G* g = grads.of[w.tensor] + w.first;
         for (int i = threadIdx.x * 8; i < w.n; i += kThreads * 32) {
-            float x[4][8];
+            Eight<G> four[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) load_vec<8>(g + i + u * kThreads * 8, w.n - i - u * kThreads * 8, x[u]);
+            for (int u = 0; u < 4; ++u) four[u].template load_own<false>(g, i + u * kThreads * 8, w.n);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 4; ++u) {
+                float x[8];
+                four[u].numbers(x);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) sum += (double)x[u][q] * (double)x[u][q];
+                for (int q = 0; q < 8; ++q) sum += (double)x[q] * (double)x[q];
+            }
         }
     }
     sum = wave_sum(sum);
@@ -132,8 +135,9 @@ __device__ __forceinline__ float clip_factor(const Rule& rule, double* part) {
     return c > 1.0f ? 1.0f : c;           // (a NaN stays)
 }
 
-// The update.  268 M parameters with bf16 gradients and copy: 1421 us with 32-bit moments (5.3 TB/s), 940 us with 8-bit ones (4.6 TB/s).  Four elements
-// a thread at a time with 32-bit moments, so that a wave's accesses are whole lines; eight with 8-bit ones, so that sixteen lanes hold a block.
+// The update.  268 M parameters with bf16 gradients and copy: 1420 us with 32-bit moments (5.3 TB/s), 925 us with 8-bit ones (4.6 TB/s; 820 where no
+// clipping has read the gradients before).  Four elements a thread at a time with 32-bit moments, so that a wave's accesses are whole lines; eight
+// with 8-bit ones, so that sixteen lanes hold a block.
 template <int BITS, typename G>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, Rule rule) {
     constexpr int V = BITS == 8 ? 8 : 4;
@@ -150,14 +154,19 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Piece* pieces, in
         const int left = w.n - i;
         const int64_t at = w.state + i;
         float p[V], gr[V], m[V], v[V];
-        load_vec<V>(w.p + i, left, p);
-        load_vec<V>(g + i, left, gr);
+        // (the gradients last: in bf16 they are waited for at once, and the others then arrive meanwhile)
         if constexpr (BITS == 32) {
             load_vec<V>(static_cast<const float*>(rule.m) + at, V, m);
             load_vec<V>(static_cast<const float*>(rule.v) + at, V, v);
+            load_vec<V>(w.p + i, left, p);
+            load_vec<V>(g + i, left, gr);
         } else {
-            unpack_fp8(*reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.m) + at), rule.m_scale[at / kStateBlock], m);
-            unpack_fp8(*reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.v) + at), rule.v_scale[at / kStateBlock], v);
+            const words2 some_m = *reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.m) + at), some_v = *reinterpret_cast<const words2*>(static_cast<const uint8_t*>(rule.v) + at);
+            const float m_scale = rule.m_scale[at / kStateBlock], v_scale = rule.v_scale[at / kStateBlock];
+            load_vec<V>(w.p + i, left, p);
+            load_vec<V>(g + i, left, gr);
+            unpack_fp8(some_m, m_scale, m);
+            unpack_fp8(some_v, v_scale, v);
 #pragma unroll
             for (int q = 0; q < V; ++q) v[q] = v[q] * v[q];
         }
