@@ -261,31 +261,30 @@ __device__ __forceinline__ ints8 operand_at(const uint8_t* a, int64_t step) {
     else return operand(*reinterpret_cast<const words4*>(a + step * 128), *reinterpret_cast<const words4*>(a + step * 128 + 64));
 }
 
-// The sums of the waves, and the results.
+// The sums of the waves, and the results: every wave adds the waves' sums of its share of the tiles, in the waves' order.
 template <int TM, int TN, int WAVES, typename T>
 __device__ __forceinline__ void join_and_store(const Product& p, f32x4 (&acc)[TM][TN], f32x4 (*part)[TM * TN][64], int wave, int64_t m0, int64_t n0) {
     const int lane = threadIdx.x & 63;
-    if constexpr (WAVES > 1) {
-        if (wave > 0) {
+    auto store = [&](int i, const f32x4& sum) { store_four<T>(p, m0 + i / TN * 16 + (lane & 15), n0 + i % TN * 16 + (lane >> 4) * 4, sum); };
+    if constexpr (WAVES == 1) {
 #pragma unroll
-            for (int i = 0; i < TM * TN; ++i) part[wave - 1][i][lane] = acc[i / TN][i % TN];
-        }
+        for (int i = 0; i < TM * TN; ++i) store(i, acc[i / TN][i % TN]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i) part[wave][i][lane] = acc[i / TN][i % TN];
         __syncthreads();
-        if (wave > 0) return;
+        for (int i = wave; i < TM * TN; i += WAVES) {
+            f32x4 sum = part[0][i][lane];
 #pragma unroll
-        for (int w = 0; w < WAVES - 1; ++w)
-#pragma unroll
-            for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] += part[w][i][lane];
+            for (int w = 1; w < WAVES; ++w) sum += part[w][i][lane];
+            store(i, sum);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) store_four<T>(p, m0 + i * 16 + (lane & 15), n0 + j * 16 + (lane >> 4) * 4, acc[i][j]);
 }
 
 template <int FA, int TM, int TN, int WAVES, typename T>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(Product p) {
-    __shared__ f32x4 part[WAVES > 1 ? WAVES - 1 : 1][TM * TN][64];
+    __shared__ f32x4 part[WAVES][TM * TN][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * (TN * 16), m0 = (int64_t)blockIdx.y * (TM * 16);
     const uint8_t *a[TM], *sa[TM], *b[TN], *sb[TN];
@@ -352,7 +351,7 @@ struct Rows { const void* x; int64_t pitch, cols; };
 
 template <int FA, int WAVES, typename X, typename T>
 __global__ __launch_bounds__(64 * WAVES) void one_row_kernel(Product p, Rows x) {
-    __shared__ f32x4 part[WAVES - 1][1][64];
+    __shared__ f32x4 part[WAVES][1][64];
     __shared__ __attribute__((aligned(16))) uint8_t rows[kRoomForRows];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
@@ -468,7 +467,7 @@ int64_t parts_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
 template <int FA, typename T>
 void launch(Product p, void* work, hipStream_t s) {
     // 16 rows of B to a workgroup, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as often (61 x 6144 x 5000
-    // in 4 bits: 10.9 us against 14.7; 64 x 2048 x 4096: 10.3 against 8.6).
+    // in 4 bits: 10.2 us against 15.6; 64 x 2048 x 4096: 9.5 against 8.3).
     const bool pairs = p.b.rows >= 5120;
     if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
     else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
