@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int kA = BM * kRowA, kB = BN * kRowB, kStage = kA + kB;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves, kLoads = kLoadsA + kLoadsB;
-    static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && BM + BN == 64 * kWaves, "every wave loads the same share");
+    static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && BM + BN <= 64 * kWaves, "every wave loads the same share");
     constexpr int kGroupSteps = STAGES == 3 ? 3 : 4;
     static_assert(STAGES >= 2 && STAGES <= 4, "a group ends at the stage it began with");
     // (arrays of their own: the compiler then sees that loads into one do not concern reads of another)
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage2[STAGES > 2 ? kStage : 16];
     __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 3 ? kStage : 16];
-    __shared__ __attribute__((aligned(1024))) uint8_t scales[(BM + BN) * 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t scales[64 * kWaves * 16];      // (a row of A or B to a thread, the last ones again where there are more threads)
 
     // Workgroups go to the XCDs in turn; each XCD takes tiles that lie together, in groups of 4 rows of tiles, so that its L2 holds what
     // they share.
@@ -444,45 +444,71 @@ void tiles(Product p, hipStream_t s) {
     hipLaunchKernelGGL((tile_kernel<FA, BM, BN, WM, WN, STAGES, T>), dim3((unsigned)((all + kXcds - 1) / kXcds * kXcds), parts), dim3(64 * WM * WN), 0, s, p);
 }
 
-// Parts that a contraction is split into where tiles of 128 are too few to keep the CUs busy: the one with the least time, 0.40 us a step of a
-// tile (0.52 in 8 bits) and what the join costs, its launch and the parts written and read.  (128 x 8192 x 8192: 26.7 us whole and 19.7 in four
-// parts in 4 bits, 37 and 22.9 in 8.)
-int parts_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
-    const int64_t tiles = (M + 127) / 128 * ((N + 127) / 128);
-    if (M <= kFewRows || tiles > 128) return 1;
-    const double step = a_fmt == SSGD_MX_FP4 ? 0.40 : 0.52, join = 4.0, results = (double)M * (double)N * 8.0 / 5.0e6;
-    int best = 1;
-    double least = step * (double)steps;
-    for (int n = 2; n <= 8 && n * tiles <= 512 && n * 4 <= steps; ++n) {
-        const double t = step * (double)((steps + n - 1) / n) + join + results * n;
-        if (t < least) { least = t; best = n; }
+// Where tiles of 256 are too few: rows of A to a tile of 128 rows of B (128, 96 in 8 bits, 64), and the parts its contraction is split into, those with
+// the least time by a model: a step of the tiles that one CU has, and for parts the join's launch and their results written and read.
+// (In 8 bits: 4001 x 2100 x 1500 22.1 us with 96 rows, 24.9 with 128, 24.6 with 64; 2100 x 1500 x 4001 25.9, 23.0 and 22.7; 300 x 6144 x 5000 22.6, 25.6 and
+// 17.8; 128 x 8192 x 8192 18.8 with 64 rows in two parts, 21.9 with 128 in four, 23.0 with 64 whole.)
+struct Tiling { int rows, parts; double time; };
+Tiling tiling_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
+    Tiling best{128, 1, 1e30};
+    for (int rows : {128, 96, 64}) {
+        if (rows == 96 && a_fmt == SSGD_MX_FP4) continue;       // (not a whole number of loads to a wave)
+        const double step = a_fmt == SSGD_MX_FP4 ? (rows == 128 ? 0.36 : 0.25) : (rows == 128 ? 0.53 : (rows == 96 ? 0.41 : 0.30));     // us, every CU with a tile
+        for (int n = 1; n <= 8 && (n == 1 || n * 4 <= steps); ++n) {
+            const int64_t tiles = (M + rows - 1) / rows * ((N + 127) / 128) * n, rounds = (tiles + 255) / 256;
+            double t = step * (double)((steps + n - 1) / n) * (tiles < 256 ? 0.7 + 0.3 / 256 * (double)tiles : (double)rounds);
+            if (n > 1) t += 3.0 + (double)M * (double)N * 8.0 / 6.0e6 * n;
+            if (t < best.time) best = {rows, n, t};
+        }
     }
     return best;
 }
+bool few_tiles(int64_t M, int64_t N) { return M <= kFewRows || (M + 255) / 256 * ((N + 255) / 256) < 200; }
+
+// 16 rows of B to a workgroup of the kernel for few rows, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as
+// often (61 x 6144 x 5000 in 4 bits: 10.2 us against 15.6; 64 x 2048 x 4096: 9.5 against 8.3).
+bool pairs_of(int64_t N) { return N >= 5120; }
+// 17 to 64 rows of A through that kernel, by the same kind of model: its steps against those of the tiles, which cost 1.5 us more to begin with.
+// (64 x 8192 x 8192 in 8 bits: 14.7 us through tiles, 23.8 through this; 64 x 6144 x 1500: 7.3 and 6.9.)
+bool takes_few_rows(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
+    if (M <= 16 || M > kFewRows) return M <= 16;
+    const bool pairs = pairs_of(N);
+    const double step = a_fmt == SSGD_MX_FP4 ? (M > 32 ? (pairs ? 0.20 : 0.15) : (pairs ? 0.10 : 0.066)) : (M > 32 ? (pairs ? 0.29 : 0.28) : (pairs ? 0.127 : 0.11));
+    const double full = (double)((N + (pairs ? 31 : 15)) / (pairs ? 32 : 16)) / 256.0;
+    return step * (double)steps * (full < 1.0 ? 0.7 + 0.3 * full : full) <= tiling_of(a_fmt, M, N, steps).time + 1.5;
+}
+
 int64_t parts_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
-    const int n = parts_of(a_fmt, M, N, mx_padded(K) / kMxPad);
+    const int64_t steps = mx_padded(K) / kMxPad;
+    const int n = takes_few_rows(a_fmt, M, N, steps) || !few_tiles(M, N) ? 1 : tiling_of(a_fmt, M, N, steps).parts;
     return n > 1 ? n * M * N * 4 : 0;
 }
 
 template <int FA, typename T>
+void tiles_of(int rows, const Product& p, hipStream_t s) {
+    // (stages: as many as LDS holds for two workgroups of a CU, four at most; with 128 rows in 8 bits, 2100 x 1500 x 4001: 30 us with two, 23 with three)
+    if (rows == 64) { tiles<FA, 64, 128, 2, 2, 4, T>(p, s); return; }
+    if constexpr (FA == SSGD_MX_FP8) { if (rows == 96) { tiles<FA, 96, 128, 2, 2, 3, T>(p, s); return; } }
+    tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
+}
+
+template <int FA, typename T>
 void launch(Product p, void* work, hipStream_t s) {
-    // 16 rows of B to a workgroup, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as often (61 x 6144 x 5000
-    // in 4 bits: 10.2 us against 15.6; 64 x 2048 x 4096: 9.5 against 8.3).
-    const bool pairs = p.b.rows >= 5120;
-    if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
-    else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
-    else if (p.a.rows <= kFewRows) { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
+    if (takes_few_rows(FA, p.a.rows, p.b.rows, p.steps)) {
+        const bool pairs = pairs_of(p.b.rows);
+        if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
+        else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
+        else { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
+    }
     // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 279 us in 4 bits against 403 with tiles of 128; 1000 x 8192 x 8192, 128
-    // tiles: 57 against 53).  Stages: as many as LDS holds, for tiles of 128 of two workgroups per CU (2100 x 1500 x 4001 in 8 bits: 30 us with
-    // two, 22 with three; 4001 x 2100 x 1500 27 and 23, with four and one workgroup per CU 28).
-    else if ((p.a.rows + 255) / 256 * ((p.b.rows + 255) / 256) < 200) {
-        constexpr int kStages = FA == SSGD_MX_FP4 ? 4 : 3;
-        const int parts = parts_of(FA, p.a.rows, p.b.rows, p.steps);
-        if (parts == 1) { tiles<FA, 128, 128, 2, 2, kStages, T>(p, s); return; }
+    // tiles: 57 against 53).
+    else if (few_tiles(p.a.rows, p.b.rows)) {
+        const Tiling how = tiling_of(FA, p.a.rows, p.b.rows, p.steps);
+        if (how.parts == 1) { tiles_of<FA, T>(how.rows, p, s); return; }
         Product q = p;
         q.out = work; q.pitch = p.b.rows; q.part_stride = p.a.rows * p.b.rows;
-        q.part_steps = (p.steps + parts - 1) / parts;
-        tiles<FA, 128, 128, 2, 2, kStages, float>(q, s);
+        q.part_steps = (p.steps + how.parts - 1) / how.parts;
+        tiles_of<FA, float>(how.rows, q, s);
         const int64_t per_row = (p.b.rows + 3) / 4, groups = p.a.rows * per_row;
         hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(work), (p.steps + q.part_steps - 1) / q.part_steps,
                            q.part_stride, static_cast<T*>(p.out), p.a.rows, p.b.rows, p.pitch, per_row);

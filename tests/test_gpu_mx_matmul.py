@@ -74,6 +74,34 @@ def test_product(env, shape, fmt):
     assert ssgd.mx_linear(x.cuda(), b, fmt, torch.bfloat16).dtype == torch.bfloat16
 
 
+# tiles of 128, 96 and 64 rows with every kind of end, whole and in parts, 17 to 64 rows on either side of the rule between the kernels
+TILES = [(2100, 1500, 900), (2050, 1030, 600), (1500, 1500, 1100), (1700, 1900, 2500), (900, 9000, 300), (1200, 1100, 600), (1000, 1000, 20000), (700, 700, 30000),
+         (500, 500, 9000), (97, 260, 5000), (64, 512, 8200), (33, 6100, 8000), (24, 4100, 16000), (40, 28700, 130), (64, 16500, 700), (48, 51300, 300)]
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("shape", TILES, ids=str)
+def test_product_by_tiles(env, shape, fmt):
+    torch, ssgd = env
+    M, N, K = shape
+    x, w = _matrix(torch, M, K, M + K), _matrix(torch, N, K, N + K + 1)
+    a, b = ssgd.mx_quantize(x.cuda(), fmt), ssgd.mx_quantize(w.cuda(), "fp4")
+    ah, bh = _host(ssgd.mx_dequantize(a)), _host(ssgd.mx_dequantize(b))
+    for dtype in ("float32", "bfloat16"):
+        _close(_host(ssgd.mx_matmul(a, b, getattr(torch, dtype))), ah, bh, fmt, dtype)
+    assert torch.equal(ssgd.mx_linear(x.cuda(), b, format=fmt), ssgd.mx_matmul(a, b, torch.float32))
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_parts_of_every_length(env, fmt):
+    """Contractions in parts whose last one has any number of steps, a single one too."""
+    torch, ssgd = env
+    for K in range(1900, 6000, 128):
+        x, w = _matrix(torch, 65, K, K), _matrix(torch, 130, K, K + 1)
+        a, b = ssgd.mx_quantize(x.cuda(), fmt), ssgd.mx_quantize(w.cuda(), "fp4")
+        _close(_host(ssgd.mx_matmul(a, b, torch.float32)), _host(ssgd.mx_dequantize(a)), _host(ssgd.mx_dequantize(b)), fmt, "float32")
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_a_layer_forward_and_backward(env, fmt):
     """y = x w^T, dx = dy w, dw = dy^T x by quantisation along rows and columns: each against the product of the values that its own
