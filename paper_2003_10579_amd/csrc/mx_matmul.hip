@@ -444,18 +444,23 @@ void tiles(Product p, hipStream_t s) {
     hipLaunchKernelGGL((tile_kernel<FA, BM, BN, WM, WN, STAGES, T>), dim3((unsigned)((all + kXcds - 1) / kXcds * kXcds), parts), dim3(64 * WM * WN), 0, s, p);
 }
 
-// Where tiles of 256 are too few: rows of A to a tile of 128 rows of B (128, 96 in 8 bits, 64), and the parts its contraction is split into, those with
-// the least time by a model: a step of the tiles that one CU has, and for parts the join's launch and their results written and read.
-// (In 8 bits: 4001 x 2100 x 1500 22.1 us with 96 rows, 24.9 with 128, 24.6 with 64; 2100 x 1500 x 4001 25.9, 23.0 and 22.7; 300 x 6144 x 5000 22.6, 25.6 and
-// 17.8; 128 x 8192 x 8192 18.8 with 64 rows in two parts, 21.9 with 128 in four, 23.0 with 64 whole.)
+// Rows of A to a tile, 256 with 256 rows of B or 128, 96 (in 8 bits) and 64 with 128, and the parts that the contraction is split into: those with the least
+// time by a model, a step of the tiles that one CU has, and for parts the join's launch and their results written and read.
+// (8192^3 in 4 bits: 275 us with 256 rows, 398 without them.  In 8 bits: 4100 x 4100 x 4096 94 us with 256, 78 with 128; 4001 x 2100 x 1500 22.1 us with 96
+// rows, 24.9 with 128, 24.6 with 64; 2100 x 1500 x 4001 25.9, 23.0 and 22.7; 300 x 6144 x 5000 22.6, 25.6 and 17.8; 128 x 8192 x 8192 18.8 with 64 rows in two
+// parts, 21.9 with 128 in four, 23.0 with 64 whole.)
+constexpr int64_t kMostParts = 1024;      // tiles of parts, 64 MB of results
 struct Tiling { int rows, parts; double time; };
 Tiling tiling_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
     Tiling best{128, 1, 1e30};
-    for (int rows : {128, 96, 64}) {
+    for (int rows : {256, 128, 96, 64}) {
         if (rows == 96 && a_fmt == SSGD_MX_FP4) continue;       // (not a whole number of loads to a wave)
-        const double step = a_fmt == SSGD_MX_FP4 ? (rows == 128 ? 0.36 : 0.25) : (rows == 128 ? 0.53 : (rows == 96 ? 0.41 : 0.30));     // us, every CU with a tile
-        for (int n = 1; n <= 8 && (n == 1 || n * 4 <= steps); ++n) {
-            const int64_t tiles = (M + rows - 1) / rows * ((N + 127) / 128) * n, rounds = (tiles + 255) / 256;
+        const double step = a_fmt == SSGD_MX_FP4 ? (rows == 256 ? 1.06 : (rows == 128 ? 0.36 : 0.25))       // us, with a tile for every CU
+                                                 : (rows == 256 ? 1.42 : (rows == 128 ? 0.53 : (rows == 96 ? 0.41 : 0.30)));
+        const int64_t across = rows == 256 ? (N + 255) / 256 : (N + 127) / 128;
+        for (int n = 1; n <= 8; ++n) {
+            const int64_t tiles = (M + rows - 1) / rows * across * n, rounds = (tiles + 255) / 256;
+            if (n > 1 && (rows == 256 || n * 4 > steps || tiles > kMostParts)) break;
             double t = step * (double)((steps + n - 1) / n) * (tiles < 256 ? 0.7 + 0.3 / 256 * (double)tiles : (double)rounds);
             if (n > 1) t += 3.0 + (double)M * (double)N * 8.0 / 6.0e6 * n;
             if (t < best.time) best = {rows, n, t};
@@ -463,7 +468,6 @@ Tiling tiling_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
     }
     return best;
 }
-bool few_tiles(int64_t M, int64_t N) { return M <= kFewRows || (M + 255) / 256 * ((N + 255) / 256) < 200; }
 
 // 16 rows of B to a workgroup of the kernel for few rows, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as
 // often (61 x 6144 x 5000 in 4 bits: 10.2 us against 15.6; 64 x 2048 x 4096: 9.5 against 8.3).
@@ -480,13 +484,18 @@ bool takes_few_rows(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
 
 int64_t parts_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
     const int64_t steps = mx_padded(K) / kMxPad;
-    const int n = takes_few_rows(a_fmt, M, N, steps) || !few_tiles(M, N) ? 1 : tiling_of(a_fmt, M, N, steps).parts;
+    const int n = takes_few_rows(a_fmt, M, N, steps) ? 1 : tiling_of(a_fmt, M, N, steps).parts;
     return n > 1 ? n * M * N * 4 : 0;
 }
 
 template <int FA, typename T>
 void tiles_of(int rows, const Product& p, hipStream_t s) {
     // (stages: as many as LDS holds for two workgroups of a CU, four at most; with 128 rows in 8 bits, 2100 x 1500 x 4001: 30 us with two, 23 with three)
+    if (rows == 256) {
+        if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
+        else tiles<FA, 256, 256, 4, 2, 3, T>(p, s);
+        return;
+    }
     if (rows == 64) { tiles<FA, 64, 128, 2, 2, 4, T>(p, s); return; }
     if constexpr (FA == SSGD_MX_FP8) { if (rows == 96) { tiles<FA, 96, 128, 2, 2, 3, T>(p, s); return; } }
     tiles<FA, 128, 128, 2, 2, FA == SSGD_MX_FP4 ? 4 : 3, T>(p, s);
@@ -499,22 +508,17 @@ void launch(Product p, void* work, hipStream_t s) {
         if (p.a.rows <= 16) { if (pairs) few_rows<FA, 1, 2, kRowWaves, T>(p, s); else few_rows<FA, 1, 1, kRowWaves, T>(p, s); }
         else if (p.a.rows <= 32) { if (pairs) few_rows<FA, 2, 2, 8, T>(p, s); else few_rows<FA, 2, 1, 8, T>(p, s); }
         else { if (pairs) few_rows<FA, 4, 2, 8, T>(p, s); else few_rows<FA, 4, 1, 4, T>(p, s); }
+        return;
     }
-    // Tiles of 256 where there are enough of them to fill most CUs (8192^3: 279 us in 4 bits against 403 with tiles of 128; 1000 x 8192 x 8192, 128
-    // tiles: 57 against 53).
-    else if (few_tiles(p.a.rows, p.b.rows)) {
-        const Tiling how = tiling_of(FA, p.a.rows, p.b.rows, p.steps);
-        if (how.parts == 1) { tiles_of<FA, T>(how.rows, p, s); return; }
-        Product q = p;
-        q.out = work; q.pitch = p.b.rows; q.part_stride = p.a.rows * p.b.rows;
-        q.part_steps = (p.steps + how.parts - 1) / how.parts;
-        tiles_of<FA, float>(how.rows, q, s);
-        const int64_t per_row = (p.b.rows + 3) / 4, groups = p.a.rows * per_row;
-        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(work), (p.steps + q.part_steps - 1) / q.part_steps,
-                           q.part_stride, static_cast<T*>(p.out), p.a.rows, p.b.rows, p.pitch, per_row);
-    }
-    else if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
-    else tiles<FA, 256, 256, 4, 2, 3, T>(p, s);
+    const Tiling how = tiling_of(FA, p.a.rows, p.b.rows, p.steps);
+    if (how.parts == 1) { tiles_of<FA, T>(how.rows, p, s); return; }
+    Product q = p;
+    q.out = work; q.pitch = p.b.rows; q.part_stride = p.a.rows * p.b.rows;
+    q.part_steps = (p.steps + how.parts - 1) / how.parts;
+    tiles_of<FA, float>(how.rows, q, s);
+    const int64_t per_row = (p.b.rows + 3) / 4, groups = p.a.rows * per_row;
+    hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(work), (p.steps + q.part_steps - 1) / q.part_steps,
+                       q.part_stride, static_cast<T*>(p.out), p.a.rows, p.b.rows, p.pitch, per_row);
 }
 
 constexpr int64_t kMostRows = int64_t(1) << 31, kMostCols = (int64_t(1) << 24) - kMxPad;
