@@ -44,7 +44,7 @@ def _close(got, a, b, fmt, dtype):
     assert np.all(np.abs(got - want) <= bound + 1.01 * place)
 
 
-# few rows (one, two and four groups of 16, partial ones), tiles of 128 and, from 200 tiles of 256 on, of 256; contractions from one column to
+# few rows (one, two and four groups of 16, partial ones), tiles of 64 and of 256; contractions from one column to
 # many steps of 128, each remainder of the stages; rows of B that are no multiple of anything
 SHAPES = [(1, 1, 1), (1, 3, 5), (2, 50, 900), (3, 50, 900), (2, 40, 17000), (1, 5200, 700), (16, 5130, 600), (20, 5121, 513), (50, 5150, 1300), (1, 16, 128), (1, 17, 4096), (1, 300, 3072), (2, 512, 3071), (15, 33, 129), (16, 100, 640), (17, 100, 512), (32, 40, 2200), (33, 70, 1000),
           (61, 130, 5000), (64, 64, 8192), (65, 1, 100), (65, 127, 300), (100, 129, 129), (65, 70, 5000), (128, 300, 9000), (200, 129, 3200), (256, 1000, 4225), (128, 128, 128), (129, 257, 256), (130, 130, 384), (300, 200, 512),
