@@ -107,14 +107,21 @@ def test_mx_linear_refuses(L, bad, rows):
 def test_mx_work_bytes(L):
     linear, matmul = L.ssgd_mx_linear_work_bytes, L.ssgd_mx_matmul_work_bytes
     assert linear(1, 10, 50, 1000) == 10 * (1024 + 32) and linear(0, 9, 50, 1000) == 9 * (512 + 32)
-    # a long contraction with few results is split, one with many is not
-    assert matmul(0, 128, 8192, 8192) >= 2 * 128 * 8192 * 4 and matmul(0, 128, 8192, 8192) % (128 * 8192 * 4) == 0
-    assert linear(0, 128, 8192, 8192) == matmul(0, 128, 8192, 8192) + 128 * (4096 + 256)
-    assert matmul(0, 128, 8192, 128) == 0 and matmul(0, 8192, 8192, 8192) == 0 and matmul(1, 64, 8192, 8192) == 0 and matmul(1, 300, 300, 0) == 0
+    # a long contraction with few results is split, one with many or a short one is not; the parts are whole sets of results
+    assert matmul(0, 128, 1000, 100000) >= 2 * 128 * 1000 * 4
+    for fmt in (0, 1):
+        for rows in (20, 64, 65, 128, 700):
+            for n in (1000, 8192):
+                for k in (4000, 8192, 30000):
+                    parts = matmul(fmt, rows, n, k)
+                    assert parts % (rows * n * 4) == 0 and parts <= 8 * rows * n * 4
+                    wide = -(-k // 128) * 128
+                    assert linear(fmt, rows, n, k) == parts + -(-rows * (wide // (1 if fmt else 2) + wide // 32) // 16) * 16
+    assert matmul(0, 128, 8192, 128) == 0 and matmul(0, 8192, 8192, 8192) == 0 and matmul(1, 16, 8192, 8192) == 0 and matmul(1, 300, 300, 0) == 0
     for f in (linear, matmul):
         assert f(2, 10, 50, 1000) == -1 and f(0, -1, 50, 10) == -1 and f(0, 1, -1, 10) == -1 and f(0, 1, 50, 1 << 24) == -1
-    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 8192, 8192, A, 0, 8192, None, None), b"work")
-    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 8192, 8192, A, 0, 8192, A + 8, None), b"work")
+    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 1000, 100000, A, 0, 1000, None, None), b"work")
+    _refused(L, L.ssgd_mx_matmul(A, A, 0, 128, A, A, 1000, 100000, A, 0, 1000, A + 8, None), b"work")
 
 
 @pytest.mark.parametrize("bad", [
