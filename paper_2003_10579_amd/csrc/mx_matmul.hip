@@ -4,8 +4,8 @@
 // 4 bits, that block's 16 bytes; in 8 bits bytes 16 g .. 16 g + 15 and the same 64 further on.  B's rows are the instruction's first
 // operand and A's its second, so that a lane's four results are consecutive columns of a row of C.
 //
-// 8192^3 in 4 bits: 275 to 305 us (3.6 to 4.0 PFLOP/s; 228 on zeros, whose bits draw less power), of which the matrix instructions alone take 189, with the reads of their operands from LDS
-// 214 and with the stores 235; in 8 by 4 bits 376 us (2.9 PFLOP/s; instructions 292).
+// 8192^3 in 4 bits: 275 to 305 us (3.6 to 4.0 PFLOP/s; 228 on zeros, whose bits draw less power), of which the matrix instructions alone take 189, with the
+// reads of their operands from LDS 214 and with the stores 235; in 8 by 4 bits 376 us (2.9 PFLOP/s; instructions 292).
 #include <type_traits>
 
 #include "ops.hpp"
