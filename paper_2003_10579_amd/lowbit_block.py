@@ -13,6 +13,12 @@ from __future__ import annotations
 
 import argparse
 import math
+import os
+import sys
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+if ROOT not in sys.path:
+    sys.path.insert(0, ROOT)
 
 
 class Block:
