@@ -457,6 +457,7 @@ class MxTensor:
     __slots__ = ("format", "shape", "device", "_values", "_scales", "_room", "_at")
 
     def __init__(self, values, scales, format, shape):
+        _torch or _load()          # (with stored arrays this may be a program's first call)
         if format not in _FORMATS:
             _refuse("mx: the format is 'fp4' or 'fp8'")
         rows, cols = shape

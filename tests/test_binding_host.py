@@ -1,0 +1,59 @@
+"""What the binding keeps and hands over, without a GPU: stand-ins for device tensors, and library calls that record instead of running."""
+import copy
+import os
+import pickle
+
+import numpy as np
+import pytest
+
+from paper_2003_10579_amd import ssgd
+
+
+class Tensor:
+    """As much of a device tensor as the binding looks at; its memory moves when it is copied."""
+    is_cuda, device = True, "a GPU"
+
+    def __init__(self, array):
+        self.array = array
+
+    shape = property(lambda self: self.array.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def element_size(self):
+        return self.array.itemsize
+
+    def data_ptr(self):
+        return self.array.ctypes.data
+
+
+@pytest.fixture(scope="module")
+def library():
+    if not os.path.exists(ssgd._LIB_PATH):
+        from paper_2003_10579_amd import build
+        build.build()
+    return ssgd.lib()
+
+
+@pytest.fixture
+def fresh(library, monkeypatch):
+    """The binding as a new process has it, with a device that needs no starting."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "init", lambda: None)
+    for name in ("_torch", "_raw_stream", "_device_now", "_lib"):
+        monkeypatch.setattr(ssgd, name, None)
+    monkeypatch.setattr(ssgd, "_DTYPES", {})
+    return torch
+
+
+def _stored(rows=3, cols=40):
+    return ssgd.MxTensor(Tensor(np.zeros((rows, 64), np.uint8)), Tensor(np.zeros((rows, 4), np.uint8)), "fp4", (rows, cols))
+
+
+def test_a_stored_matrix_is_enough_to_begin_with(fresh):
+    """The first thing that a program does may be a product of matrices that it has read from a file."""
+    _stored()
+    assert ssgd._torch is fresh and ssgd._lib is not None
+    assert ssgd._DTYPES == {fresh.float32: ssgd.F32, fresh.bfloat16: ssgd.BF16}
+    assert callable(ssgd._raw_stream) and callable(ssgd._device_now)

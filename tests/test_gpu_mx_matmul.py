@@ -221,3 +221,18 @@ def test_refusals(env):
         with pytest.raises(ssgd.SsgdError) as e:
             call()
         assert e.value.status == ssgd.EINVAL
+
+
+def test_stored_matrices_in_a_first_call(env, monkeypatch):
+    """A product, and values read back, of matrices from stored arrays before any other operator has run."""
+    torch, ssgd = env
+    a, b = (ssgd.mx_quantize(_matrix(torch, n, 300, n).cuda(), f) for n, f in ((5, "fp8"), (9, "fp4")))
+    want, back = ssgd.mx_matmul(a, b, torch.float32), ssgd.mx_dequantize(a, torch.bfloat16)
+    arrays = [(q.values, q.scales, q.format, q.shape) for q in (a, b)]
+    def fresh():
+        for name in ("_torch", "_raw_stream", "_device_now"):
+            monkeypatch.setattr(ssgd, name, None)
+        monkeypatch.setattr(ssgd, "_DTYPES", {})
+        return [ssgd.MxTensor(*q) for q in arrays]
+    assert torch.equal(ssgd.mx_matmul(*fresh(), torch.float32), want)
+    assert torch.equal(ssgd.mx_dequantize(fresh()[0], torch.bfloat16), back)
