@@ -469,6 +469,9 @@ class MxTensor:
         self.format, self.shape, self.device, self._room = format, (rows, cols), values.device, None
         self._values, self._scales, self._at = values, scales, (values.data_ptr(), scales.data_ptr())
 
+    def __reduce__(self):          # (a copy or a stored one has addresses of its own)
+        return MxTensor, (self.values, self.scales, self.format, self.shape)
+
     @classmethod
     def empty(cls, rows, cols, format, device):
         _torch or _load()

@@ -57,3 +57,14 @@ def test_a_stored_matrix_is_enough_to_begin_with(fresh):
     assert ssgd._torch is fresh and ssgd._lib is not None
     assert ssgd._DTYPES == {fresh.float32: ssgd.F32, fresh.bfloat16: ssgd.BF16}
     assert callable(ssgd._raw_stream) and callable(ssgd._device_now)
+
+
+def test_a_copied_matrix_has_its_own_addresses(fresh):
+    """Copies, and what is read back from a pickle, point at their own arrays and not where the first ones were."""
+    q = _stored()
+    q.values.array[:], q.scales.array[:] = 5, 7
+    for other in (copy.deepcopy(q), pickle.loads(pickle.dumps(q)), copy.copy(q)):
+        assert other._at == (other.values.data_ptr(), other.scales.data_ptr())
+        assert (other.format, other.shape, other.device) == (q.format, q.shape, q.device)
+        assert np.all(other.values.array == 5) and np.all(other.scales.array == 7)
+    assert copy.deepcopy(q)._at != q._at and copy.copy(q)._at == q._at

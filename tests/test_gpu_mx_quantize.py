@@ -173,3 +173,22 @@ def test_refusals(env):
                                      (q.values, q.scales, "fp6", (8, 64)), (q.values.float(), q.scales, "fp4", (8, 64))):
         with pytest.raises(ssgd.SsgdError):
             ssgd.MxTensor(values, scales, f, shape)
+
+
+def test_copies_are_matrices_of_their_own(env):
+    """A deep copy and a stored matrix keep their values when the first one changes."""
+    import copy
+    import io
+    torch, ssgd = env
+    x = torch.randn(9, 200, generator=torch.Generator().manual_seed(3)).cuda()
+    for fmt in ("fp4", "fp8"):
+        q = ssgd.mx_quantize(x, fmt)
+        want = ssgd.mx_dequantize(q)
+        stored = io.BytesIO()
+        torch.save(q, stored)
+        stored.seek(0)
+        others = [copy.deepcopy(q), torch.load(stored, weights_only=False)]       # (written a line above)
+        q.values.zero_()
+        for other in others:
+            assert other.shape == (9, 200) and other.format == fmt and torch.equal(ssgd.mx_dequantize(other), want)
+        assert not ssgd.mx_dequantize(copy.copy(q)).any()
