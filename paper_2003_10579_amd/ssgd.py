@@ -430,6 +430,9 @@ class AdamW:
             _lib.ssgd_adamw_destroy(self.h)
             self.h = None
 
+    def __reduce__(self):          # (both would free the handle)
+        _refuse("adamw: an optimizer cannot be copied or pickled; its state is m, v, m_scale, v_scale and t")
+
     def __del__(self):
         if _lib is not None:        # the interpreter may be past it
             self.close()

@@ -68,3 +68,51 @@ def test_a_copied_matrix_has_its_own_addresses(fresh):
         assert (other.format, other.shape, other.device) == (q.format, q.shape, q.device)
         assert np.all(other.values.array == 5) and np.all(other.scales.array == 7)
     assert copy.deepcopy(q)._at != q._at and copy.copy(q)._at == q._at
+
+
+class Recorder:
+    """A library whose calls succeed and are written down."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            if name == "ssgd_adamw_create":
+                args[-1]._obj.value = 0x1234
+            return args[0] * 128 if name == "ssgd_adamw_state_elements" else ssgd.OK
+        return call
+
+
+@pytest.fixture
+def optimizer(fresh, monkeypatch):
+    """(torch, the recorder, a function that makes an AdamW of three parameters and their copies)."""
+    import contextlib
+    torch = fresh
+
+    class Parameter(torch.nn.Parameter):
+        is_cuda = True
+    recorder = Recorder()
+    ssgd._load()
+    monkeypatch.setattr(ssgd, "_lib", recorder)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(ssgd, "_call", lambda entry, device, *args: entry(*args))
+
+    def make(**more):
+        params = [Parameter(torch.ones(n)) for n in (3, 0, 5)]
+        return params, ssgd.AdamW(params, **more)
+    return torch, recorder, make
+
+
+def test_an_optimizer_is_not_copied(optimizer):
+    """A copy would free the first one's handle a second time."""
+    torch, recorder, make = optimizer
+    _, opt = make()
+    for attempt in (copy.copy, copy.deepcopy, pickle.dumps):
+        with pytest.raises(ssgd.SsgdError) as e:
+            attempt(opt)
+        assert e.value.status == ssgd.EINVAL and "adamw" in str(e.value)
+    opt.close()
+    opt.close()
+    assert [name for name, _ in recorder.calls].count("ssgd_adamw_destroy") == 1
