@@ -364,12 +364,30 @@ def _call(entry, device, *args):
         _check(status)
 
 
+def _moment(name):
+    """An array of the optimizer's state: its handle keeps the address, so what is assigned is copied into it."""
+    def get(self):
+        return self._moments[name]
+
+    def put(self, value):
+        own = self._moments[name]
+        if own is None and value is None:
+            return
+        if not (own is not None and isinstance(value, _torch.Tensor) and value.shape == own.shape and value.dtype == own.dtype):
+            _refuse(f"adamw: {name} takes a tensor of its own shape and type, where there is one")
+        own.copy_(value.detach())
+    return property(get, put)
+
+
 class AdamW:
     """AdamW over many tensors at once (ssgd_adamw_*): fp32 parameters, updated in place; `copies` (a list of bfloat16
     tensors, entries may be None) receive them rounded.  The moments are `m` and `v`, flat arrays of 32-bit numbers or, with
     `state_bits=8`, of E4M3 values (of m and of the root of v) with a scale per 128 elements in `m_scale`, `v_scale`; `t`
-    counts the updates.  These five are all that a checkpoint needs.  With `max_norm` gradients are clipped to that norm
-    over all tensors, and `grad_norm` (one element on the device) holds the norm of the last step's."""
+    counts the updates.  These five are all that a checkpoint needs (a tensor that is assigned to one of the arrays is copied
+    into it).  With `max_norm` gradients are clipped to that norm over all tensors, and `grad_norm` (one element on the
+    device) holds the norm of the last step's."""
+
+    m, v, m_scale, v_scale = (_moment(name) for name in ("m", "v", "m_scale", "v_scale"))
 
     def __init__(self, params, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, max_norm=0.0, state_bits=32, seed=0, copies=None):
         _torch or _load()
@@ -394,10 +412,9 @@ class AdamW:
         total = lib().ssgd_adamw_state_elements(n, sizes)
         if state_bits not in (8, 32):
             _refuse("adamw: state_bits is 8 or 32")
-        self.m = torch.zeros(total, device=dev, dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn)
-        self.v = torch.zeros_like(self.m)
-        self.m_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
-        self.v_scale = torch.zeros(total // 128, device=dev) if state_bits == 8 else None
+        moment = lambda: torch.zeros(total, device=dev, dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn)  # noqa: E731
+        scale = lambda: torch.zeros(total // 128, device=dev) if state_bits == 8 else None  # noqa: E731
+        self._moments = {"m": moment(), "v": moment(), "m_scale": scale(), "v_scale": scale()}
         self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
         self.t = 0
         self._keep, self._device, self._grads = (params, copies), dev, (C.c_void_p * n)()

@@ -116,3 +116,25 @@ def test_an_optimizer_is_not_copied(optimizer):
     opt.close()
     opt.close()
     assert [name for name, _ in recorder.calls].count("ssgd_adamw_destroy") == 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_assigned_moments_go_into_the_optimizers_own(optimizer, bits):
+    """The handle keeps the addresses of the arrays that it was made with: moments that a program assigns are copied into them."""
+    torch, _, make = optimizer
+    _, opt = make(state_bits=bits)
+    names = ["m", "v"] + (["m_scale", "v_scale"] if bits == 8 else [])
+    places = {name: getattr(opt, name).data_ptr() for name in names}
+    for k, name in enumerate(names):
+        new = torch.full_like(getattr(opt, name), k + 1.0)
+        setattr(opt, name, new)
+        assert getattr(opt, name).data_ptr() == places[name] and torch.all(getattr(opt, name).float() == k + 1)
+        for wrong in (new[:1], new.float().double(), None, 3.0):
+            with pytest.raises(ssgd.SsgdError):
+                setattr(opt, name, wrong)
+    if bits == 32:
+        opt.m_scale = opt.v_scale = None          # as a checkpoint of such an optimizer has them
+        assert opt.m_scale is None and opt.v_scale is None
+        with pytest.raises(ssgd.SsgdError):
+            opt.m_scale = torch.zeros(3)
+    opt.close()

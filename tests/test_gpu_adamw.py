@@ -292,3 +292,27 @@ def test_refusals(env):
     opt.close()
     with pytest.raises(ssgd.SsgdError):
         opt.step([p], 0.1)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_checkpoint_that_is_assigned(env, bits):
+    """Moments that a program assigns are what the next step uses: two steps, and one step from the stored state of the first, agree."""
+    torch, ssgd = env
+    g = torch.Generator().manual_seed(bits)
+    start, grads = torch.randn(700, generator=g).cuda(), [torch.randn(700, generator=g).cuda() for _ in range(2)]
+    p = start.clone()
+    opt = ssgd.AdamW([p], state_bits=bits, seed=9)
+    opt.step(grads[:1], 0.1)
+    names = ("m", "v", "m_scale", "v_scale")
+    stored = {k: None if getattr(opt, k) is None else getattr(opt, k).clone() for k in names}
+    q = p.clone()
+    opt.step(grads[1:], 0.1)
+    other = ssgd.AdamW([q], state_bits=bits, seed=9)
+    for k in names:
+        setattr(other, k, stored[k])
+    other.t = 1
+    del stored
+    other.step(grads[1:], 0.1)
+    assert torch.equal(p, q) and torch.equal(opt.m.float(), other.m.float()) and torch.equal(opt.v.float(), other.v.float())
+    opt.close()
+    other.close()
