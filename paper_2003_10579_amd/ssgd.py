@@ -417,7 +417,8 @@ class AdamW:
         self._moments = {"m": moment(), "v": moment(), "m_scale": scale(), "v_scale": scale()}
         self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
         self.t = 0
-        self._keep, self._device, self._grads = (params, copies), dev, (C.c_void_p * n)()
+        self._places = [(p, p.data_ptr()) for p in params + [c for c in copies if c is not None]]
+        self._device, self._grads = dev, (C.c_void_p * n)()
         pointers = C.c_void_p * n
         o = AdamWOptions(float(betas[0]), float(betas[1]), float(eps), float(max_norm), state_bits, seed)
         h = C.c_void_p()
@@ -429,11 +430,15 @@ class AdamW:
         self.h = h
 
     def step(self, grads, lr):
-        """One update with a list of gradients, contiguous tensors of one type (float32 or bfloat16) and their parameters' sizes."""
+        """One update with a list of gradients, contiguous tensors of one type (float32 or bfloat16) and their parameters' sizes.
+        Parameters and copies have to be where they were when the optimizer was made."""
         if self.h is None:
             _refuse("adamw: closed")
         if len(grads) != len(self._sizes):
             _refuse("adamw step: one gradient per tensor")
+        for p, place in self._places:
+            if p.data_ptr() != place:
+                _refuse("adamw step: a parameter or its copy has moved since the optimizer was made")
         kind, dev, at = grads[0].dtype, self._device, self._grads
         for k, (g, n) in enumerate(zip(grads, self._sizes)):
             if not (g.dtype == kind and g.numel() == n and g.device == dev and g.is_contiguous()):

@@ -99,10 +99,15 @@ def optimizer(fresh, monkeypatch):
     monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
     monkeypatch.setattr(ssgd, "_call", lambda entry, device, *args: entry(*args))
 
+    made = []
+
     def make(**more):
         params = [Parameter(torch.ones(n)) for n in (3, 0, 5)]
-        return params, ssgd.AdamW(params, **more)
-    return torch, recorder, make
+        made.append(ssgd.AdamW(params, **more))
+        return params, made[-1]
+    yield torch, recorder, make
+    for opt in made:
+        opt.close()          # (while the recorder is there: the handles are made up)
 
 
 def test_an_optimizer_is_not_copied(optimizer):
@@ -137,4 +142,25 @@ def test_assigned_moments_go_into_the_optimizers_own(optimizer, bits):
         assert opt.m_scale is None and opt.v_scale is None
         with pytest.raises(ssgd.SsgdError):
             opt.m_scale = torch.zeros(3)
+    opt.close()
+
+
+def test_parameters_that_have_moved_are_refused(optimizer):
+    """A parameter whose data was replaced (p.data = ..., a module that was converted) is no longer where the handle writes."""
+    torch, recorder, make = optimizer
+    copies = [torch.ones(3, dtype=torch.bfloat16), None, torch.ones(5, dtype=torch.bfloat16)]
+    params, opt = make(copies=copies)
+    grads = [torch.ones(n) for n in (3, 0, 5)]
+    opt.step(grads, 0.1)
+    steps = lambda: [name for name, _ in recorder.calls].count("ssgd_adamw_step")  # noqa: E731
+    assert steps() == 1 and opt.t == 1
+    for moved in (params[2], copies[0]):
+        before = moved.data
+        moved.data = before.clone()
+        with pytest.raises(ssgd.SsgdError) as e:
+            opt.step(grads, 0.1)
+        assert e.value.status == ssgd.EINVAL and "moved" in str(e.value) and steps() == 1 and opt.t == 1
+        moved.data = before
+    opt.step(grads, 0.1)
+    assert steps() == 2 and opt.t == 2
     opt.close()

@@ -316,3 +316,20 @@ def test_a_checkpoint_that_is_assigned(env, bits):
     assert torch.equal(p, q) and torch.equal(opt.m.float(), other.m.float()) and torch.equal(opt.v.float(), other.v.float())
     opt.close()
     other.close()
+
+
+def test_a_moved_parameter_is_refused(env):
+    torch, ssgd = env
+    p = torch.nn.Parameter(torch.ones(300, device="cuda"))
+    opt = ssgd.AdamW([p])
+    g = torch.ones(300, device="cuda")
+    opt.step([g], 0.1)
+    before = p.data
+    p.data = before.clone()
+    with pytest.raises(ssgd.SsgdError) as e:
+        opt.step([g], 0.1)
+    assert e.value.status == ssgd.EINVAL and opt.t == 1
+    p.data = before
+    opt.step([g], 0.1)
+    assert opt.t == 2
+    opt.close()
