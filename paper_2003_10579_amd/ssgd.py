@@ -328,14 +328,15 @@ def debug_batch(seed, replica, worker, ordinal, version, m, N):
 # (A call's host time is what its caller waits for where the kernels are short, so checks build no text unless they fail and
 # outputs share an allocation.)
 
-_torch = _raw_stream = _device_now = None
+_torch = _raw_stream = _device_now = _changed = None
 _DTYPES = {}
 
 
 def _load():
     """torch and what every call needs of it, looked up once."""
-    global _torch, _raw_stream, _device_now
+    global _torch, _raw_stream, _device_now, _changed
     import torch
+    from torch.autograd.graph import increment_version as _changed
     lib()
     _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
     _raw_stream, _device_now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
@@ -417,7 +418,8 @@ class AdamW:
         self._moments = {"m": moment(), "v": moment(), "m_scale": scale(), "v_scale": scale()}
         self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
         self.t = 0
-        self._places = [(p, p.data_ptr()) for p in params + [c for c in copies if c is not None]]
+        self._written = params + [c for c in copies if c is not None]
+        self._places = [(p, p.data_ptr()) for p in self._written]
         self._device, self._grads = dev, (C.c_void_p * n)()
         pointers = C.c_void_p * n
         o = AdamWOptions(float(betas[0]), float(betas[1]), float(eps), float(max_norm), state_bits, seed)
@@ -445,6 +447,7 @@ class AdamW:
                 _refuse("adamw step: gradients are contiguous tensors of one type, of their parameters' sizes and device")
             at[k] = g.data_ptr()
         _call(_lib.ssgd_adamw_step, dev, self.h, at, _dtype(kind), lr, self.t + 1, None if self.grad_norm is None else self.grad_norm.data_ptr())
+        _changed(self._written)        # (autograd's check of what it has kept for a backward pass)
         self.t += 1
 
     def close(self):

@@ -164,3 +164,14 @@ def test_parameters_that_have_moved_are_refused(optimizer):
     opt.step(grads, 0.1)
     assert steps() == 2 and opt.t == 2
     opt.close()
+
+
+def test_a_step_raises_the_version_counters(optimizer):
+    torch, _, make = optimizer
+    copies = [torch.ones(3, dtype=torch.bfloat16), None, None]
+    params, opt = make(copies=copies)
+    watched = [params[0], params[2], copies[0]]
+    before = [t._version for t in watched]
+    opt.step([torch.ones(n) for n in (3, 0, 5)], 0.1)
+    assert all(t._version > b for t, b in zip(watched, before))
+    opt.close()

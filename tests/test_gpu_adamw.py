@@ -333,3 +333,22 @@ def test_a_moved_parameter_is_refused(env):
     opt.step([g], 0.1)
     assert opt.t == 2
     opt.close()
+
+
+def test_torch_sees_that_a_step_has_changed_the_parameters(env):
+    """What autograd has kept of a parameter or its copy for a backward pass is out of date after a step: torch has to refuse it."""
+    torch, ssgd = env
+    p, frozen = torch.nn.Parameter(torch.ones(300, device="cuda")), torch.ones(50, device="cuda")
+    copy = torch.ones(300, device="cuda", dtype=torch.bfloat16)
+    with torch.inference_mode():
+        apart = torch.ones(20, device="cuda")           # (has no counter)
+    opt = ssgd.AdamW([p, frozen, apart], copies=[copy, None, None])
+    x = torch.ones(300, device="cuda", requires_grad=True)
+    before = [t._version for t in (p, frozen, copy)]
+    loss = (x * p).sum()
+    opt.step([torch.ones_like(t) for t in (p, frozen, apart)], 0.1)
+    assert all(t._version > b for t, b in zip((p, frozen, copy), before))
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    assert torch.all(p < 1) and torch.all(apart < 1)
+    opt.close()
