@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import warnings
 
 import numpy as np
 
@@ -325,6 +326,8 @@ def debug_batch(seed, replica, worker, ordinal, version, m, N):
 
 
 # ---- operators of a low-precision training step: on the device and the current stream of their tensors ----------------
+# They record no graph for autograd: backward passes are calls of their own (rmsnorm_backward, products with transposed quantisations), and a tensor
+# that requires a gradient is taken with a warning where torch would record one.
 # (A call's host time is what its caller waits for where the kernels are short, so checks build no text unless they fail and
 # outputs share an allocation.)
 
@@ -463,11 +466,18 @@ class AdamW:
             self.close()
 
 
+def _unrecorded(what):
+    warnings.warn(f"{what}: no graph is recorded, so this tensor gets no gradient through it (the gradients have calls of their own; "
+                  "detached tensors or torch.no_grad() say that this is meant)", stacklevel=4)
+
+
 def _matrix(x, what):
     """(device, dtype, rows, cols, pitch) of a matrix with contiguous rows."""
     _torch or _load()
     if not x.is_cuda or x.dim() != 2:
         _refuse(f"{what}: a matrix on the GPU is wanted")
+    if x.requires_grad and _torch.is_grad_enabled():
+        _unrecorded(what)
     rows, cols = x.shape
     pitch, step = x.stride()
     if rows <= 1:
@@ -586,7 +596,7 @@ def mx_matmul(a, b, dtype=None):
 
 def mx_linear(x, w, format="fp8", dtype=None):
     """x w^T for rows x (float32 or bfloat16), quantised to `format` on the way, and an "fp4" MxTensor w (outputs x inputs), as a
-    matrix of `dtype` (x's unless it is given)."""
+    matrix of `dtype` (x's unless it is given).  Autograd records nothing."""
     dev, kind, M, K, pitch = _matrix(x, "mx_linear")
     if format not in _FORMATS:
         _refuse("mx_linear: the format is 'fp4' or 'fp8'")
@@ -612,12 +622,14 @@ def _beside(t, x, what):
 def _weight(w, x, what):
     if not (w.dim() == 1 and w.numel() == x.shape[1] and w.is_contiguous() and w.device == x.device):
         _refuse(f"{what}: a contiguous weight per column is wanted")
+    if w.requires_grad and _torch.is_grad_enabled():
+        _unrecorded(what)
     return w.data_ptr(), _dtype(w.dtype)
 
 
 def rmsnorm(x, weight, residual=None, eps=1e-6, output=None):
     """(y, s, rstd) of the root-mean-square norm of the rows of s = x + residual (s = x without one).  y has x's type or, with
-    output="fp8", is an MxTensor for the product behind it; s and rstd are what rmsnorm_backward takes."""
+    output="fp8", is an MxTensor for the product behind it; s and rstd are what rmsnorm_backward takes (autograd records nothing)."""
     dev, kind, rows, d, pitch = _matrix(x, "rmsnorm")
     if output is not None and output != "fp8":
         _refuse("rmsnorm: the output is None (x's type) or 'fp8'")

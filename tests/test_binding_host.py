@@ -175,3 +175,25 @@ def test_a_step_raises_the_version_counters(optimizer):
     opt.step([torch.ones(n) for n in (3, 0, 5)], 0.1)
     assert all(t._version > b for t, b in zip(watched, before))
     opt.close()
+
+
+def test_inputs_whose_gradient_would_be_lost_are_named(optimizer):
+    """The operators record no graph: a tensor that requires a gradient is taken with a warning, and without one where no graph is wanted."""
+    import warnings
+    torch, _, _ = optimizer
+
+    class Matrix(torch.nn.Parameter):
+        is_cuda = True
+    x, w = Matrix(torch.ones(4, 6)), Matrix(torch.ones(6))
+    plain = Matrix(torch.ones(4, 6), requires_grad=False)
+    for call in (lambda: ssgd._matrix(x, "an operator"), lambda: ssgd._weight(w, plain, "an operator"), lambda: ssgd._beside(x, plain, "an operator")):
+        with pytest.warns(UserWarning, match="an operator.*no graph"):
+            call()
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            with torch.no_grad():
+                call()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        ssgd._matrix(plain, "an operator")
+        ssgd._weight(w.detach(), plain, "an operator")
