@@ -561,11 +561,26 @@ bool sizes_ok(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
     return format_ok(a_fmt) && M >= 0 && N >= 0 && K >= 0 && M < kMostRows && N < kMostRows && K <= kMostCols;
 }
 
-const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, const void* out, int32_t out_dtype, int64_t out_pitch) {
+// Threads of the product's launch.
+int64_t threads_of(int32_t a_fmt, int64_t M, int64_t N, int64_t K, bool itself) {
+    const int64_t steps = mx_padded(K) / kMxPad;
+    if (itself) return (N + 15) / 16 * (64 * kRowWaves);
+    if (takes_few_rows(a_fmt, M, N, steps)) {
+        const int64_t columns = pairs_of(N) ? 32 : 16;
+        return (N + columns - 1) / columns * (steps <= kAhead ? 64 : 64 * kRowWaves);
+    }
+    const int rows = tiling_of(a_fmt, M, N, steps).rows, across = rows == 256 ? 256 : 128;
+    return ((M + rows - 1) / rows * ((N + across - 1) / across) + kXcds - 1) / kXcds * kXcds * (rows == 256 ? 512 : 256);
+}
+
+// `itself`: the product quantises its rows.
+const char* refused(int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K, const void* out, int32_t out_dtype, int64_t out_pitch, bool itself) {
     if (!format_ok(a_fmt) || !dtype_ok(out_dtype)) return "mx product: a format and an output type of the enumerations";
     if (!sizes_ok(a_fmt, M, N, K) || out_pitch < N) return "mx product: M and N from zero to 2^31, K to 2^24 - 128, pitch >= N";
     if (M == 0 || N == 0) return nullptr;
-    if ((M + 127) / 128 * ((N + 127) / 128) > kMostBlocks) return "mx product: too many results";
+    // (a launch ends at 2^32 threads; what it has follows from the kernel, and is in question only where there are many results)
+    const int64_t tiles = (M + 127) / 128 * ((N + 127) / 128);
+    if (tiles > kMostBlocks || (K > 0 && tiles > kMostBlocks / 16 && threads_of(a_fmt, M, N, K, itself) >> 32 != 0)) return "mx product: too many results";
     if (K > 0 && (!b_values || !b_scales || !aligned(b_values, 16) || !aligned(b_scales, 16))) return "mx product: values and scales are 16-byte aligned arrays";
     if (!out || !aligned(out, (uintptr_t)dtype_bytes(out_dtype))) return "mx product: the output is null or misaligned";
     return nullptr;
@@ -581,7 +596,7 @@ int64_t ssgd_mx_matmul_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K
 ssgd_status ssgd_mx_matmul(const void* a_values, const void* a_scales, int32_t a_fmt, int64_t M, const void* b_values, const void* b_scales, int64_t N, int64_t K,
                            void* out, int32_t out_dtype, int64_t out_pitch, void* work, void* hip_stream) {
     return op_entry([&]() -> ssgd_status {
-        if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch)) return op_fail(SSGD_EINVAL, why);
+        if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch, false)) return op_fail(SSGD_EINVAL, why);
         if (M == 0 || N == 0) return SSGD_OK;
         if (K > 0 && (!a_values || !a_scales || !aligned(a_values, 16) || !aligned(a_scales, 16))) return op_fail(SSGD_EINVAL, "mx product: values and scales are 16-byte aligned arrays");
         if ((!work || !aligned(work, 16)) && parts_bytes(a_fmt, M, N, K) > 0) return op_fail(SSGD_EINVAL, "mx product: a 16-byte aligned work area");
@@ -599,11 +614,12 @@ int64_t ssgd_mx_linear_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K
 ssgd_status ssgd_mx_linear(const void* x, int32_t dtype, int64_t pitch, int64_t M, int32_t a_fmt, const void* b_values, const void* b_scales, int64_t N, int64_t K,
                            void* out, int32_t out_dtype, int64_t out_pitch, void* work, void* hip_stream) {
     return op_entry([&]() -> ssgd_status {
-        if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch)) return op_fail(SSGD_EINVAL, why);
+        const bool itself = sizes_ok(a_fmt, M, N, K) && quantises_itself(a_fmt, M, K);
+        if (const char* why = refused(a_fmt, M, b_values, b_scales, N, K, out, out_dtype, out_pitch, itself)) return op_fail(SSGD_EINVAL, why);
         if (M == 0 || N == 0) return SSGD_OK;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (K == 0) return zeros(M, N, out, out_dtype, out_pitch, stream);
-        if (quantises_itself(a_fmt, M, K)) {
+        if (itself) {
             if (!dtype_ok(dtype) || pitch < K) return op_fail(SSGD_EINVAL, "mx linear: a type of the enumeration, pitch >= K");
             if (!x || !aligned(x, (uintptr_t)dtype_bytes(dtype))) return op_fail(SSGD_EINVAL, "mx linear: the rows are null or misaligned");
             const Product p = product_of(nullptr, nullptr, a_fmt, M, b_values, b_scales, N, K, out, out_pitch);

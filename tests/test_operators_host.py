@@ -152,3 +152,11 @@ def test_rmsnorm_work_floats(L):
         floats = L.ssgd_rmsnorm_work_floats(rows, d)
         assert floats % d == 0 and 1 <= floats // d <= min(rows, 1024)
     assert L.ssgd_rmsnorm_work_floats(-1, 100) == -1 and L.ssgd_rmsnorm_work_floats(1, 0) == -1
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1 << 28, 1000), (2, 1 << 27, 513), (1, 1 << 28, 100000), (16, 1 << 28, 1000), (10, (1 << 28) + 1, 640), (3, 1 << 29, 513)])
+def test_mx_products_refuse_more_workgroups_than_a_launch_has(L, M, N, K):
+    """Few rows of A and very many of B: a workgroup of 512 per 16 or 32 rows of B, and a launch has less than 2^32 threads."""
+    _refused(L, L.ssgd_mx_linear(A, 0, K, M, 1, A, A, N, K, A, 0, N, A, None), b"too many")
+    if N >= 1 << 28:
+        _refused(L, L.ssgd_mx_matmul(A, A, 1, M, A, A, N, K, A, 0, N, A, None), b"too many")
