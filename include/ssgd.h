@@ -278,7 +278,7 @@ ssgd_status ssgd_mx_dequantize(const void *values, const void *scales, int32_t f
  * ssgd_mx_quantize lays them out; out M x N in out_dtype, rows out_pitch elements apart.  Accumulated in fp32 in a fixed order and
  * rounded once.  (The matrix unit adds 4-bit products exactly; of products of 8 by 4 bits it drops what is below about 2^-14 of the
  * largest of 128, an error of 4e-6 of a typical result.)  A block that is NaN makes the results that use it NaN.  K = 0 gives zeros; K is at most 2^24 - 128.
- * M and N are below 2^31, and refused too where a launch would need 2^32 threads: 2^23 tiles of 128 x 128 results, and for up to 64 rows of A N from
+ * M and N are below 2^31, and refused too where a launch would need 2^32 threads: 2^23 tiles of 128 x 128 results, and for up to 16 rows of A N from
  * 2^27 (rows quantised on the way) or 2^28 on.
  * work: ssgd_mx_matmul_work_bytes bytes, 16-byte aligned (zero for most shapes: it holds the parts of a long contraction with few results). */
 int64_t ssgd_mx_matmul_work_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K);
@@ -327,8 +327,8 @@ ssgd_status ssgd_rmsnorm_backward(const void *dy, int64_t dy_pitch, const void *
 typedef struct ssgd_adamw ssgd_adamw; /* opaque, library-owned */
 typedef struct {
     double beta1, beta2; /* in [0, 1) */
-    double eps;          /* > 0 */
-    double max_norm;     /* >= 0; 0: no clipping */
+    double eps;          /* > 0, an fp32 number too */
+    double max_norm;     /* >= 0; 0: no clipping; one above 0 is not 0 in fp32 */
     int32_t state_bits;  /* 32 or 8 */
     uint64_t seed;       /* of the stochastic rounding */
 } ssgd_adamw_options;

@@ -267,8 +267,11 @@ ssgd_status ssgd_adamw_create(int32_t tensors, const int64_t* sizes, float* cons
         const int64_t total = ssgd_adamw_state_elements(tensors, sizes);
         if (total < 0) return op_fail(SSGD_EINVAL, "adamw: at least one tensor, sizes of zero or more");
         const ssgd_adamw_options o = *options;
-        if (!unit(o.beta1) || !unit(o.beta2) || !(o.eps > 0) || !std::isfinite(o.eps) || !(o.max_norm >= 0) || (o.state_bits != 8 && o.state_bits != 32))
-            return op_fail(SSGD_EINVAL, "adamw: betas in [0, 1), eps > 0, max_norm >= 0, state_bits 8 or 32");
+        // (as the update has them, in fp32)
+        const float eps = (float)o.eps, max_norm = (float)o.max_norm;
+        if (!unit(o.beta1) || !unit(o.beta2) || !(eps > 0) || !std::isfinite(eps) || !(o.max_norm >= 0) || (max_norm == 0 && o.max_norm > 0) ||
+            (o.state_bits != 8 && o.state_bits != 32))
+            return op_fail(SSGD_EINVAL, "adamw: betas in [0, 1), eps > 0 and max_norm >= 0 as fp32 numbers, state_bits 8 or 32");
         if (total > 0 && (!m || !v || !aligned(m, 16) || !aligned(v, 16))) return op_fail(SSGD_EINVAL, "adamw: m and v must be 16-byte aligned device arrays");
         if (total > 0 && o.state_bits == 8 && (!m_scale || !v_scale)) return op_fail(SSGD_EINVAL, "adamw: 8-bit moments need m_scale and v_scale");
         const int64_t piece = total < kFewElements ? kSmallPiece : kPiece;

@@ -160,3 +160,12 @@ def test_mx_products_refuse_more_workgroups_than_a_launch_has(L, M, N, K):
     _refused(L, L.ssgd_mx_linear(A, 0, K, M, 1, A, A, N, K, A, 0, N, A, None), b"too many")
     if N >= 1 << 28:
         _refused(L, L.ssgd_mx_matmul(A, A, 1, M, A, A, N, K, A, 0, N, A, None), b"too many")
+
+
+@pytest.mark.parametrize("bad", [dict(eps=1e-50), dict(eps=1e39), dict(max_norm=1e-50)])
+def test_adamw_refuses_what_fp32_does_not_hold(L, bad):
+    """The update is in fp32: an eps or a norm to clip to that becomes zero there would divide by zero, or not clip at all."""
+    o = ssgd.AdamWOptions(0.9, 0.999, bad.get("eps", 1e-8), bad.get("max_norm", 0.0), 32, 0)
+    P, h = C.c_void_p * 1, C.c_void_p(0x1234)
+    _refused(L, L.ssgd_adamw_create(1, (C.c_int64 * 1)(100), P(A), P(None), (C.c_double * 1)(0.1), C.byref(o), A, A, None, None, C.byref(h)), b"adamw")
+    assert h.value == 0x1234
