@@ -296,7 +296,8 @@ ssgd_status ssgd_mx_linear(const void *x, int32_t dtype, int64_t pitch, int64_t 
  *   s = x + residual (rounded to dtype; without a residual s = x),  rstd = (mean of s^2 + eps)^(-1/2),  y = s rstd weight
  * x, residual, sum and y have `dtype`, weight weight_dtype (d contiguous elements).  sum receives s and may be x or residual itself (same pitch); it
  * is given exactly when a residual is.  Output: either y, or values and scales (16-byte aligned), the rows quantised to SSGD_MX_FP8 (without
- * a rounding to dtype in between).  rstd (fp32, one per row) is for the backward pass.  1 <= d < 2^25; sums in fp32 and fp64. */
+ * a rounding to dtype in between).  rstd (fp32, one per row) is for the backward pass.  1 <= d < 2^25; sums in fp32 and fp64, for
+ * all values of the types (squares that fp32 does not hold are taken in fp64). */
 ssgd_status ssgd_rmsnorm(const void *x, int64_t x_pitch, const void *residual, int64_t residual_pitch, const void *weight, int32_t dtype,
                          int32_t weight_dtype, int64_t rows, int64_t d, double eps, void *sum, int64_t sum_pitch, void *y, int64_t y_pitch,
                          void *values, void *scales, float *rstd, void *hip_stream);

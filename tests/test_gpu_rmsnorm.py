@@ -246,3 +246,40 @@ def test_refusals(env):
         with pytest.raises(ssgd.SsgdError) as e:
             call()
         assert e.value.status == ssgd.EINVAL
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("d", [5, 400, 900, 1900, 4000, 8000, 16000, 17000])
+def test_rows_whose_squares_fp32_does_not_hold(env, d, dtype, residual):
+    """Rows from 1e-30 to 3e37 beside ordinary ones, eps from nothing to past fp32: s^2 leaves fp32 on both sides, rstd and y do not."""
+    torch, ssgd = env
+    dt = getattr(torch, dtype)
+    levels = torch.tensor([1.0, 1e25, 1e-25, 3e19, 1e-30, 3e37, 2.0, 1e20, 1e-20, 0.0])[:, None].cuda()
+    g = torch.Generator().manual_seed(d)
+    x = ((0.5 + torch.rand(10, d, generator=g)) * torch.randn(10, d, generator=g).sign()).cuda()
+    r = (x * 0.5 * levels).to(dt) if residual else None
+    x = (x * levels).to(dt)
+    w = (1 + 0.2 * torch.randn(d, generator=g)).cuda()
+    dy = torch.randn(10, d, generator=g).to(dt).cuda()
+    total = x if r is None else (x.float() + r.float()).to(dt)
+    for eps in (1e-6, 1e-50, 1e39):
+        y, s, rstd = ssgd.rmsnorm(x, w, residual=r, eps=eps)
+        assert torch.equal(s, total)
+        h = _host(total)
+        rs = 1 / np.sqrt((h * h).mean(1) + eps)
+        # 16 terms at most in fp32, a root and a quotient; below the normal numbers 2^-149 is a place
+        assert np.all(np.abs(_host(rstd) - rs) <= 16 * U32 * rs + 2.0 ** -149)
+        yw = h * rs[:, None] * _host(w)
+        assert np.all(np.abs(_host(y) - yw) <= 20 * U32 * np.abs(yw) + 1.01 * _half_place(yw, dtype) + np.abs(h * _host(w)) * 2.0 ** -149 + 1e-40)
+        q = ssgd.rmsnorm(x, w, residual=r, eps=eps, output="fp8")[0]
+        back = _host(ssgd.mx_dequantize(q))
+        # half a place of E4M3 at most 2^-4 of a value, and 2^-10 times the scale, 2^-8 of the block's largest value, below its normal numbers; a
+        # block's largest value may be cut off at 448 / 512
+        block = np.abs(np.pad(yw, ((0, 0), (0, -d % 32)))).reshape(10, -1, 32).max(2).repeat(32, 1)[:, :d]
+        assert np.all(np.abs(back - yw) <= (0.125 + 2.0 ** -10) * np.abs(yw) + 2.0 ** -17 * block + np.abs(h * _host(w)) * 2.0 ** -148 + 1e-38)
+        if eps == 1e-6:
+            dx, dw = ssgd.rmsnorm_backward(dy, s, w, rstd)
+            _, _, dxw, dww, size, dwsize = _formulas(h, _host(w), eps, _host(dy), 0.0)
+            assert np.all(np.abs(_host(dx) - dxw) <= 64 * U32 * size + 1.01 * _half_place(dxw, dtype) + 1e-38)
+            assert np.all(np.abs(_host(dw) - dww) <= 24 * U32 * dwsize + np.abs(_host(dy) * h).sum(0) * 2.0 ** -149 + 1e-40)
