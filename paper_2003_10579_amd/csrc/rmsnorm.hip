@@ -247,10 +247,14 @@ __device__ __forceinline__ void store_dx(const Backward& a, int64_t row, int64_t
     store_vec<8>(static_cast<T*>(a.dx) + row * a.dx_pitch + col, end - col, dx);
 }
 
-template <typename T, int LANES, int NV>
+// MANY: teams that take more than kChain rows.  After so many, a thread's fp32 sums of dw move to fp64 ones, in LDS (a kernel of its own, since those
+// are up to 128 KB of a CU's and few calls have the rows: more than 64 for each of 256 to 4096 teams).
+constexpr int kChain = 64;
+template <typename T, int LANES, int NV, bool MANY>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Backward a) {
     constexpr int kRows = LANES == 64 ? 4 : 1;
     __shared__ double part[LANES / 64];
+    __shared__ double wide[MANY ? NV * 8 : 1][MANY ? LANES * kRows : 1];
     __shared__ float dw_of[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? LANES * NV * 8 : 1];
     const int lane = threadIdx.x & (LANES - 1), team = threadIdx.x / LANES;
     constexpr bool kShort = LANES == 64 && NV == 1;
@@ -287,8 +291,23 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
         }
     };
     const int64_t first = (int64_t)blockIdx.x * kRows + team, step = a.groups * kRows;
+    // (a thread's own places: no other thread reads or writes them)
+    auto each_sum = [&](auto f) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f(wide[v * 8 + q][threadIdx.x], dw[v][q]);
+    };
+    if constexpr (MANY) each_sum([](double& sum, float&) { sum = 0.0; });
+    int taken = 0;
     if constexpr (kAhead) load(first);
     for (int64_t row = first; row < a.rows; row += step) {
+        if constexpr (MANY) {
+            if (taken++ == kChain) {
+                each_sum([](double& sum, float& x) { sum += x; x = 0.0f; });
+                taken = 1;
+            }
+        }
         if constexpr (!kAhead) load(row);
         float dy[NV][8], xhat[NV][8];
         const float rstd = next_rstd;
@@ -320,6 +339,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
         }
     }
     if (a.partial == nullptr) return;
+    if constexpr (MANY) each_sum([](double& sum, float& x) { x = (float)(sum + x); });
     if constexpr (kRows > 1) {
         // the rows of a workgroup's waves first, in their order
         if (team > 0) {
@@ -345,13 +365,18 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
 }
 
 // The same backward: dy and s twice, and the workgroup's partial sum of dw read and written for every row (2048 x 20000 in bf16: 153 us, 2.1 TB/s of
-// what has to be moved).
+// what has to be moved).  Behind the partial sums lie fp64 ones, where there are more than kChain rows to a workgroup: every kChain rows they take
+// what the fp32 one holds, and the last row leaves their sum, rounded, in its place.
 template <typename T>
 __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
     __shared__ double part[16];
-    bool first = true;
+    const bool many = a.rows > a.groups * kChain;
+    double* wide = reinterpret_cast<double*>(a.partial + a.groups * a.d) + (int64_t)blockIdx.x * a.d;
+    int taken = 0;
+    bool begun = false;        // the fp64 sums hold something
     for (int64_t row = blockIdx.x; row < a.rows; row += a.groups) {
         const float rstd = a.rstd[row];
+        const bool last = row + a.groups >= a.rows, first = taken == 0, over = many && (last || taken == kChain - 1);
         double sum = 0.0;
         for (int64_t col = threadIdx.x * 8; col < a.d; col += 8192) {
             float dy[8], s[8], w[8];
@@ -381,9 +406,15 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             } else load_vec<8>(to, a.d - col, dw);
 #pragma unroll
             for (int q = 0; q < 8; ++q) dw[q] += dy[q] * s[q];
-            store_vec<8>(to, a.d - col, dw);
+            if (over) {
+                for (int q = 0; q < 8 && col + q < a.d; ++q) {
+                    const double all = (begun ? wide[col + q] : 0.0) + dw[q];
+                    if (last) dw[q] = (float)all; else wide[col + q] = all;
+                }
+            }
+            if (last || !over) store_vec<8>(to, a.d - col, dw);
         }
-        first = false;
+        if (over) { taken = 0; begun = true; } else ++taken;
     }
 }
 
@@ -443,17 +474,20 @@ int64_t groups_for(int64_t rows, int64_t d) {
     return groups < most ? groups : most;
 }
 
-template <typename T>
+// Whether a team takes more rows than it adds in fp32.
+bool many_rows(int64_t rows, int64_t d) { return rows > groups_for(rows, d) * (lanes_for(d) == 64 ? 4 : 1) * kChain; }
+
+template <typename T, bool MANY>
 void launch_backward(const Backward& a, hipStream_t s) {
     const int lanes = lanes_for(a.d);
     const dim3 grid((unsigned)a.groups), group(lanes == 64 ? 256 : lanes);
     if (a.d > kMostKept) hipLaunchKernelGGL((backward_long_kernel<T>), grid, dim3(1024), 0, s, a);
-    else if (a.d <= 512) hipLaunchKernelGGL((backward_kernel<T, 64, 1>), grid, group, 0, s, a);
-    else if (a.d <= 1024) hipLaunchKernelGGL((backward_kernel<T, 64, 2>), grid, group, 0, s, a);
-    else if (a.d <= 2048) hipLaunchKernelGGL((backward_kernel<T, 256, 1>), grid, group, 0, s, a);
-    else if (a.d <= 4096) hipLaunchKernelGGL((backward_kernel<T, 256, 2>), grid, group, 0, s, a);
-    else if (a.d <= 8192) hipLaunchKernelGGL((backward_kernel<T, 1024, 1>), grid, group, 0, s, a);
-    else hipLaunchKernelGGL((backward_kernel<T, 1024, 2>), grid, group, 0, s, a);
+    else if (a.d <= 512) hipLaunchKernelGGL((backward_kernel<T, 64, 1, MANY>), grid, group, 0, s, a);
+    else if (a.d <= 1024) hipLaunchKernelGGL((backward_kernel<T, 64, 2, MANY>), grid, group, 0, s, a);
+    else if (a.d <= 2048) hipLaunchKernelGGL((backward_kernel<T, 256, 1, MANY>), grid, group, 0, s, a);
+    else if (a.d <= 4096) hipLaunchKernelGGL((backward_kernel<T, 256, 2, MANY>), grid, group, 0, s, a);
+    else if (a.d <= 8192) hipLaunchKernelGGL((backward_kernel<T, 1024, 1, MANY>), grid, group, 0, s, a);
+    else hipLaunchKernelGGL((backward_kernel<T, 1024, 2, MANY>), grid, group, 0, s, a);
 }
 
 bool shape_ok(int32_t dtype, int32_t w_dtype, int64_t rows, int64_t d) {
@@ -492,7 +526,11 @@ ssgd_status ssgd_rmsnorm(const void* x, int64_t x_pitch, const void* residual, i
     });
 }
 
-int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d) { return shape_ok(SSGD_F32, SSGD_F32, rows, d) ? groups_for(rows, d) * d : -1; }
+int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d) {
+    if (!shape_ok(SSGD_F32, SSGD_F32, rows, d)) return -1;
+    // (a sum to a workgroup, and where rows are read twice and many, one in fp64 too)
+    return groups_for(rows, d) * d * (d > kMostKept && many_rows(rows, d) ? 3 : 1);
+}
 
 ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* s, int64_t s_pitch, const void* weight, int32_t dtype, int32_t weight_dtype,
                                   const float* rstd, const void* dsum, int64_t dsum_pitch, int64_t rows, int64_t d, void* dx, int64_t dx_pitch, float* dweight,
@@ -511,7 +549,10 @@ ssgd_status ssgd_rmsnorm_backward(const void* dy, int64_t dy_pitch, const void* 
         a.d = (int32_t)d; a.w_bf16 = weight_dtype == SSGD_BF16;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (rows > 0) {
-            if (dtype == SSGD_F32) launch_backward<float>(a, stream); else launch_backward<bf16_t>(a, stream);
+            // (without dw nothing is added up over rows)
+            const bool many = dweight != nullptr && many_rows(rows, d);
+            if (dtype == SSGD_F32) { if (many) launch_backward<float, true>(a, stream); else launch_backward<float, false>(a, stream); }
+            else { if (many) launch_backward<bf16_t, true>(a, stream); else launch_backward<bf16_t, false>(a, stream); }
         }
         ssgd_status st = op_hip(hipGetLastError(), "rmsnorm backward");
         if (st == SSGD_OK && dweight != nullptr) {

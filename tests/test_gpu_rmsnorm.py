@@ -283,3 +283,32 @@ def test_rows_whose_squares_fp32_does_not_hold(env, d, dtype, residual):
             _, _, dxw, dww, size, dwsize = _formulas(h, _host(w), eps, _host(dy), 0.0)
             assert np.all(np.abs(_host(dx) - dxw) <= 64 * U32 * size + 1.01 * _half_place(dxw, dtype) + 1e-38)
             assert np.all(np.abs(_host(dw) - dww) <= 24 * U32 * dwsize + np.abs(_host(dy) * h).sum(0) * 2.0 ** -149 + 1e-40)
+
+
+@pytest.mark.parametrize("dtype,d,teams", [("float32", 20, 4096), ("bfloat16", 20, 4096), ("bfloat16", 600, 3072), ("bfloat16", 1030, 1024), ("bfloat16", 2100, 768),
+                                           ("float32", 4200, 256), ("bfloat16", 4200, 256), ("bfloat16", 9000, 256), ("bfloat16", 17000, 256)])
+def test_gradient_of_the_weight_over_very_many_rows(env, dtype, d, teams):
+    """1200 rows to each team of threads, equal ones, whose products add up in one direction: however many, at most 64 of them are added in fp32 before
+    they join a wider sum."""
+    torch, ssgd = env
+    dt, rows = getattr(torch, dtype), teams * 1200 + 37
+    g = torch.Generator().manual_seed(d)
+    dy, s = ((0.1 + torch.rand(1, d, generator=g)).to(dt).cuda() for _ in range(2))
+    rstd = torch.full((rows,), 0.9, device="cuda")
+    want = rows * _host(dy)[0] * _host(s)[0] * float(rstd[0])
+    _, dw = ssgd.rmsnorm_backward(dy.expand(rows, d).contiguous(), s.expand(rows, d).contiguous(), torch.ones(d, device="cuda"), rstd)
+    # two products, 64 sums, the rounding of a team's sum, those of four teams and the result's
+    assert np.all(np.abs(_host(dw) - want) <= 72 * U32 * want)
+
+
+def test_nothing_is_written_beside_the_work_area_of_many_long_rows(env):
+    torch, ssgd = env
+    L, rows, d = ssgd.lib(), 16500, 16390
+    dy, w, rstd = torch.ones(rows, d, device="cuda", dtype=torch.bfloat16), torch.ones(d, device="cuda"), torch.ones(rows, device="cuda")
+    floats = L.ssgd_rmsnorm_work_floats(rows, d)
+    work, dw, dx = torch.full((floats + 64,), 7.0, device="cuda"), torch.full((d + 64,), 7.0, device="cuda"), torch.empty_like(dy)
+    assert L.ssgd_rmsnorm_backward(dy.data_ptr(), d, dy.data_ptr(), d, w.data_ptr(), 1, 0, rstd.data_ptr(), None, 0, rows, d, dx.data_ptr(), d, dw.data_ptr() + 128,
+                                   work.data_ptr() + 128, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.all(dw[32:32 + d] == rows)
+    for t, n in ((work, floats), (dw, d)):
+        assert torch.all(t[:32] == 7) and torch.all(t[32 + n:] == 7)
