@@ -83,11 +83,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves, kLoads = kLoadsA + kLoadsB;
     static_assert(kLoadsA * 1024 * kWaves == kA && kLoadsB * 1024 * kWaves == kB && BM + BN <= 64 * kWaves, "every wave loads the same share");
     constexpr int kGroupSteps = STAGES == 3 ? 3 : 4;
-    static_assert(STAGES >= 2 && STAGES <= 4, "a group ends at the stage it began with");
+    static_assert(STAGES == 3 || STAGES == 4, "a group ends at the stage it began with");
     // (arrays of their own: the compiler then sees that loads into one do not concern reads of another)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
-    __shared__ __attribute__((aligned(1024))) uint8_t stage2[STAGES > 2 ? kStage : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t stage2[kStage];
     __shared__ __attribute__((aligned(1024))) uint8_t stage3[STAGES > 3 ? kStage : 16];
     __shared__ __attribute__((aligned(1024))) uint8_t scales[64 * kWaves * 16];      // (a row of A or B to a thread, the last ones again where there are more threads)
 
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
         *reinterpret_cast<words4*>(scales + threadIdx.x * 16) = words4{w[0], w[1], w[2], w[3]};
     }
     issue(stage0, 0);
-    if constexpr (STAGES > 2) issue(stage1, 1);
+    issue(stage1, 1);
     if constexpr (STAGES > 3) issue(stage2, 2);
     // A stage is read when its own loads have arrived in every wave, and loaded again only behind the next meeting, when all have read it.
     // The counts are those of the loads issued after it: STAGES - 2 steps, and from the second step of a group on its successor's scales
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
             const int k = f * kGroupSteps;
             wait_and_meet<kFlying>();
             read_scales(first_of(f));
-            issue(STAGES == 2 ? stage1 : (STAGES == 3 ? stage2 : stage3), k + STAGES - 1);
+            issue(STAGES == 3 ? stage2 : stage3, k + STAGES - 1);
             contract(stage0, k0);
             wait_and_meet<kFlying>();
             issue(stage0, k + STAGES);
@@ -209,11 +209,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
             contract(stage1, k1);
             wait_and_meet<kFlying + 1>();
             issue(stage1, k + STAGES + 1);
-            contract(STAGES > 2 ? stage2 : stage0, k2);
-            if constexpr (STAGES != 3) {
-                wait_and_meet<kFlying + (STAGES > 3 ? 1 : 0)>();
-                issue(STAGES > 3 ? stage2 : stage0, k + STAGES + 2);
-                contract(STAGES > 3 ? stage3 : stage1, k3);
+            contract(stage2, k2);
+            if constexpr (STAGES == 4) {
+                wait_and_meet<kFlying + 1>();
+                issue(stage2, k + STAGES + 2);
+                contract(stage3, k3);
             }
         }
     }
@@ -221,24 +221,16 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p) {
     wait_and_meet<0>();
     if (left > 0) {
         read_scales(steps >= 4 ? first_of(whole) : 4 - steps);
-        if constexpr (STAGES > 3) {
+        if constexpr (STAGES == 4) {
             contract(stage0, k0);
             if (left > 1) contract(stage1, k1);
             if (left > 2) contract(stage2, k2);
-        } else if constexpr (STAGES > 2) {
+        } else {
             issue(stage2, done + 2);
             contract(stage0, k0);
             if (left > 1) contract(stage1, k1);
             wait_and_meet<0>();
             if (left > 2) contract(stage2, k2);
-        } else {
-            issue(stage1, done + 1);
-            contract(stage0, k0);
-            wait_and_meet<0>();
-            issue(stage0, done + 2);
-            if (left > 1) contract(stage1, k1);
-            wait_and_meet<0>();
-            if (left > 2) contract(stage0, k2);
         }
     }
     // (the last meeting has seen every load arrive: nothing is on its way into LDS when the workgroup ends)
@@ -490,7 +482,8 @@ int64_t parts_bytes(int32_t a_fmt, int64_t M, int64_t N, int64_t K) {
 
 template <int FA, typename T>
 void tiles_of(int rows, const Product& p, hipStream_t s) {
-    // (stages: as many as LDS holds for two workgroups of a CU, four at most; with 128 rows in 8 bits, 2100 x 1500 x 4001: 30 us with two, 23 with three)
+    // (stages: with 128 rows of B as many as LDS holds for two workgroups of a CU, four at most; 128 rows in 8 bits, 2100 x 1500 x 4001: 30 us with two, 23
+    // with three.  With 256, four or three are 136 and 152 KB, a workgroup to a CU.)
     if (rows == 256) {
         if constexpr (FA == SSGD_MX_FP4) tiles<FA, 256, 256, 2, 4, 4, T>(p, s);
         else tiles<FA, 256, 256, 4, 2, 3, T>(p, s);
