@@ -236,3 +236,85 @@ def test_stored_matrices_in_a_first_call(env, monkeypatch):
         return [ssgd.MxTensor(*q) for q in arrays]
     assert torch.equal(ssgd.mx_matmul(*fresh(), torch.float32), want)
     assert torch.equal(ssgd.mx_dequantize(fresh()[0], torch.bfloat16), back)
+
+
+def _cut(torch, x, offset, pad):
+    """The same rows inside wider ones of NaN."""
+    room = torch.full((x.shape[0], x.shape[1] + pad), float("nan"), dtype=x.dtype, device="cuda")
+    room[:, offset:offset + x.shape[1]] = x
+    return room[:, offset:offset + x.shape[1]]
+
+
+def _same(torch, a, b):
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a, nan=7.0), torch.nan_to_num(b, nan=7.0))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("K", [513, 519, 544, 640, 2999, 8191])
+def test_one_and_two_rows_from_any_place_and_with_any_values(env, K, fmt, dtype):
+    """The product that quantises its rows itself: rows at odd places among NaN, blocks with infinities and NaN (the first, one inside, the last), of zeros,
+    of the smallest and the largest numbers, as quantisation and product one after the other have them."""
+    torch, ssgd = env
+    dt, N = getattr(torch, dtype), 70
+    b = ssgd.mx_quantize(_matrix(torch, N, K, 2).cuda(), "fp4")
+    for M in (1, 2):
+        x = _matrix(torch, M, K, K + M).to(dt).cuda()
+        special = []
+        for at in (0, K // 2, K - 1):
+            for value in (float("inf"), -float("inf"), float("nan")):
+                y = x.clone()
+                y[-1, at] = value
+                special.append(y)
+        y = x.clone(); y[0, :300] = 0.0; special.append(y)
+        special += [torch.zeros_like(x), x * 1e-38, x.sign() * 3e38, x * 2.0 ** -133]
+        for y in [x] + special:
+            want = ssgd.mx_matmul(ssgd.mx_quantize(y, fmt), b, torch.float32)
+            assert _same(torch, ssgd.mx_linear(y, b, fmt, torch.float32), want)
+            for offset, pad in ((1, 3), (3, 7), (8, 8)):
+                assert _same(torch, ssgd.mx_linear(_cut(torch, y, offset, pad), b, fmt, torch.float32), want)
+        assert all(torch.isnan(ssgd.mx_linear(y, b, fmt)[-1]).all() for y in special[:9])
+        if M == 2:
+            assert not any(torch.isnan(ssgd.mx_linear(y, b, fmt)[0]).any() for y in special[:9])
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("M", [3, 16, 17, 40, 64, 70, 300])
+def test_rows_from_any_place(env, M, fmt):
+    torch, ssgd = env
+    for N, K in ((70, 200), (5200, 700), (300, 5000)):
+        b, x = ssgd.mx_quantize(_matrix(torch, N, K, 2).cuda(), "fp4"), _matrix(torch, M, K, 3).cuda()
+        for dt in (torch.float32, torch.bfloat16):
+            y = x.to(dt)
+            want = ssgd.mx_matmul(ssgd.mx_quantize(y, fmt), b, dt)
+            for offset, pad in ((1, 3), (3, 7), (8, 8)):
+                assert torch.equal(ssgd.mx_linear(_cut(torch, y, offset, pad), b, fmt), want)
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("kind", [0, 1])
+def test_strided_and_misaligned_outputs_whole(env, fmt, kind):
+    """Every row of an output whose rows lie apart and begin anywhere, in both types, through the C entries of the product and of the layer."""
+    torch, ssgd = env
+    L, dt, name = ssgd.lib(), (torch.float32, torch.bfloat16)[kind], ("fp4", "fp8")[fmt]
+    stream = torch.cuda.current_stream().cuda_stream
+    for M, N, K in ((1, 37, 200), (1, 37, 700), (2, 5125, 700), (16, 130, 700), (30, 5201, 700), (50, 130, 700), (64, 5201, 1300), (140, 135, 300), (140, 135, 5000), (300, 517, 900),
+                    (1100, 1205, 300), (3500, 3601, 130)):
+        x = _matrix(torch, M, K, 1).cuda()
+        a, b = ssgd.mx_quantize(x, name), ssgd.mx_quantize(_matrix(torch, N, K, 2).cuda(), "fp4")
+        want = ssgd.mx_matmul(a, b, dt)
+        work = torch.full((max(L.ssgd_mx_matmul_work_bytes(fmt, M, N, K), L.ssgd_mx_linear_work_bytes(fmt, M, N, K)) // 4 + 8,), float("nan"), device="cuda")
+        for pad, offset in ((0, 0), (8, 4), (5, 1), (3, 2)):
+            for layer in (False, True):
+                room = torch.full((M + 2, N + pad), 7.0, device="cuda", dtype=dt)
+                flat, at = room.reshape(-1), N + pad + offset
+                out = flat.data_ptr() + at * flat.element_size()
+                if layer:
+                    status = L.ssgd_mx_linear(x.data_ptr(), 0, K, M, fmt, b.values.data_ptr(), b.scales.data_ptr(), N, K, out, kind, N + pad, work.data_ptr(), stream)
+                else:
+                    status = L.ssgd_mx_matmul(a.values.data_ptr(), a.scales.data_ptr(), fmt, M, b.values.data_ptr(), b.scales.data_ptr(), N, K, out, kind, N + pad, work.data_ptr(), stream)
+                assert status == 0
+                body = torch.as_strided(flat, (M, N), (N + pad, 1), at)
+                assert torch.equal(body, want), (M, N, K, pad, offset, layer)
+                body.fill_(7.0)
+                assert torch.all(flat == 7)
