@@ -318,3 +318,18 @@ def test_strided_and_misaligned_outputs_whole(env, fmt, kind):
                 assert torch.equal(body, want), (M, N, K, pad, offset, layer)
                 body.fill_(7.0)
                 assert torch.all(flat == 7)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_the_smallest_and_largest_scales(env, fmt):
+    """Blocks with scale byte 0 (2^-127, from numbers at and below the smallest normal ones) and with the largest one, through every kernel."""
+    torch, ssgd = env
+    for M, N, K in ((1, 40, 256), (1, 40, 1024), (2, 40, 640), (20, 40, 640), (70, 140, 640), (300, 517, 640)):
+        one, other = torch.ones(M, K, device="cuda"), torch.ones(N, K, device="cuda")
+        for low, high in ((-126, 120), (-128, 125), (-128, 127), (-127, 60)):        # (half of 2^-127 is the smallest E2M1 has)
+            small, large = one * 2.0 ** -100 * 2.0 ** (low + 100), ssgd.mx_quantize(other * 2.0 ** high)
+            assert torch.all(small > 0)
+            want = torch.full((M, N), K * 2.0 ** (low + high), device="cuda")
+            q = ssgd.mx_quantize(small, fmt)
+            assert torch.equal(ssgd.mx_matmul(q, large, torch.float32), want) and torch.equal(ssgd.mx_linear(small, large, fmt), want)
+            assert torch.equal(ssgd.mx_matmul(ssgd.mx_quantize(one * 2.0 ** high, fmt), ssgd.mx_quantize(other * 2.0 ** -100 * 2.0 ** (low + 100)), torch.float32), want)
