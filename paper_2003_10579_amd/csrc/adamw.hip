@@ -1,7 +1,7 @@
 // AdamW over many tensors in one launch (two with clipping), moments in 32 or 8 bits.
 //
-// Per element: 28 bytes with fp32 moments and gradients (p, m, v read and written, g read), 14.1 with 8-bit moments and fp32
-// gradients; clipping reads the gradients a second time.  About 20 operations an element: bound by memory.  Tensors are cut
+// Per element: 28 bytes with fp32 moments and gradients (p, m, v read and written, g read), 16.1 with 8-bit moments and fp32
+// gradients, 14.1 with bf16 ones; clipping reads the gradients a second time.  About 20 operations an element: bound by memory.  Tensors are cut
 // into pieces of 8192 elements, a workgroup each, from a table made with the handle; what changes from call to call, the
 // gradients' addresses, travels in the kernel's arguments, so a step copies nothing and has no host work per piece.
 #include <cmath>
@@ -93,7 +93,7 @@ __device__ __forceinline__ void unpack_fp8(words2 w, float scale, float (&x)[8])
 }
 
 // Sum of squares of the pieces of a launch, in fp64 (fp32 squares overflow from 1.8e19 on), one number per workgroup.  Bound by memory: 268 M bf16
-// gradients 139 us, 3.9 TB/s, behind an update that left the caches full of lines to be written back.
+// gradients 138 us, 3.9 TB/s, behind an update that left the caches full of lines to be written back.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void square_kernel(const Piece* pieces, int32_t n_pieces, Grads<G> grads, double* partials) {
     __shared__ double part[kThreads / 64];
@@ -135,7 +135,7 @@ __device__ __forceinline__ float clip_factor(const Rule& rule, double* part) {
     return c > 1.0f ? 1.0f : c;           // (a NaN stays)
 }
 
-// The update.  268 M parameters with bf16 gradients and copy: 1420 us with 32-bit moments (5.3 TB/s), 925 us with 8-bit ones (4.6 TB/s; 820 where no
+// The update.  268 M parameters with bf16 gradients and copy: 1416 us with 32-bit moments (5.3 TB/s), 950 us with 8-bit ones (4.6 TB/s; 820 where no
 // clipping has read the gradients before).  Four elements a thread at a time with 32-bit moments, so that a wave's accesses are whole lines; eight
 // with 8-bit ones, so that sixteen lanes hold a block.
 template <int BITS, typename G>

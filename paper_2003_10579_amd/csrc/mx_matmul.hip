@@ -464,6 +464,9 @@ Tiling tiling_of(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {
 // 16 rows of B to a workgroup of the kernel for few rows, or 32 where they still give as many workgroups as keep the CUs busy: A is then read half as
 // often (61 x 6144 x 5000 in 4 bits: 10.2 us against 15.6; 64 x 2048 x 4096: 9.5 against 8.3).
 bool pairs_of(int64_t N) { return N >= 5120; }
+// Up to 16 rows go through that kernel whatever the contraction: the tiles, which would take them as they take 17, win with more than 8 rows of a very long one
+// only (4096 x 30000, eight and 16 rows: 12.7 and 14.1 us, the tiles 14.9, in 4 bits, 15.9 and 20.2, the tiles 16.5, in 8; 1000 x 30000: 11.2 and 12.9 to 12.0,
+// 14.7 and 19.6 to 14.5).
 // 17 to 64 rows of A through that kernel, by the same kind of model: its steps against those of the tiles, which cost 1.5 us more to begin with.
 // (64 x 8192 x 8192 in 8 bits: 14.7 us through tiles, 23.8 through this; 64 x 6144 x 1500: 7.3 and 6.9.)
 bool takes_few_rows(int32_t a_fmt, int64_t M, int64_t N, int64_t steps) {

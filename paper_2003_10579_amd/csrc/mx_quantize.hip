@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Source s, Target t, int6
     store_block<FMT>(t, row, col, x);
 }
 
-// A tile of 128 x 128 (8192 x 6144 fp32 to 4 bits both ways: 58 us, 4.4 TB/s; 4001 x 2100 bf16 to 8 bits: 12.7 us, 2.7 TB/s, two tiles to a CU).  The
+// A tile of 128 x 128 (8192 x 6144 fp32 to 4 bits both ways: 60 us, 4.2 TB/s; 4001 x 2100 bf16 to 8 bits: 12.7 us, 2.7 TB/s, two tiles to a CU).  The
 // rows of a column's block begin 16 columns further on than those of the block before, so that four lanes on
 // one column and sixteen on the next ones meet in no bank.
 __device__ __forceinline__ int place(int row, int col) { return row * kTile + (row >> 5) * 16 + col; }

@@ -4,8 +4,8 @@
 //   rstd = (mean s^2 + eps)^(-1/2),  y = (s rstd) w
 //   dx = rstd (g - xhat mean(g xhat)) + dsum,  g = dy w,  xhat = s rstd;    dw = sum over rows of dy xhat
 //
-// About 8 operations per element forward, 12 backward: bound by memory (16384 x 4096 in bf16: forward with 8-bit output 89 us, 5.3 TB/s; backward
-// 105 us with its sums over rows, 5.1 TB/s; rows of 999, 8192 of them, 12.8 and 18.8 us).  A row stays in the registers of 64, 256 or 1024 threads, eight
+// About 8 operations per element forward, 12 backward: bound by memory (16384 x 4096 in bf16: forward with 8-bit output 83 us, 5.7 TB/s; backward
+// 107 us and its sums over workgroups 6, 4.8 TB/s in all; rows of 999, 8192 of them, 12.8 and 15.7 us, the latter without dsum).  A row stays in the registers of 64, 256 or 1024 threads, eight
 // or sixteen columns each, between the sum of squares and the output, so it is read once; the threads go on to further rows with
 // their part of w, and backward with their part of dw, kept.  Rows of more than 16384 columns are read a second time instead.
 #include <cmath>

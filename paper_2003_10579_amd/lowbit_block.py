@@ -57,6 +57,8 @@ class Block:
         dw2 = ssgd.mx_matmul(dt, ssgd.mx_quantize_transposed(z, "fp4"), torch.float32)
         dz = ssgd.mx_matmul(dq, self.q2t) * (z > 0)
         dq, dt = ssgd.mx_quantize_both(dz, "fp8", "fp8")
+        # (the activations that the product took: what it used of them in 8 bits is what the weight's gradient is of.  As the right operand they are
+        # rounded once more, to 4 bits)
         dw1 = ssgd.mx_matmul(dt, ssgd.mx_quantize_transposed(ssgd.mx_dequantize(y, torch.bfloat16), "fp4"), torch.float32)
         dx, dgain = ssgd.rmsnorm_backward(ssgd.mx_matmul(dq, self.q1t), s, self.gain, rstd, dsum=dout)
         self.optimizer.step([dgain, dw1, dw2], lr)
