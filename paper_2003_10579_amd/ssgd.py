@@ -422,7 +422,7 @@ class AdamW:
         self.grad_norm = torch.zeros(1, device=dev) if max_norm else None
         self.t = 0
         self._written = params + [c for c in copies if c is not None]
-        self._places = [(p, p.data_ptr()) for p in self._written]
+        self._places = [p.data_ptr() for p in self._written]
         self._device, self._grads = dev, (C.c_void_p * n)()
         pointers = C.c_void_p * n
         o = AdamWOptions(float(betas[0]), float(betas[1]), float(eps), float(max_norm), state_bits, seed)
@@ -441,14 +441,14 @@ class AdamW:
             _refuse("adamw: closed")
         if len(grads) != len(self._sizes):
             _refuse("adamw step: one gradient per tensor")
-        for p, place in self._places:
-            if p.data_ptr() != place:
-                _refuse("adamw step: a parameter or its copy has moved since the optimizer was made")
+        place_of = _torch.Tensor.data_ptr
+        if list(map(place_of, self._written)) != self._places:
+            _refuse("adamw step: a parameter or its copy has moved since the optimizer was made")
         kind, dev, at = grads[0].dtype, self._device, self._grads
-        for k, (g, n) in enumerate(zip(grads, self._sizes)):
-            if not (g.dtype == kind and g.numel() == n and g.device == dev and g.is_contiguous()):
+        for g, n in zip(grads, self._sizes):
+            if not (g.dtype is kind and g.numel() == n and g.device == dev and g.is_contiguous()):
                 _refuse("adamw step: gradients are contiguous tensors of one type, of their parameters' sizes and device")
-            at[k] = g.data_ptr()
+        at[:] = list(map(place_of, grads))
         _call(_lib.ssgd_adamw_step, dev, self.h, at, _dtype(kind), lr, self.t + 1, None if self.grad_norm is None else self.grad_norm.data_ptr())
         _changed(self._written)        # (autograd's check of what it has kept for a backward pass)
         self.t += 1
@@ -495,7 +495,6 @@ class MxTensor:
     __slots__ = ("format", "shape", "device", "_values", "_scales", "_room", "_at")
 
     def __init__(self, values, scales, format, shape):
-        _torch or _load()          # (with stored arrays this may be a program's first call)
         if format not in _FORMATS:
             _refuse("mx: the format is 'fp4' or 'fp8'")
         rows, cols = shape
@@ -504,6 +503,7 @@ class MxTensor:
                 values.element_size() == scales.element_size() == 1 and
                 tuple(values.shape) == (rows, wide // 2 if format == "fp4" else wide) and tuple(scales.shape) == (rows, wide // 32)):
             _refuse(f"mx: values and scales do not have the layout of {rows} x {cols}")
+        _torch or _load()          # (with stored arrays this may be a program's first call)
         self.format, self.shape, self.device, self._room = format, (rows, cols), values.device, None
         self._values, self._scales, self._at = values, scales, (values.data_ptr(), scales.data_ptr())
 

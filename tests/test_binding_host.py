@@ -59,6 +59,15 @@ def test_a_stored_matrix_is_enough_to_begin_with(fresh):
     assert callable(ssgd._raw_stream) and callable(ssgd._device_now)
 
 
+def test_arrays_that_are_no_matrix_are_refused_without_a_gpu(monkeypatch):
+    monkeypatch.setattr(ssgd, "_torch", None)
+    for values, scales, fmt, shape in ((np.zeros((3, 64), np.uint8), np.zeros((3, 3), np.uint8), "fp4", (3, 40)), (np.zeros((3, 64), np.uint8), np.zeros((3, 4), np.uint8), "fp6", (3, 40))):
+        with pytest.raises(ssgd.SsgdError) as e:
+            ssgd.MxTensor(Tensor(values), Tensor(scales), fmt, shape)
+        assert e.value.status == ssgd.EINVAL
+    assert ssgd._torch is None
+
+
 def test_a_copied_matrix_has_its_own_addresses(fresh):
     """Copies, and what is read back from a pickle, point at their own arrays and not where the first ones were."""
     q = _stored()
