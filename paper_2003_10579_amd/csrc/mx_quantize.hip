@@ -113,22 +113,10 @@ __global__ __launch_bounds__(kThreads) void back_kernel(const uint8_t* values, c
     if (g >= groups) return;
     const int64_t row = g / groups_per_row, col = (g - row * groups_per_row) * 8;
     const uint32_t byte = scales[row * scale_bytes + col / kMxBlock];
-    // 2^(byte - 127): a number below the normal ones for byte 0, NaN for 255
-    const float scale = __builtin_bit_cast(float, byte == 255u ? 0x7FC00000u : (byte == 0u ? 0x00400000u : byte << 23));
+    const float scale = mx_scale_value(byte);
     float x[8];
-    if constexpr (FMT == SSGD_MX_FP4) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(values + row * row_bytes + col / 2);
-        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
-        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
-    } else {
-        const words2 w = *reinterpret_cast<const words2*>(values + row * row_bytes + col);
-        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, true);
-        const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, true);
-        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) x[q] *= scale;
+    if constexpr (FMT == SSGD_MX_FP4) mx_unpack_fp4(*reinterpret_cast<const uint32_t*>(values + row * row_bytes + col / 2), scale, x);
+    else mx_unpack_fp8(*reinterpret_cast<const words2*>(values + row * row_bytes + col), scale, x);
     store_vec<8>(out + row * pitch + col, cols - col, x);
 }
 

@@ -1,4 +1,5 @@
-// Shared by the operators of a low-precision training step (adamw.hip, rmsnorm.hip, mx_quantize.hip, mx_matmul.hip).
+// Shared by the operators of a low-precision training step (adamw.hip, rmsnorm.hip, block_norm.hip, mx_quantize.hip, mx_matmul.hip, mx_dense.hip,
+// mx_backward.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -125,6 +126,14 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
     x = umax(x, dpp<kHalfMirror>(x));
     return umax(x, dpp<kMirror>(x));
 }
+__device__ __forceinline__ uint32_t max_of_8(uint32_t x) { x = max_of_4(x); return umax(x, dpp<kHalfMirror>(x)); }
+// Largest of the four lanes with the same place in a row of 16.
+__device__ __forceinline__ uint32_t max_of_rows(uint32_t x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);      // rows 0 and 1, 2 and 3
+    x = umax(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return umax(b[0], b[1]);
+}
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
 __device__ __forceinline__ float wave_sum(float x) {
@@ -172,6 +181,29 @@ __device__ __forceinline__ words2 mx_pack_fp8(const float (&x)[8], uint32_t byte
     lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[0], y[1], s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[2], y[3], s, true);
     hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[4], y[5], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[6], y[7], s, true);
     return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+__device__ __forceinline__ uint32_t mx_pack_fp8(float a, float b, float c, float d, uint32_t byte) {
+    const float s = mx_scale_of(byte), most = __builtin_bit_cast(float, mx_limit(byte));
+    shorts2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __builtin_amdgcn_fmed3f(a, -most, most), __builtin_amdgcn_fmed3f(b, -most, most), s, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __builtin_amdgcn_fmed3f(c, -most, most), __builtin_amdgcn_fmed3f(d, -most, most), s, true);
+    return byte == 255u ? 0u : __builtin_bit_cast(uint32_t, r);
+}
+// 2^(byte - 127) as a number: one below the normal ones for byte 0, NaN for 255.
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte == 255u ? 0x7FC00000u : (byte == 0u ? 0x00400000u : byte << 23)); }
+__device__ __forceinline__ void mx_unpack_fp8(const words2& w, float scale, float (&x)[8]) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.x, true);
+    const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)w.y, true);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] *= scale;
+}
+__device__ __forceinline__ void mx_unpack_fp4(uint32_t w, float scale, float (&x)[8]) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] *= scale;
 }
 // The same from eight bfloat16, two to a word, as they are.
 // (A bit cast of a vector's element reads its first one: copies are taken.)
