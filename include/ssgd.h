@@ -292,6 +292,42 @@ ssgd_status ssgd_mx_linear(const void *x, int32_t dtype, int64_t pitch, int64_t 
                            const void *b_scales, int64_t N, int64_t K, void *out, int32_t out_dtype, int64_t out_pitch, void *work,
                            void *hip_stream);
 
+/* The product with a dense layer's epilogue, or with that of a gated feed-forward block:
+ *   p = A B^T + bias,   out[m][n] = residual + act(p[m][n])      or, gated (N even, no bias, no residual),   out[m][c] = act(p[m][2 c]) p[m][2 c + 1]
+ * so a gated block's B has gate and up rows in turn.  act: none, relu, gelu (x Phi(x), Phi the normal distribution's function to 1e-7) or silu (x / (1 + e^-x)); infinities
+ * and NaN follow the formulas.  In fp32 from the product's sums on, rounded once to the output: out (M x N, gated M x N / 2) in out_dtype, or values and
+ * scales (16-byte aligned), the rows quantised to SSGD_MX_FP8.  p itself goes, where the backward pass wants it, to kept (kept_dtype) or to kept_values
+ * and kept_scales (SSGD_MX_FP8), all nullable.  K = 0: p = bias. */
+typedef enum { SSGD_ACT_NONE = 0, SSGD_ACT_RELU = 1, SSGD_ACT_GELU = 2, SSGD_ACT_SILU = 3 } ssgd_activation;
+typedef struct {
+    int32_t gated, activation;
+    int32_t bias_dtype, residual_dtype, out_dtype, kept_dtype;
+    const void *bias;                            /* nullable, N contiguous elements */
+    const void *residual; int64_t residual_pitch; /* nullable */
+    void *out; int64_t out_pitch; void *values, *scales;
+    void *kept; int64_t kept_pitch; void *kept_values, *kept_scales;
+} ssgd_mx_epilogue;
+/* A: either rows x (M x K, dtype, pitch), quantised to a_fmt on the way, or a_values and a_scales.  Limits as for ssgd_mx_matmul.  The epilogue is read during the call.
+ * work: ssgd_mx_dense_work_bytes bytes, 16-byte aligned (from_rows: A is x; eight_bits: an output or what is kept is in 8 bits). */
+int64_t ssgd_mx_dense_work_bytes(int32_t a_fmt, int32_t from_rows, int32_t eight_bits, int64_t M, int64_t N, int64_t K);
+ssgd_status ssgd_mx_dense(const void *x, int32_t dtype, int64_t pitch, const void *a_values, const void *a_scales, int32_t a_fmt, int64_t M,
+                          const void *b_values, const void *b_scales, int64_t N, int64_t K, const ssgd_mx_epilogue *epilogue, void *work,
+                          void *hip_stream);
+/* What lies between the products of its backward pass.  dy (rows x cols) is the gradient of act(p), or of the gated block's output, and p what the forward pass has
+ * kept (rows x cols, gated rows x 2 cols): a matrix in p_dtype, or p_values and p_scales (SSGD_MX_FP8); neither is needed with SSGD_ACT_NONE, not gated.
+ *   dp = dy act'(p)      gated:   dp[m][2 c] = dy u act'(g),  dp[m][2 c + 1] = dy act(g),   g = p[m][2 c], u = p[m][2 c + 1]      (relu'(0) = 0)
+ * Outputs, each nullable but one: dp quantised along its rows (values, scales in fmt) and along its columns (values_t, scales_t in fmt_t), for the products with the transposed
+ * weight and with the layer's input; act(p), or the gated block's output, along its columns (values_h, scales_h in fmt_h), for the next weight's gradient; dbias
+ * (fp32, not gated), the sum of dp over its rows.  work: ssgd_mx_activation_backward_work_floats floats, 16-byte aligned, used when dbias is given. */
+int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols);
+ssgd_status ssgd_mx_activation_backward(const void *dy, int32_t dtype, int64_t dy_pitch, int64_t rows, int64_t cols, int32_t gated, int32_t activation,
+                                        const void *p, int32_t p_dtype, int64_t p_pitch, const void *p_values, const void *p_scales, int32_t fmt,
+                                        void *values, void *scales, int32_t fmt_t, void *values_t, void *scales_t, int32_t fmt_h, void *values_h,
+                                        void *scales_h, float *dbias, float *work, void *hip_stream);
+/* A microscaled matrix (rows x cols in fmt), quantised again along its columns: the transposed matrix in fmt_t, from the values that the first one stands for. */
+ssgd_status ssgd_mx_transpose(const void *values, const void *scales, int32_t fmt, int64_t rows, int64_t cols, int32_t fmt_t, void *values_t,
+                              void *scales_t, void *hip_stream);
+
 /* Root-mean-square norm of rows of d columns with the residual's addition:
  *   s = x + residual (rounded to dtype; without a residual s = x),  rstd = (mean of s^2 + eps)^(-1/2),  y = s rstd weight
  * x, residual, sum and y have `dtype`, weight weight_dtype (d contiguous elements).  sum receives s and may be x or residual itself (same pitch); it
@@ -309,6 +345,30 @@ int64_t ssgd_rmsnorm_work_floats(int64_t rows, int64_t d);
 ssgd_status ssgd_rmsnorm_backward(const void *dy, int64_t dy_pitch, const void *s, int64_t s_pitch, const void *weight, int32_t dtype,
                                   int32_t weight_dtype, const float *rstd, const void *dsum, int64_t dsum_pitch, int64_t rows, int64_t d,
                                   void *dx, int64_t dx_pitch, float *dweight, float *work, void *hip_stream);
+
+/* What lies between two blocks of a residual stream: the norm behind the first, its gate, the scaled residual, and the norm in front of the second.
+ *   sum = scale s + gate (o rstd_o) post_weight,   rstd_o = (mean of o^2 + eps)^(-1/2)         (rounded to dtype)
+ *   y = sum rstd weight,                          rstd = (mean of sum^2 + eps)^(-1/2)
+ * o, s, sum and y have `dtype`; the weights are d contiguous elements of their own types.  gate (nullable: 1): `gates` rows of d elements of gate_dtype,
+ * gate_pitch apart, each for rows / gates rows of the stream that lie together (one for all: a gate per column; rows % gates == 0).  Output: y, or values and
+ * scales (SSGD_MX_FP8, 16-byte aligned).  The sum is taken in fp64 and rounded once.  rstd_o and rstd (fp32, one per row) are for the backward
+ * pass.  rows < 2^31, 1 <= d < 2^24. */
+ssgd_status ssgd_block_norm(const void *o, int64_t o_pitch, const void *s, int64_t s_pitch, const void *post_weight, int32_t post_dtype,
+                            const void *weight, int32_t weight_dtype, const void *gate, int32_t gate_dtype, int64_t gates, int64_t gate_pitch,
+                            double scale, double eps, int32_t dtype, int64_t rows, int64_t d, void *sum, int64_t sum_pitch, void *y, int64_t y_pitch,
+                            void *values, void *scales, float *rstd_o, float *rstd, void *hip_stream);
+/* Its gradients, from o, sum and both rstd of the forward pass; dsum (nullable): the gradient that reaches the sum past the second norm.
+ *   G = rstd (dy weight - sum rstd mean(dy weight sum rstd)) + dsum,   t = G gate post_weight
+ *   grad_s = scale G,   grad_o = rstd_o (t - o rstd_o mean(t o rstd_o))
+ *   dweight = sum over rows of dy sum rstd,   dpost = sum over rows of G gate o rstd_o,   dgate[g] = sum over its rows of G post_weight o rstd_o
+ * dpost and dweight (fp32, nullable, given together), dgate (fp32, gates x d contiguous, nullable).  work: ssgd_block_norm_work_floats floats (gates: 1 without a
+ * gate), 16-byte aligned, used when dweight is given. */
+int64_t ssgd_block_norm_work_floats(int64_t rows, int64_t d, int64_t gates);
+ssgd_status ssgd_block_norm_backward(const void *dy, int64_t dy_pitch, const void *o, int64_t o_pitch, const void *sum, int64_t sum_pitch,
+                                     const void *post_weight, int32_t post_dtype, const void *weight, int32_t weight_dtype, const void *gate,
+                                     int32_t gate_dtype, int64_t gates, int64_t gate_pitch, double scale, const float *rstd_o, const float *rstd,
+                                     const void *dsum, int64_t dsum_pitch, int32_t dtype, int64_t rows, int64_t d, void *grad_o, int64_t grad_o_pitch,
+                                     void *grad_s, int64_t grad_s_pitch, float *dpost, float *dweight, float *dgate, float *work, void *hip_stream);
 
 /* AdamW over many tensors at once.  For every element, with the gradient g, the update's number t and
  *   g' = g c,   c = min(1, max_norm / (norm + 1e-6)),   norm = (sum of g^2 over all tensors)^(1/2)

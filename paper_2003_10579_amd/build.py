@@ -8,13 +8,16 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libssgd.so")
 SOURCES = ["linear_tile.hip", "linear_tile_lsq.hip", "api.hip", "schedule.hip", "linear.hip", "linear_defer.hip", "full_loss.hip", "full_grad.hip", "mlp.hip", "mc.hip",
-           "adamw.hip", "mx_quantize.hip", "rmsnorm.hip", "mx_matmul.hip"]
-HEADERS = ["common.hpp", "limits.hpp", "rng.hpp", "mlp.hpp", "ops.hpp", "mx_product.hpp", "column_sums.hpp", os.path.join("..", "..", "include", "ssgd.h")]
+           "adamw.hip", "mx_quantize.hip", "rmsnorm.hip", "mx_matmul.hip",
+           "mx_dense.hip", "mx_backward.hip", "block_norm.hip"]
+HEADERS = ["common.hpp", "limits.hpp", "rng.hpp", "mlp.hpp", "ops.hpp", "mx_product.hpp", "activations.hpp", "column_sums.hpp", os.path.join("..", "..", "include", "ssgd.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # event-process arithmetic (clock sums, AdaSync rule) must round like plain IEEE operations
 NO_CONTRACT = {"schedule.hip": ["-ffp-contract=off"], "mc.hip": ["-ffp-contract=off"], "api.hip": ["-ffp-contract=off"],
-               "adamw.hip": ["-ffp-contract=off"]}     # moments in 8 bits are rounded at thresholds
+               "adamw.hip": ["-ffp-contract=off"],     # moments in 8 bits are rounded at thresholds
+               # an epilogue gives the same bits in every kernel that it is a part of (its sums of products are written as such)
+               "mx_dense.hip": ["-ffp-contract=off"], "mx_backward.hip": ["-ffp-contract=off"]}
 
 
 def hipcc() -> str:

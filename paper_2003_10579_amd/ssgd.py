@@ -19,6 +19,8 @@ _VARIANTS = {"k_sync": K_SYNC, "k_batch_sync": K_BATCH_SYNC, "k_async": K_ASYNC,
 F32, BF16 = 0, 1
 MX_FP4, MX_FP8 = 0, 1
 _FORMATS = {"fp4": MX_FP4, "fp8": MX_FP8}
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+_ACTIVATIONS = {None: ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
 _KINDS = {"lsq": LSQ, "softmax": SOFTMAX, "mlp2": MLP2}
 
 EXPORTS = [
@@ -30,7 +32,9 @@ EXPORTS = [
     "ssgd_last_kernel_ms", "ssgd_adamw_state_elements", "ssgd_adamw_create", "ssgd_adamw_step", "ssgd_adamw_destroy",
     "ssgd_mx_row_bytes", "ssgd_mx_quantize", "ssgd_mx_dequantize",
     "ssgd_mx_matmul_work_bytes", "ssgd_mx_matmul", "ssgd_mx_linear_work_bytes", "ssgd_mx_linear",
+    "ssgd_mx_dense_work_bytes", "ssgd_mx_dense", "ssgd_mx_activation_backward_work_floats", "ssgd_mx_activation_backward", "ssgd_mx_transpose",
     "ssgd_rmsnorm", "ssgd_rmsnorm_work_floats", "ssgd_rmsnorm_backward",
+    "ssgd_block_norm", "ssgd_block_norm_work_floats", "ssgd_block_norm_backward",
     "ssgd_destroy",
 ]
 
@@ -59,6 +63,13 @@ class AdaSync(C.Structure):
 class AdamWOptions(C.Structure):
     _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("max_norm", C.c_double),
                 ("state_bits", C.c_int32), ("seed", C.c_uint64)]
+
+
+class MxEpilogue(C.Structure):
+    _fields_ = [("gated", C.c_int32), ("activation", C.c_int32), ("bias_dtype", C.c_int32), ("residual_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("kept_dtype", C.c_int32), ("bias", C.c_void_p), ("residual", C.c_void_p), ("residual_pitch", C.c_int64), ("out", C.c_void_p),
+                ("out_pitch", C.c_int64), ("values", C.c_void_p), ("scales", C.c_void_p), ("kept", C.c_void_p), ("kept_pitch", C.c_int64),
+                ("kept_values", C.c_void_p), ("kept_scales", C.c_void_p)]
 
 
 _lib = None
@@ -132,6 +143,19 @@ def lib():
         L.ssgd_mx_linear_work_bytes.restype = i64
         L.ssgd_mx_linear_work_bytes.argtypes = [i32, i64, i64, i64]
         L.ssgd_mx_linear.argtypes = [ptr, i32, i64, i64, i32, ptr, ptr, i64, i64, ptr, i32, i64, ptr, ptr]
+        L.ssgd_mx_dense_work_bytes.restype = i64
+        L.ssgd_mx_dense_work_bytes.argtypes = [i32, i32, i32, i64, i64, i64]
+        L.ssgd_mx_dense.argtypes = [ptr, i32, i64, ptr, ptr, i32, i64, ptr, ptr, i64, i64, C.POINTER(MxEpilogue), ptr, ptr]
+        L.ssgd_mx_activation_backward_work_floats.restype = i64
+        L.ssgd_mx_activation_backward_work_floats.argtypes = [i64, i64]
+        L.ssgd_mx_activation_backward.argtypes = [ptr, i32, i64, i64, i64, i32, i32, ptr, i32, i64, ptr, ptr] + [i32, ptr, ptr] * 3 + [ptr, ptr, ptr]
+        L.ssgd_mx_transpose.argtypes = [ptr, ptr, i32, i64, i64, i32, ptr, ptr, ptr]
+        L.ssgd_block_norm.argtypes = ([ptr, i64, ptr, i64, ptr, i32, ptr, i32, ptr, i32, i64, i64, C.c_double, C.c_double, i32, i64, i64, ptr, i64, ptr, i64] +
+                                      [ptr] * 5)
+        L.ssgd_block_norm_work_floats.restype = i64
+        L.ssgd_block_norm_work_floats.argtypes = [i64, i64, i64]
+        L.ssgd_block_norm_backward.argtypes = ([ptr, i64, ptr, i64, ptr, i64, ptr, i32, ptr, i32, ptr, i32, i64, i64, C.c_double, ptr, ptr, ptr, i64, i32, i64, i64,
+                                                ptr, i64, ptr, i64] + [ptr] * 5)
         L.ssgd_rmsnorm.argtypes = [ptr, i64, ptr, i64, ptr, i32, i32, i64, i64, C.c_double, ptr, i64, ptr, i64, ptr, ptr, ptr, ptr]
         L.ssgd_rmsnorm_work_floats.restype = i64
         L.ssgd_rmsnorm_work_floats.argtypes = [i64, i64]
@@ -670,3 +694,197 @@ def rmsnorm_backward(dy, s, weight, rstd, dsum=None):
     _call(_lib.ssgd_rmsnorm_backward, dev, dy.data_ptr(), pitch, s_at, s_pitch, w, kind, w_kind, rstd.data_ptr(), more, more_pitch, rows, d, dx.data_ptr(), d,
           dw.data_ptr(), work.data_ptr())
     return dx, dw
+
+
+# ---- a gated feed-forward block in few bits: what lies between its products ---------------------------------------------------------------------------
+
+def _activation(name, what):
+    kind = _ACTIVATIONS.get(name)
+    return _refuse(f"{what}: the activation is None, 'relu', 'gelu' or 'silu'") if kind is None else kind
+
+
+def _epilogue(what, x, w, gated, activation, bias, residual, format, dtype, output, keep):
+    if isinstance(x, MxTensor):
+        (M, K), dev, f = x.shape, x.device, _FORMATS[x.format]
+        rows, kind, like = (None, 0, 0, *x._at), BF16, _torch.bfloat16
+    else:
+        dev, kind, M, K, pitch = _matrix(x, what)
+        if format not in _FORMATS:
+            _refuse(f"{what}: the format is 'fp4' or 'fp8'")
+        f, rows, like = _FORMATS[format], (x.data_ptr(), kind, pitch, None, None), x.dtype
+    if not (isinstance(w, MxTensor) and w.format == "fp4" and w.shape[1] == K and w.device == dev):
+        _refuse(f"{what}: w is an 'fp4' MxTensor with x's columns, on its device")
+    N = w.shape[0]
+    if gated and N % 2:
+        _refuse(f"{what}: w has gate and up rows in turn")
+    if dtype is not None:
+        kind, like = _dtype(dtype), dtype
+    if output is not None and output != "fp8":
+        _refuse(f"{what}: the output is None (a matrix) or 'fp8'")
+    if keep is not None and keep != "same" and keep != "fp8":
+        _refuse(f"{what}: what is kept is None, 'same' (a matrix of the output's type) or 'fp8'")
+    e = MxEpilogue(gated, _activation(activation, what))
+    if bias is not None:
+        if not (bias.dim() == 1 and bias.numel() == N and bias.is_contiguous() and bias.device == dev):
+            _refuse(f"{what}: a contiguous bias per output is wanted")
+        if bias.requires_grad and _torch.is_grad_enabled():
+            _unrecorded(what)
+        e.bias, e.bias_dtype = bias.data_ptr(), _dtype(bias.dtype)
+    if residual is not None:
+        if residual.shape != (M, N) or residual.device != dev:
+            _refuse(f"{what}: a residual of the output's shape, on its device, is wanted")
+        _, e.residual_dtype, _, _, e.residual_pitch = _matrix(residual, what)
+        e.residual = residual.data_ptr()
+    results = N // 2 if gated else N
+    if output is None:
+        out = _torch.empty(M, results, dtype=like, device=dev)
+        e.out, e.out_pitch, e.out_dtype = out.data_ptr(), results, kind
+    else:
+        out = MxTensor.empty(M, results, "fp8", dev)
+        e.values, e.scales = out._at
+    if keep is not None:
+        if keep == "fp8":
+            kept = MxTensor.empty(M, N, "fp8", dev)
+            e.kept_values, e.kept_scales = kept._at
+        else:
+            kept = _torch.empty(M, N, dtype=like, device=dev)
+            e.kept, e.kept_pitch, e.kept_dtype = kept.data_ptr(), N, kind
+    work = _work(_lib.ssgd_mx_dense_work_bytes(f, rows[0] is not None, output is not None or keep == "fp8", M, N, K), dev)
+    _call(_lib.ssgd_mx_dense, dev, *rows, f, M, *w._at, N, K, e, None if work is None else work.data_ptr())
+    return out if keep is None else (out, kept)
+
+
+def mx_dense(x, w, bias=None, activation=None, residual=None, format="fp8", dtype=None, output=None, keep=None):
+    """residual + act(x w^T + bias) in one pass, for an MxTensor x or rows (float32 or bfloat16) that are quantised to `format` on the way, and an "fp4"
+    MxTensor w (outputs x inputs).  activation: None, "relu", "gelu" or "silu".  The result is a matrix of `dtype` (x's unless it is given, bfloat16 for an
+    MxTensor) or, with output="fp8", an MxTensor for the product behind it.  keep="same" (a matrix of dtype) or "fp8" (an MxTensor, a checkpoint in 8 bits)
+    gives (result, x w^T + bias): what mx_dense_backward takes.  Autograd records nothing."""
+    return _epilogue("mx_dense", x, w, 0, activation, bias, residual, format, dtype, output, keep)
+
+
+def gate_up(gate, up):
+    """The weight of mx_gated from those of both projections (hidden x inputs each): their rows in turn."""
+    if gate.dim() != 2 or gate.shape != up.shape or gate.dtype != up.dtype or gate.device != up.device:
+        _refuse("gate_up: two matrices of one shape, type and device are wanted")
+    import torch
+    return torch.stack((gate, up), 1).flatten(0, 1)
+
+
+def mx_gated(x, w, activation="silu", format="fp8", dtype=None, output=None, keep=None):
+    """Both projections of a gated feed-forward block, its activation and their product in one pass: h[:, c] = act(p[:, 2 c]) p[:, 2 c + 1] with
+    p = x w^T, w an "fp4" MxTensor whose rows are gate and up in turn (gate_up).  The other arguments, and (h, p), as for mx_dense; p is what
+    mx_gated_backward takes."""
+    return _epilogue("mx_gated", x, w, 1, activation, None, None, format, dtype, output, keep)
+
+
+def _activation_backward(what, dy, p, gated, activation, hidden, format, format_transposed, bias):
+    dev, kind, rows, cols, pitch = _matrix(dy, what)
+    act = _activation(activation, what)
+    wide = 2 * cols if gated else cols
+    if p is None and not gated and act == ACT_NONE and hidden is None:
+        kept = (None, 0, 0, None, None)
+    elif isinstance(p, MxTensor):
+        if p.format != "fp8" or p.shape != (rows, wide) or p.device != dev:
+            _refuse(f"{what}: what the forward pass has kept is wanted")
+        kept = (None, 0, 0, *p._at)
+    else:
+        if p is None or p.shape != (rows, wide) or p.device != dev:
+            _refuse(f"{what}: what the forward pass has kept is wanted")
+        _, p_kind, _, _, p_pitch = _matrix(p, what)
+        kept = (p.data_ptr(), p_kind, p_pitch, None, None)
+    q, t = MxTensor.empty(rows, wide, format, dev), MxTensor.empty(wide, rows, format_transposed, dev)
+    h = None if hidden is None else MxTensor.empty(cols, rows, hidden, dev)
+    db = work = None
+    if bias:
+        floats = _lib.ssgd_mx_activation_backward_work_floats(rows, cols)
+        if floats < 0:
+            _refuse(f"{what}: less than 2^25 columns")
+        db, work = _torch.empty(cols, dtype=_torch.float32, device=dev), _torch.empty(floats, dtype=_torch.float32, device=dev)
+    _call(_lib.ssgd_mx_activation_backward, dev, dy.data_ptr(), kind, pitch, rows, cols, gated, act, *kept, _FORMATS[format], *q._at, _FORMATS[format_transposed], *t._at,
+          *((0, None, None) if h is None else (_FORMATS[hidden], *h._at)), *((None, None) if db is None else (db.data_ptr(), work.data_ptr())))
+    return q, t, h, db
+
+
+def mx_dense_backward(dy, p, activation=None, hidden=None, format="fp8", format_transposed="fp8", bias=True):
+    """(d, dt, ht, dbias) from the gradient dy of act(p), p = x w^T + bias as mx_dense has kept it (a matrix or an "fp8" MxTensor; None will do without an
+    activation).  d = dy act'(p) along its rows is for the gradient of x (a product with w's transposed quantisation), dt along its columns for that of w (one with
+    x's, which mx_transpose gives); ht is act(p) along its columns in the format `hidden`, for the next weight's gradient, or None; dbias is float32, or None."""
+    return _activation_backward("mx_dense_backward", dy, p, 0, activation, hidden, format, format_transposed, bias)
+
+
+def mx_gated_backward(dh, p, activation="silu", hidden="fp4", format="fp8", format_transposed="fp8"):
+    """(d, dt, ht) from the gradient dh of a gated block's h and its p as mx_gated has kept it: d and dt are the gradient of p, gate and up in turn, along its
+    rows and columns, and ht is h along its columns in the format `hidden`, or None."""
+    return _activation_backward("mx_gated_backward", dh, p, 1, activation, hidden, format, format_transposed, False)[:3]
+
+
+def mx_transpose(q, format="fp4"):
+    """The columns of an MxTensor, from the values that it stands for, as the rows of one in `format`: a checkpoint as the right operand of a weight's
+    gradient."""
+    if not isinstance(q, MxTensor):
+        _refuse("mx_transpose: an MxTensor is wanted")
+    rows, cols = q.shape
+    t = MxTensor.empty(cols, rows, format, q.device)
+    _call(_lib.ssgd_mx_transpose, q.device, *q._at, _FORMATS[q.format], rows, cols, _FORMATS[format], *t._at)
+    return t
+
+
+def _gate(gate, rows, d, dev, what):
+    """(pointer, type, number, pitch) of a gate per column (d), or of one for each of several runs of rows (gates x d)."""
+    if gate is None:
+        return None, 0, 1, 0
+    if not (gate.shape == (d,) or (gate.dim() == 2 and gate.shape[1] == d and gate.shape[0] > 0 and rows % gate.shape[0] == 0)) or gate.device != dev:
+        _refuse(f"{what}: a gate per column, or one for each of several equal runs of rows, is wanted")
+    _, kind, gates, _, pitch = _matrix(gate if gate.dim() == 2 else gate.unsqueeze(0), what)
+    return gate.data_ptr(), kind, gates, pitch
+
+
+def block_norm(o, s, post_weight, weight, gate=None, scale=1.0, eps=1e-6, output=None):
+    """(y, sum, rstd_o, rstd) between two blocks of a residual stream: sum = scale s + gate norm(o) post_weight and y = norm(sum) weight, with the root-mean-square
+    norm of rows.  gate: None, one value per column, or a row of them for each of several equal runs of rows; scale: a number.  y has the rows' type or, with
+    output="fp8", is an MxTensor for the product behind it; the rest is what block_norm_backward takes (autograd records nothing)."""
+    dev, kind, rows, d, pitch = _matrix(o, "block_norm")
+    if output is not None and output != "fp8":
+        _refuse("block_norm: the output is None (the rows' type) or 'fp8'")
+    s_at, s_pitch = _beside(s, o, "block_norm")
+    post, post_kind = _weight(post_weight, o, "block_norm")
+    w, w_kind = _weight(weight, o, "block_norm")
+    gate_at, gate_kind, gates, gate_pitch = _gate(gate, rows, d, dev, "block_norm")
+    total, stds = _torch.empty(rows, d, dtype=o.dtype, device=dev), _torch.empty(2, rows, dtype=_torch.float32, device=dev)
+    if output is None:
+        y = _torch.empty(rows, d, dtype=o.dtype, device=dev)
+        to = (y.data_ptr(), d, None, None)
+    else:
+        y = MxTensor.empty(rows, d, "fp8", dev)
+        to = (None, 0, *y._at)
+    at = stds.data_ptr()
+    _call(_lib.ssgd_block_norm, dev, o.data_ptr(), pitch, s_at, s_pitch, post, post_kind, w, w_kind, gate_at, gate_kind, gates, gate_pitch, scale, eps, kind, rows, d,
+          total.data_ptr(), d, *to, at, at + 4 * rows)
+    return y, total, stds[0], stds[1]
+
+
+def block_norm_backward(dy, o, sum, post_weight, weight, rstd_o, rstd, gate=None, scale=1.0, dsum=None):
+    """(do, ds, dpost_weight, dweight, dgate) from the gradient dy of block_norm's y and, where there is one, dsum that reaches the sum past the second norm.
+    The gradients of the weights and of the gate (None without one) are float32."""
+    dev, kind, rows, d, pitch = _matrix(dy, "block_norm_backward")
+    o_at, o_pitch = _beside(o, dy, "block_norm_backward")
+    sum_at, sum_pitch = _beside(sum, dy, "block_norm_backward")
+    more, more_pitch = _beside(dsum, dy, "block_norm_backward")
+    post, post_kind = _weight(post_weight, dy, "block_norm_backward")
+    w, w_kind = _weight(weight, dy, "block_norm_backward")
+    for r in (rstd_o, rstd):
+        if not (r.dtype == _torch.float32 and r.shape == (rows,) and r.is_contiguous() and r.device == dev):
+            _refuse("block_norm_backward: one float32 rstd per row of both norms is wanted")
+    gate_at, gate_kind, gates, gate_pitch = _gate(gate, rows, d, dev, "block_norm_backward")
+    grad_o, grad_s = _torch.empty(rows, d, dtype=dy.dtype, device=dev), _torch.empty(rows, d, dtype=dy.dtype, device=dev)
+    sides = _torch.empty(2, d, dtype=_torch.float32, device=dev)
+    dgate = None if gate is None else _torch.empty(gate.shape, dtype=_torch.float32, device=dev)
+    floats = _lib.ssgd_block_norm_work_floats(rows, d, gates)
+    if floats < 0:
+        _refuse("block_norm_backward: rows < 2^31, 1 <= columns < 2^24")
+    work = _torch.empty(floats, dtype=_torch.float32, device=dev)
+    at = sides.data_ptr()
+    _call(_lib.ssgd_block_norm_backward, dev, dy.data_ptr(), pitch, o_at, o_pitch, sum_at, sum_pitch, post, post_kind, w, w_kind, gate_at, gate_kind, gates, gate_pitch, scale,
+          rstd_o.data_ptr(), rstd.data_ptr(), more, more_pitch, kind, rows, d, grad_o.data_ptr(), d, grad_s.data_ptr(), d, at, at + 4 * d, None if dgate is None else dgate.data_ptr(),
+          work.data_ptr())
+    return grad_o, grad_s, sides[0], sides[1], dgate

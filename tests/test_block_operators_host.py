@@ -1,0 +1,146 @@
+"""Host-side checks of the operators of a gated feed-forward block that need no GPU: invalid arguments are refused before the device is touched."""
+import os
+
+import pytest
+
+from paper_2003_10579_amd import ssgd
+
+A = 0x1000       # an address that is never followed
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(ssgd._LIB_PATH):
+        from paper_2003_10579_amd import build
+        build.build()
+    return ssgd.lib()
+
+
+def _refused(L, status, word):
+    assert status == ssgd.EINVAL and word in L.ssgd_last_error(None)
+
+
+def _dense(L, bad, gated=0, from_rows=False):
+    g = lambda k, d: bad.get(k, d)  # noqa: E731
+    N = g("N", 20)
+    results = N // 2 if gated else N
+    e = ssgd.MxEpilogue(g("gated", gated), g("act", 2), g("bias_dtype", 0), g("residual_dtype", 0), g("out_dtype", 0), g("kept_dtype", 0), g("bias", None if gated else A),
+                        g("residual", None if gated else A), g("residual_pitch", N), g("out", A), g("out_pitch", results), g("values", None), g("scales", None), g("kept", A), g("kept_pitch", N),
+                        g("kept_values", None), g("kept_scales", None))
+    x = g("x", A if from_rows else None)
+    return L.ssgd_mx_dense(x, g("dtype", 0), g("pitch", 1000), g("a", None if from_rows else A), g("sa", None if from_rows else A), g("fmt", 0), g("M", 10), g("b", A), g("sb", A), N,
+                           g("K", 1000), e, g("work", A), None)
+
+
+BAD = [dict(fmt=2), dict(act=4), dict(act=-1), dict(gated=2), dict(M=-1), dict(N=-1), dict(K=-1), dict(M=1 << 31), dict(K=1 << 24), dict(b=None), dict(sb=None), dict(b=A + 8), dict(sb=A + 4), dict(out=None),
+       dict(out=A + 2), dict(out_dtype=2), dict(out_pitch=9), dict(values=A), dict(values=A, scales=A), dict(out=None, values=A + 8, scales=A), dict(out=None, values=A, scales=A + 8),
+       dict(out=None, values=A), dict(kept=A + 2), dict(kept_dtype=7), dict(kept_pitch=19), dict(kept_values=A, kept_scales=A), dict(kept=None, kept_values=A), dict(kept=None, kept_values=A + 8, kept_scales=A),
+       dict(kept=None, kept_values=A, kept_scales=A + 1)]
+
+
+@pytest.mark.parametrize("bad", BAD + [dict(a=None), dict(sa=None), dict(a=A + 8), dict(sa=A + 8), dict(x=A), dict(bias=A + 1), dict(bias_dtype=2), dict(residual=A + 2), dict(residual_dtype=-1),
+                                       dict(residual_pitch=19)])
+def test_mx_dense_refuses(L, bad):
+    _refused(L, _dense(L, bad), b"mx dense")
+
+
+@pytest.mark.parametrize("bad", BAD + [dict(N=21), dict(bias=A), dict(residual=A)])
+def test_mx_gated_refuses(L, bad):
+    _refused(L, _dense(L, bad, gated=1), b"mx dense")
+
+
+@pytest.mark.parametrize("rows", [1, 10])
+@pytest.mark.parametrize("bad", [dict(x=A + 2), dict(dtype=2), dict(pitch=999), dict(a=A, sa=A), dict(work=None), dict(work=A + 8)])
+def test_mx_dense_refuses_rows(L, bad, rows):
+    if rows == 1 and "work" in bad:
+        assert L.ssgd_mx_dense_work_bytes(0, 1, 0, 1, 20, 1000) == 0          # one row needs none
+        return
+    _refused(L, _dense(L, dict(bad, M=rows), from_rows=True), b"mx dense")
+
+
+def test_mx_dense_with_nothing_to_do(L):
+    assert _dense(L, dict(M=0, out=None)) == ssgd.OK and _dense(L, dict(N=0, out=None)) == ssgd.OK
+    _refused(L, L.ssgd_mx_dense(None, 0, 0, A, A, 0, 10, A, A, 20, 100, None, A, None), b"epilogue")
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1 << 28, 1000), (16, 1 << 28, 1000), (1 << 30, 1 << 20, 128), (1 << 30, 1 << 24, 0)])
+def test_mx_dense_refuses_more_threads_than_a_launch_has(L, M, N, K):
+    _refused(L, _dense(L, dict(M=M, N=N, K=K, out=A)), b"too many")
+
+
+def test_mx_dense_work_bytes(L):
+    work = L.ssgd_mx_dense_work_bytes
+    # one launch needs none; rows quantised in front of the product; sums of few rows for an output in 8 bits; parts of a long contraction
+    assert work(0, 0, 0, 4000, 4000, 4000) == 0 and work(1, 0, 1, 4000, 4000, 4000) == 0 and work(1, 1, 0, 2, 500, 900) == 0
+    assert work(1, 1, 0, 10, 50, 1000) == 10 * (1024 + 32) and work(1, 1, 1, 1, 50, 1000) == 200 and work(0, 0, 1, 16, 50, 1000) == 16 * 50 * 4
+    assert work(1, 1, 1, 10, 50, 1000) == 10 * (1024 + 32) + 2000
+    assert work(0, 0, 0, 128, 1000, 100000) == L.ssgd_mx_matmul_work_bytes(0, 128, 1000, 100000) > 0
+    assert work(0, 1, 1, 10, 50, 0) == 0
+    for bad in ((2, 10, 50, 1000), (0, -1, 50, 10), (0, 1, -1, 10), (0, 1, 50, 1 << 24)):
+        assert work(bad[0], 0, 0, *bad[1:]) == -1
+    _refused(L, _dense(L, dict(M=128, N=1000, K=100000, residual_pitch=1000, out_pitch=1000, kept_pitch=1000, work=None)), b"work")
+
+
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("bad", [
+    dict(dy=None), dict(dy=A + 2), dict(dtype=2), dict(pitch=39), dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 30, pitch=1 << 30), dict(gated=2), dict(act=4), dict(act=-1), dict(p=None),
+    dict(p=A + 2), dict(p_dtype=3), dict(p_pitch=39), dict(p_values=A, p_scales=A), dict(p=None, p_values=A), dict(p=None, p_values=A + 8, p_scales=A), dict(p=None, p_values=A, p_scales=A + 8), dict(fmt=2),
+    dict(fmt_t=-1), dict(fmt_h=2), dict(values=None), dict(scales=None), dict(values=A + 8), dict(scales=A + 8), dict(values_t=None), dict(scales_t=A + 4), dict(values_h=A + 4), dict(scales_h=None),
+    dict(values=None, scales=None, values_t=None, scales_t=None, values_h=None, scales_h=None), dict(rows=(1 << 31) - 1, cols=1 << 29, pitch=1 << 29, p_pitch=1 << 30),
+])
+def test_mx_activation_backward_refuses(L, bad, gated):
+    g = lambda k, d: bad.get(k, d)  # noqa: E731
+    _refused(L, L.ssgd_mx_activation_backward(g("dy", A), g("dtype", 0), g("pitch", 40), g("rows", 10), g("cols", 40), g("gated", gated), g("act", 3), g("p", A), g("p_dtype", 0), g("p_pitch", 80 if gated else 40),
+                                              g("p_values", None), g("p_scales", None), g("fmt", 0), g("values", A), g("scales", A), g("fmt_t", 0), g("values_t", A), g("scales_t", A), g("fmt_h", 0),
+                                              g("values_h", A), g("scales_h", A), None, None, None), b"mx activation backward")
+
+
+def test_mx_activation_backward_bias(L):
+    call = lambda gated, cols, db, work: L.ssgd_mx_activation_backward(A, 0, cols, 10, cols, gated, 3, A, 0, 2 * cols, None, None, 1, A, A, 1, A, A, 0, None, None, db, work, None)  # noqa: E731
+    for args in ((1, 40, A, A), (0, 40, A, None), (0, 40, A, A + 8), (0, 40, A + 2, A), (0, 1 << 25, A, A)):
+        _refused(L, call(*args), b"bias")
+    floats = L.ssgd_mx_activation_backward_work_floats
+    assert floats(0, 40) == 0 and floats(1, 40) == 40 and floats(129, 40) == 80 and floats(-1, 40) == -1 and floats(10, 1 << 25) == -1
+    assert L.ssgd_mx_activation_backward(None, 0, 0, 10, 0, 0, 3, None, 0, 0, None, None, 1, None, None, 1, None, None, 0, None, None, None, None, None) == ssgd.OK
+
+
+@pytest.mark.parametrize("bad", [dict(values=None), dict(scales=None), dict(values_t=None), dict(scales_t=None), dict(values=A + 8), dict(scales=A + 8), dict(values_t=A + 4), dict(scales_t=A + 4), dict(fmt=2),
+                                 dict(fmt_t=-1), dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 31), dict(rows=(1 << 31) - 1, cols=(1 << 31) - 1)])
+def test_mx_transpose_refuses(L, bad):
+    g = lambda k, d: bad.get(k, d)  # noqa: E731
+    _refused(L, L.ssgd_mx_transpose(g("values", A), g("scales", A), g("fmt", 1), g("rows", 10), g("cols", 40), g("fmt_t", 0), g("values_t", A), g("scales_t", A), None), b"mx transpose")
+    assert L.ssgd_mx_transpose(None, None, 1, 0, 40, 0, None, None, None) == ssgd.OK
+
+
+SHARED = [dict(o=None), dict(o=A + 2), dict(o_pitch=99), dict(post=None), dict(post=A + 2), dict(post_dtype=2), dict(w=None), dict(w=A + 1), dict(w_dtype=-1), dict(gate=A + 2), dict(gate=A, gate_dtype=2),
+          dict(gate=A, gates=0), dict(gate=A, gates=3), dict(gate=A, gates=2, gate_pitch=99), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e39), dict(dtype=2), dict(rows=-1), dict(rows=1 << 31),
+          dict(d=0), dict(d=1 << 24), dict(rstd_o=None), dict(rstd=None), dict(rstd=A + 2), dict(sum=None), dict(sum=A + 2), dict(sum_pitch=99)]
+
+
+@pytest.mark.parametrize("bad", SHARED + [dict(s=None), dict(s=A + 2), dict(s_pitch=99), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(y=None), dict(y=A + 2), dict(y_pitch=99),
+                                          dict(values=A, scales=A), dict(y=None, values=A), dict(y=None, values=A + 8, scales=A), dict(y=None, values=A, scales=A + 8)])
+def test_block_norm_refuses(L, bad):
+    g = lambda k, d: bad.get(k, d)  # noqa: E731
+    _refused(L, L.ssgd_block_norm(g("o", A), g("o_pitch", 100), g("s", A), g("s_pitch", 100), g("post", A), g("post_dtype", 0), g("w", A), g("w_dtype", 0), g("gate", None), g("gate_dtype", 0), g("gates", 1),
+                                  g("gate_pitch", 100), g("scale", 1.0), g("eps", 1e-6), g("dtype", 0), g("rows", 10), g("d", 100), g("sum", A), g("sum_pitch", 100), g("y", A), g("y_pitch", 100),
+                                  g("values", None), g("scales", None), g("rstd_o", A), g("rstd", A), None), b"block norm")
+
+
+@pytest.mark.parametrize("bad", SHARED + [dict(dy=None), dict(dy=A + 2), dict(dy_pitch=99), dict(dsum=A + 2), dict(dsum=A, dsum_pitch=99), dict(grad_o=None), dict(grad_o_pitch=99), dict(grad_s=A + 2),
+                                          dict(grad_s_pitch=99), dict(dpost=None), dict(dw=None), dict(dw=A + 2), dict(dgate=A), dict(work=None), dict(work=A + 8)])
+def test_block_norm_backward_refuses(L, bad):
+    g = lambda k, d: bad.get(k, d)  # noqa: E731
+    _refused(L, L.ssgd_block_norm_backward(g("dy", A), g("dy_pitch", 100), g("o", A), g("o_pitch", 100), g("sum", A), g("sum_pitch", 100), g("post", A), g("post_dtype", 0), g("w", A), g("w_dtype", 0),
+                                           g("gate", None), g("gate_dtype", 0), g("gates", 1), g("gate_pitch", 100), g("scale", 1.0), g("rstd_o", A), g("rstd", A), g("dsum", None), g("dsum_pitch", 100),
+                                           g("dtype", 0), g("rows", 10), g("d", 100), g("grad_o", A), g("grad_o_pitch", 100), g("grad_s", A), g("grad_s_pitch", 100), g("dpost", A), g("dw", A),
+                                           g("dgate", None), g("work", A), None), b"block norm")
+
+
+def test_block_norm_work_floats(L):
+    floats = L.ssgd_block_norm_work_floats
+    assert floats(0, 100, 1) == 0
+    for rows, d, gates in ((1, 1, 1), (3, 100, 3), (1 << 20, 100, 1), (1 << 20, 3000, 16), (500, 20000, 1), (5000, 300, 5000)):       # two sums for every unit of rows, a unit to a gate at least
+        units = floats(rows, d, gates) // (2 * d)
+        assert floats(rows, d, gates) == 2 * d * units and gates <= units <= rows and units % gates == 0
+    for bad in ((-1, 100, 1), (1 << 31, 100, 1), (10, 0, 1), (10, 1 << 24, 1), (10, 100, 0), (10, 100, 3)):
+        assert floats(*bad) == -1
