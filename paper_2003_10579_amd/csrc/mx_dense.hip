@@ -2,8 +2,8 @@
 //
 //   p = A B^T + bias          out[m][n] = residual + act(p[m][n])          or          out[m][c] = act(p[m][2 c]) p[m][2 c + 1]
 //
-// The kernels of the product (mx_product.hpp) hand their sums over in registers, eight columns of a row side by side, so a gate and what it
-// multiplies are neighbours; p is kept for the backward pass where that is wanted, and each of the two outputs goes out as a matrix or quantised to 8 bits
+// The kernels of the product (mx_product.hpp) hand their sums over, eight columns of a row to a lane, so a gate and what it multiplies are
+// neighbours; p is kept for the backward pass where that is wanted, and each of the two outputs goes out as a matrix or quantised to 8 bits
 // without a rounding in between.  Where a workgroup does not have the whole sum (contractions in parts) or a block of 32 columns (few rows), fp32
 // sums go to a work area and a second launch finishes them.
 #include "activations.hpp"
@@ -12,10 +12,6 @@
 using namespace ssgd;
 
 namespace {
-
-// Largest magnitude of a block of 32 columns: the product's lanes with eight columns each are 16 apart, a second launch's side by side.
-struct Apart { static __device__ __forceinline__ uint32_t largest(uint32_t x) { return max_of_rows(x); } };
-struct Beside { static __device__ __forceinline__ uint32_t largest(uint32_t x) { return max_of_4(x); } };
 
 struct Held { void* to; uint8_t *values, *scales; int64_t pitch, value_bytes, scale_bytes; int32_t bf16; };      // a matrix, or microscaled, or nothing
 
@@ -36,7 +32,7 @@ struct Common {
         if (h.bf16) store_vec<V>(static_cast<bf16_t*>(h.to) + m * h.pitch + n, left, x);
         else store_vec<V>(static_cast<float*>(h.to) + m * h.pitch + n, left, x);
     }
-    // Bias and sums of eight columns, nothing where there are no columns.
+    // The bias of eight columns, and their sums with it: nothing where there are no columns.
     __device__ __forceinline__ void bias_of(int64_t n, float (&b)[8]) const {
         if (bias != nullptr) load<8>(bias, bias_bf16, n, cols - n, b);
     }
@@ -50,33 +46,18 @@ struct Common {
             for (int q = 0; q < 8; ++q) p[q] = n + q < cols ? p[q] : 0.0f;
         }
     }
-    // Eight columns from n on, of `width` that there are; `first`: this lane stores the block's scale.
-    template <typename Lanes>
-    static __device__ __forceinline__ void store8(const Held& h, int64_t m, int64_t n, int64_t width, bool live, bool first, const float (&x)[8]) {
+    // Eight columns from n on, of `width` that there are; four lanes side by side have a block.
+    static __device__ __forceinline__ void store8(const Held& h, int64_t m, int64_t n, int64_t width, bool live, const float (&x)[8]) {
         if (h.values != nullptr) {
             uint32_t most = 0;
 #pragma unroll
             for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-            const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(Lanes::largest(most));
+            const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
             if (live && n < h.value_bytes) {
                 *reinterpret_cast<words2*>(h.values + m * h.value_bytes + n) = mx_pack_fp8(x, byte);
-                if (first) h.scales[m * h.scale_bytes + n / kMxBlock] = (uint8_t)byte;
+                if ((threadIdx.x & 3) == 0) h.scales[m * h.scale_bytes + n / kMxBlock] = (uint8_t)byte;
             }
         } else if (h.to != nullptr && live) store<8>(h, m, n, width - n, x);
-    }
-    template <typename Lanes>
-    __device__ __forceinline__ void dense8(int64_t m, int64_t n, bool first, const float (&b)[8], float (&p)[8]) const {
-        const bool live = m < rows;
-        add_bias(n, b, p);
-        store8<Lanes>(kept, m, n, cols, live, first, p);
-        activate(activation, p);
-        if (residual != nullptr && live && n < cols) {
-            float r[8];
-            load<8>(residual, residual_bf16, m * residual_pitch + n, cols - n, r);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) p[q] += r[q];
-        }
-        store8<Lanes>(out, m, n, cols, live, first, p);
     }
     // Four results of eight columns.
     __device__ __forceinline__ void gate(const float (&p)[8], float (&h)[4]) const {
@@ -136,69 +117,76 @@ struct Epilogue : Common {
         if (out.values != nullptr && mx_padded(results) * (GATED ? 2 : 1) > n) n = mx_padded(results) * (GATED ? 2 : 1);
         return n;
     }
-    template <int TM, int TN>
-    __device__ __forceinline__ void tile(int64_t m0, int64_t n0, int g, f32x4 (&acc)[TM][TN]) const {
-        static_assert(TN % 4 == 0, "a block of gated results is two blocks of columns");
-        auto eight = [&](int i, int j, float (&p)[8]) {
-            const f32x4 &a = acc[i][j], &b = acc[i][j + 1];
-            p[0] = a.x; p[1] = a.y; p[2] = a.z; p[3] = a.w; p[4] = b.x; p[5] = b.y; p[6] = b.z; p[7] = b.w;
-        };
+    // What eight columns of a row need before their sums are there: the residual in bf16 as it comes (in fp32 it would take twice the registers, and is read when it is used).
+    static constexpr bool kAhead = !GATED;
+    struct Nothing {};
+    using Raw = std::conditional_t<GATED, Nothing, words4>;
+    __device__ __forceinline__ void ahead(int64_t m, int64_t n, Raw& r) const {
         if constexpr (!GATED) {
-#pragma unroll
-            for (int j = 0; j < TN; j += 2) {
-                const int64_t n = n0 + j * 16 + g * 8;
-                float b[8], p[8];
-                bias_of(n, b);
-#pragma unroll
-                for (int i = 0; i < TM; ++i) { eight(i, j, p); dense8<Apart>(m0 + i * 16, n, g == 0, b, p); }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < TN; j += 4) {
-                const int64_t n = n0 + j * 16 + g * 8, c = (n0 + j * 16) / 2 + g * 4;
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const int64_t m = m0 + i * 16;
-                    const bool live = m < rows;
-                    float h[2][4];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        float p[8];
-                        eight(i, j + 2 * q, p);
-                        add_bias(n + 32 * q, p, p);          // (no bias: the columns past the end alone)
-                        store8<Apart>(kept, m, n + 32 * q, cols, live, g == 0, p);
-                        gate(p, h[q]);
-                    }
-                    if (out.values != nullptr) {
-                        uint32_t most = 0;
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(h[q / 4][q % 4]));
-                        const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(Apart::largest(most));
-                        if (live && c < out.value_bytes) {
-                            uint8_t* to = out.values + m * out.value_bytes + c;
-                            *reinterpret_cast<uint32_t*>(to) = mx_pack_fp8(h[0][0], h[0][1], h[0][2], h[0][3], byte);
-                            *reinterpret_cast<uint32_t*>(to + 16) = mx_pack_fp8(h[1][0], h[1][1], h[1][2], h[1][3], byte);
-                            if (g == 0) out.scales[m * out.scale_bytes + c / kMxBlock] = (uint8_t)byte;
-                        }
-                    } else if (live) {
-                        store<4>(out, m, c, results - c, h[0]);
-                        store<4>(out, m, c + 16, results - c - 16, h[1]);
-                    }
-                }
-            }
+            r = words4{0u, 0u, 0u, 0u};
+            if (residual == nullptr || !residual_bf16 || m >= rows || n >= cols) return;
+            Eight<bf16_t> x;
+            x.load_own<false>(static_cast<const bf16_t*>(residual) + m * residual_pitch, n, cols);
+            r = x.w;
         }
     }
+    __device__ __forceinline__ void add_residual(int64_t m, int64_t n, const Raw& r, float (&p)[8]) const {
+        float x[8];
+        if (residual_bf16) {
+            Eight<bf16_t> e;
+            e.w = r;
+            e.numbers(x);
+        } else load_vec<8>(static_cast<const float*>(residual) + m * residual_pitch + n, m < rows ? cols - n : 0, x);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) p[q] += x[q];
+    }
+    // Eight columns of p, with what `ahead` has brought, to eight results, or four, and these to their output; p itself to where it is kept.  Lanes side by side have
+    // columns side by side, whole blocks of them.
+    __device__ __forceinline__ void results_of(int64_t m, int64_t n, const Raw& r, float (&p)[8]) const {
+        if constexpr (!GATED) {
+            activate(activation, p);
+            if (residual != nullptr) add_residual(m, n, r, p);
+        } else {
+            float h[4];
+            gate(p, h);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) p[q] = h[q];
+        }
+    }
+    __device__ __forceinline__ void store_results(int64_t m, int64_t n, const float (&p)[8]) const {
+        const bool live = m < rows;
+        if constexpr (!GATED) store8(out, m, n, cols, live, p);
+        else {
+            const float h[4] = {p[0], p[1], p[2], p[3]};
+            const int64_t c = n / 2;
+            if (out.values != nullptr) {
+                uint32_t most = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) most = umax(most, magnitude(h[q]));
+                const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_8(most));
+                if (live && c < out.value_bytes) {
+                    *reinterpret_cast<uint32_t*>(out.values + m * out.value_bytes + c) = mx_pack_fp8(h[0], h[1], h[2], h[3], byte);
+                    if ((threadIdx.x & 7) == 0) out.scales[m * out.scale_bytes + c / kMxBlock] = (uint8_t)byte;
+                }
+            } else if (live) store<4>(out, m, c, results - c, h);
+        }
+    }
+    __device__ __forceinline__ bool keeps() const { return kept.to != nullptr || kept.values != nullptr; }
+    __device__ __forceinline__ void keep(int64_t m, int64_t n, const float (&p)[8]) const { store8(kept, m, n, cols, m < rows, p); }
 };
 
 // The parts of a contraction (none: a contraction of no columns), added in order, and the epilogue: eight columns a thread.
 template <bool GATED>
-__global__ __launch_bounds__(256) void finish_kernel(const float* parts, int32_t n, int64_t stride, Common e, int64_t groups, int64_t per_row) {
+__global__ __launch_bounds__(256) void finish_kernel(const float* parts, int32_t n, int64_t stride, Epilogue<GATED> e, int64_t groups, int64_t per_row) {
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (u >= groups) return;                 // (rows have a multiple of 32 groups: whole blocks)
+    if (u >= groups) return;                 // (rows have a multiple of 16 groups, gated 32: whole blocks)
     const int64_t row = u / per_row, col = (u - row * per_row) * 8;
     float p[8], b[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) p[q] = 0.0f;
+    typename Epilogue<GATED>::Raw r;
+    e.ahead(row, col, r);
+    e.bias_of(col, b);
     const float* at = parts + row * e.cols + col;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -208,25 +196,10 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* parts, int32_t
 #pragma unroll
         for (int q = 0; q < 8; ++q) p[q] += x[q];
     }
-    if constexpr (!GATED) {
-        e.bias_of(col, b);
-        e.dense8<Beside>(row, col, (threadIdx.x & 3) == 0, b, p);
-    } else {
-        float h[4];
-        Common::store8<Beside>(e.kept, row, col, e.cols, true, (threadIdx.x & 3) == 0, p);
-        e.gate(p, h);
-        const int64_t c = col / 2;
-        if (e.out.values != nullptr) {
-            uint32_t most = 0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) most = umax(most, magnitude(h[q]));
-            const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_8(most));
-            if (c < e.out.value_bytes) {
-                *reinterpret_cast<uint32_t*>(e.out.values + row * e.out.value_bytes + c) = mx_pack_fp8(h[0], h[1], h[2], h[3], byte);
-                if ((threadIdx.x & 7) == 0) e.out.scales[row * e.out.scale_bytes + c / kMxBlock] = (uint8_t)byte;
-            }
-        } else Common::store<4>(e.out, row, c, e.results - c, h);
-    }
+    e.add_bias(col, b, p);
+    e.keep(row, col, p);
+    e.results_of(row, col, r, p);
+    e.store_results(row, col, p);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
@@ -251,7 +224,7 @@ int64_t finish_columns(int64_t results, bool gated) { return (gated ? 2 : 1) * m
 template <bool GATED>
 void finish(const Common& e, const float* parts, int n, hipStream_t s) {
     const int64_t per_row = finish_columns(e.results, GATED) / 8, groups = e.rows * per_row;
-    hipLaunchKernelGGL((finish_kernel<GATED>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, parts, n, e.rows * e.cols, e, groups, per_row);
+    hipLaunchKernelGGL((finish_kernel<GATED>), dim3((unsigned)((groups + 255) / 256)), dim3(256), 0, s, parts, n, e.rows * e.cols, Epilogue<GATED>{e}, groups, per_row);
 }
 
 // The product, its results to Out.

@@ -247,7 +247,62 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(Product p, Out out) 
 #pragma unroll
             for (int j = 0; j < TN; j += 2) store_eight<typename Out::type>(p, m0 + row_a + i * 16, n0 + col + j * 16 + g * 8, acc[i][j], acc[i][j + 1]);
     } else {
-        out.tile(m0 + row_a, n0 + col, g, acc);
+        // The sums of sixteen rows of a wave at a time through the stages' room, so that an epilogue has rows: eight columns to a lane, lanes side by side.  One piece of code for all: what is unrolled over 128 sums with every kind of output is more than the instruction cache holds.
+        constexpr int kPitch = TN * 16 + 4, kStrip = 16 * kPitch * 4, kStrips = kStage / kStrip, kPerRow = TN * 2, kPass = 64 / kPerRow, kPasses = 16 / kPass;
+        static_assert(kWaves <= 2 * kStrips, "a strip to every wave in two stages");
+        wait_and_meet<0>();
+        float* strip = reinterpret_cast<float*>(wave < kStrips ? stage0 + wave * kStrip : stage1 + (wave - kStrips) * kStrip);
+        const int lane_row = lane / kPerRow, lane_col = lane % kPerRow * 8;
+        const int64_t n = n0 + col + lane_col;
+        const int64_t m_first = m0 + (wave / WN) * TM * 16 + lane_row;
+        float b[8];
+        typename Out::Raw r[kPasses];
+        out.bias_of(n, b);
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) out.ahead(m_first + q * kPass, n, r[q]);
+#pragma unroll 1
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m_first + i * 16;
+#pragma unroll
+            for (int k = 0; k < TM; ++k) {
+                if (k != i) continue;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4*>(strip + r16 * kPitch + j / 2 * 32 + g * 8 + j % 2 * 4) = acc[k][j];
+            }
+            asm volatile("" ::: "memory");
+            auto sums = [&](int q, float (&s)[8]) {
+                const float* from = strip + (lane_row + q * kPass) * kPitch + lane_col;
+                const f32x4 x = *reinterpret_cast<const f32x4*>(from), y = *reinterpret_cast<const f32x4*>(from + 4);
+                s[0] = x.x; s[1] = x.y; s[2] = x.z; s[3] = x.w; s[4] = y.x; s[5] = y.y; s[6] = y.z; s[7] = y.w;
+                out.add_bias(n, b, s);
+            };
+            if constexpr (Out::kAhead) {
+                // What the next rows need is asked for before these are stored: a load is back when the stores before it are, too.
+                float s[kPasses][8];
+#pragma unroll
+                for (int q = 0; q < kPasses; ++q) { sums(q, s[q]); out.results_of(m + q * kPass, n, r[q], s[q]); }
+                if (i + 1 < TM) {
+#pragma unroll
+                    for (int q = 0; q < kPasses; ++q) out.ahead(m + 16 + q * kPass, n, r[q]);
+                }
+#pragma unroll
+                for (int q = 0; q < kPasses; ++q) out.store_results(m + q * kPass, n, s[q]);
+                if (out.keeps()) {
+#pragma unroll
+                    for (int q = 0; q < kPasses; ++q) { sums(q, s[q]); out.keep(m + q * kPass, n, s[q]); }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kPasses; ++q) {
+                    float s[8];
+                    sums(q, s);
+                    out.keep(m + q * kPass, n, s);
+                    out.results_of(m + q * kPass, n, r[q], s);
+                    out.store_results(m + q * kPass, n, s);
+                }
+            }
+            asm volatile("" ::: "memory");
+        }
     }
 }
 
