@@ -2,6 +2,8 @@
 // along its rows and along its columns; and a checkpoint in few bits quantised again along its columns.
 //
 //   dp = dy act'(p),   h = act(p)          gated, in pairs of columns g, u:   dg = dy u act'(g),   du = dy act(g),   h = act(g) u
+#include <type_traits>
+
 #include "activations.hpp"
 #include "column_sums.hpp"
 
@@ -21,22 +23,18 @@ struct Gradient {
     Target along, columns, hidden;
 };
 
-// A wave has 32 rows of the 128 columns of a tile: of every sixteen lanes, four side by side have a block of 32 columns, eight each, and the next four
-// the eight rows below.  So a block along a row is four lanes', and one along a column eight registers of the lanes four, eight and twelve further on.
-constexpr int kTurn4 = 0x124, kTurn8 = 0x128;
-__device__ __forceinline__ uint32_t max_of_turns(uint32_t x) { x = umax(x, dpp<kTurn4>(x)); return umax(x, dpp<kTurn8>(x)); }
-__device__ __forceinline__ float sum_of_turns(float x) {
-    x += __builtin_bit_cast(float, dpp<kTurn4>(__builtin_bit_cast(uint32_t, x)));
-    return x + __builtin_bit_cast(float, dpp<kTurn8>(__builtin_bit_cast(uint32_t, x)));
-}
+// A wave has 32 rows of the 128 columns of a tile: sixteen lanes side by side have eight columns each, the next sixteen the eight rows below.  So a block along a row is
+// four lanes', and one along a column eight registers of the four lanes with the same place in a row of sixteen.
 struct Place {
     int64_t row, col;       // the lane's first
-    int turn;               // of its rows
+    int32_t wave, turn, own;      // turn: of its rows, own: its first column in the tile
     __device__ __forceinline__ Place(int64_t r0, int64_t c0) {
         const int lane = threadIdx.x & 63;
-        turn = (lane >> 2) & 3;
-        row = r0 + (threadIdx.x >> 6) * 32 + turn * 8;
-        col = c0 + (lane >> 4) * 32 + (lane & 3) * 8;
+        wave = threadIdx.x >> 6;
+        turn = lane >> 4;
+        own = (lane & 15) * 8;
+        row = r0 + wave * 32 + turn * 8;
+        col = c0 + own;
     }
 };
 
@@ -53,112 +51,194 @@ __device__ __forceinline__ void store_along(const Target& t, int64_t row, int64_
     else *reinterpret_cast<words2*>(to + col) = mx_pack_fp8(x, byte);
     if ((threadIdx.x & 3) == 0) t.scales[row * t.scale_bytes + col / kMxBlock] = (uint8_t)byte;
 }
-// Eight rows of a column as a part of the transposed matrix's row `col`.
-__device__ __forceinline__ void store_column(const Target& t, const Place& at, int64_t col, bool live, const float (&x)[8]) {
-    uint32_t most = 0;
+// The columns of a tile, quantised, on their way to the transposed matrix: 128 rows of one are 128 or 64 bytes side by side there, of which a lane has eight or four
+// (stored by the lanes themselves, in pieces of 32 bytes: 8192 x 8192 pairs in 8 bits 227 us instead of 158).  The 16-byte parts of a column, and columns next to each
+// other, change places by the column's number, so that the lanes that write at a time, and those that read, meet in no bank.
+template <int COLS> struct Columns {
+    uint32_t values[COLS * 32];
+    uint8_t scales[COLS * 4];
+    static __device__ __forceinline__ int part8(int col, int part) { return ((col ^ ((col >> 6) & 1)) * 8 + (part ^ ((col >> 3) & 7))) * 4; }
+    static __device__ __forceinline__ int part4(int col, int part) { return ((col ^ ((col >> 5) & 3)) * 4 + (part ^ ((col >> 3) & 3))) * 4; }
+    // Eight rows of column `col` of the tile.
+    __device__ __forceinline__ void put(int32_t fmt, const Place& at, int col, const float (&x)[8]) {
+        uint32_t most = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-    most = max_of_turns(most);
-    const uint32_t byte = t.fmt == SSGD_MX_FP4 ? mx_scale_byte<SSGD_MX_FP4>(most) : mx_scale_byte<SSGD_MX_FP8>(most);
-    if (!live) return;
-    uint8_t* to = t.values + col * t.row_bytes;
-    if (t.fmt == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(to + at.row / 2) = mx_pack_fp4(x, byte);
-    else *reinterpret_cast<words2*>(to + at.row) = mx_pack_fp8(x, byte);
-    if (at.turn == 0) t.scales[col * t.scale_bytes + at.row / kMxBlock] = (uint8_t)byte;
-}
-
-// In place: p becomes dp (gated) or act(p), dy becomes h or dp.
-template <int ACT, bool GATED, int W>
-__device__ __forceinline__ void differentiate(float (&p)[8][8], float (&dy)[8][W]) {
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-        for (int q = 0; q < W; ++q) {
-            float y, slope;
-            if constexpr (GATED) {
-                const float up = p[r][2 * q + 1];
-                activation_and_slope(ACT, p[r][2 * q], y, slope);
-                p[r][2 * q] = dy[r][q] * up * slope;
-                p[r][2 * q + 1] = dy[r][q] * y;
-                dy[r][q] = y * up;
-            } else {
-                activation_and_slope(ACT, p[r][q], y, slope);
-                dy[r][q] = ACT == SSGD_ACT_RELU ? (slope > 0.0f ? dy[r][q] : 0.0f) : dy[r][q] * slope;
-                p[r][q] = y;
-            }
+        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
+        most = max_of_rows(most);
+        uint32_t byte;
+        if (fmt == SSGD_MX_FP4) {
+            byte = mx_scale_byte<SSGD_MX_FP4>(most);
+            values[part4(col, at.wave) + at.turn] = mx_pack_fp4(x, byte);
+        } else {
+            byte = mx_scale_byte<SSGD_MX_FP8>(most);
+            *reinterpret_cast<words2*>(&values[part8(col, at.wave * 2 + (at.turn >> 1)) + (at.turn & 1) * 2]) = mx_pack_fp8(x, byte);
         }
-}
+        if (at.turn == 0) scales[col * 4 + at.wave] = (uint8_t)byte;
+    }
+    // All of them, when all waves have met: column 0 is row `first` of the transposed matrix, of `rows`.
+    __device__ __forceinline__ void store(const Target& t, int64_t first, int64_t rows, int64_t r0) const {
+        const int parts = t.fmt == SSGD_MX_FP4 ? 4 : 8, shift = t.fmt == SSGD_MX_FP4 ? 2 : 3;
+        const int64_t at = t.fmt == SSGD_MX_FP4 ? r0 / 2 : r0;
+        for (int u = threadIdx.x; u < COLS * parts; u += kThreads) {
+            const int col = u >> shift, part = u & (parts - 1);
+            if (first + col >= rows) continue;
+            const words4 w = *reinterpret_cast<const words4*>(&values[t.fmt == SSGD_MX_FP4 ? part4(col, part) : part8(col, part)]);
+            *reinterpret_cast<words4*>(t.values + (first + col) * t.row_bytes + at + part * 16) = w;
+        }
+        if ((int)threadIdx.x < COLS && first + threadIdx.x < rows)
+            *reinterpret_cast<uint32_t*>(t.scales + (first + threadIdx.x) * t.scale_bytes + r0 / kMxBlock) = *reinterpret_cast<const uint32_t*>(&scales[threadIdx.x * 4]);
+    }
+};
 
-template <typename T, bool GATED>
-__global__ __launch_bounds__(kThreads) void gradient_kernel(Gradient a) {
-    constexpr int W = GATED ? 4 : 8;
-    __shared__ float sums[4][kTile];
-    const int64_t tile_row = blockIdx.x / a.across, c0 = (blockIdx.x - tile_row * a.across) * kTile;
-    const Place at(tile_row * kTile, c0);
-    const int64_t own_col = GATED ? at.col / 2 : at.col;
-    float p[8][8], dy[8][W];
+// Eight rows of W columns as they come, two columns at a time as numbers.  (Values in few bits stay packed until they are used: with all of a lane's 64 numbers of
+// p and dy in registers beside those of dp a SIMD had two waves.)
+struct Fp8 {};       // with scales
+template <typename T, int W> struct Raw;
+template <int W> struct Raw<float, W> {
+    float x[8][W];
+    __device__ __forceinline__ void load(int r, const float* row, int64_t left) { load_vec<W>(row, left, x[r]); }
+    __device__ __forceinline__ void clear(int r) {
+#pragma unroll
+        for (int q = 0; q < W; ++q) x[r][q] = 0.0f;
+    }
+    __device__ __forceinline__ f32x2 pair(int r, int k) const { return f32x2{x[r][2 * k], x[r][2 * k + 1]}; }
+};
+template <int W> struct Raw<bf16_t, W> {
+    uint32_t x[8][W / 2];
+    __device__ __forceinline__ void load(int r, const bf16_t* row, int64_t left) {
+        if (left >= W) {
+            if constexpr (W == 8) {
+                const words4 v = *reinterpret_cast<const words4_any*>(row);
+                x[r][0] = v.x; x[r][1] = v.y; x[r][2] = v.z; x[r][3] = v.w;
+            } else {
+                const words2 v = *reinterpret_cast<const words2_any*>(row);
+                x[r][0] = v.x; x[r][1] = v.y;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < W / 2; ++k) x[r][k] = (2 * k < left ? (uint32_t)row[2 * k] : 0u) | (2 * k + 1 < left ? (uint32_t)row[2 * k + 1] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void clear(int r) {
+#pragma unroll
+        for (int k = 0; k < W / 2; ++k) x[r][k] = 0u;
+    }
+    __device__ __forceinline__ f32x2 pair(int r, int k) const { return f32x2{bf16_to_f32(x[r][k] & 0xFFFFu), __builtin_bit_cast(float, x[r][k] & 0xFFFF0000u)}; }
+};
+template <> struct Raw<Fp8, 8> {
+    words2 x[8];
+    float scale[8];
+    __device__ __forceinline__ f32x2 pair(int r, int k) const {
+        const int w = (int)(k < 2 ? x[r].x : x[r].y);
+        const f32x2 v = k % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(w, true) : __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+        return f32x2{v.x * scale[r], v.y * scale[r]};
+    }
+};
+template <typename P>
+__device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, Raw<P, 8>& p) {
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
         const int64_t row = at.row + r;
-        const bool live = row < a.rows;
-        load_vec<W>(static_cast<const T*>(a.dy) + row * a.dy_pitch + own_col, live ? a.cols - own_col : 0, dy[r]);
-        if (a.p_values != nullptr) {
-            words2 w = {0u, 0u};
+        if constexpr (std::is_same_v<P, Fp8>) {
+            p.x[r] = words2{0u, 0u};
             uint32_t byte = 0;
-            if (live) {
-                w = *reinterpret_cast<const words2*>(a.p_values + row * a.p_bytes + at.col);
+            if (row < a.rows) {
+                p.x[r] = *reinterpret_cast<const words2*>(a.p_values + row * a.p_bytes + at.col);
                 byte = a.p_scales[row * a.p_scale_bytes + at.col / kMxBlock];
             }
-            mx_unpack_fp8(w, mx_scale_value(byte), p[r]);
-            // (a block that is NaN has columns past the last one too)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) if (at.col + q >= a.p_cols) p[r][q] = 0.0f;
-        } else if (a.p == nullptr) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) p[r][q] = 0.0f;
-        } else if (a.p_bf16) load_vec<8>(static_cast<const bf16_t*>(a.p) + row * a.p_pitch + at.col, live ? a.p_cols - at.col : 0, p[r]);
-        else load_vec<8>(static_cast<const float*>(a.p) + row * a.p_pitch + at.col, live ? a.p_cols - at.col : 0, p[r]);
+            // (columns past the last one in a block that is NaN are NaN too: what the formulas make of them is what they make of the block's others)
+            p.scale[r] = mx_scale_value(byte);
+        } else if (a.p == nullptr) p.clear(r);
+        else p.load(r, static_cast<const P*>(a.p) + row * a.p_pitch + at.col, row < a.rows ? a.p_cols - at.col : 0);
     }
-    if (a.activation == SSGD_ACT_RELU) differentiate<SSGD_ACT_RELU, GATED>(p, dy);
-    else if (a.activation == SSGD_ACT_GELU) differentiate<SSGD_ACT_GELU, GATED>(p, dy);
-    else if (a.activation == SSGD_ACT_SILU) differentiate<SSGD_ACT_SILU, GATED>(p, dy);
-    else differentiate<SSGD_ACT_NONE, GATED>(p, dy);
-    auto gradient = [&]() -> float (&)[8][8] { if constexpr (GATED) return p; else return dy; };
-    auto output = [&]() -> float (&)[8][W] { if constexpr (GATED) return dy; else return p; };
-    float (&d)[8][8] = gradient();
-    float (&h)[8][W] = output();
+}
+
+// Two columns of p, and of dy (gated: one), at a time: their part of dp, and their columns, which need no other.
+template <int ACT, bool GATED, typename T, typename P>
+__device__ __forceinline__ void differentiate(const Gradient& a, const Place& at, const Raw<P, 8>& p, const Raw<T, GATED ? 4 : 8>& dy, float (&d)[8][8], Columns<kTile>& columns,
+                                              Columns<GATED ? kTile / 2 : kTile>& hidden) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float h[GATED ? 1 : 2][8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const f32x2 x = p.pair(r, k);
+            float y, slope;
+            if constexpr (GATED) {
+                const f32x2 both = dy.pair(r, k / 2);
+                const float g = k % 2 ? both.y : both.x;
+                activation_and_slope(ACT, x.x, y, slope);
+                d[r][2 * k] = g * x.y * slope;
+                d[r][2 * k + 1] = g * y;
+                h[0][r] = y * x.y;
+            } else {
+                const f32x2 g = dy.pair(r, k);
+                activation_and_slope(ACT, x.x, y, slope);
+                d[r][2 * k] = ACT == SSGD_ACT_RELU ? (slope > 0.0f ? g.x : 0.0f) : g.x * slope;
+                h[0][r] = y;
+                activation_and_slope(ACT, x.y, y, slope);
+                d[r][2 * k + 1] = ACT == SSGD_ACT_RELU ? (slope > 0.0f ? g.y : 0.0f) : g.y * slope;
+                h[1][r] = y;
+            }
+        }
+        if (a.columns.values != nullptr) {
+#pragma unroll
+            for (int q = 2 * k; q < 2 * k + 2; ++q) {
+                const float x[8] = {d[0][q], d[1][q], d[2][q], d[3][q], d[4][q], d[5][q], d[6][q], d[7][q]};
+                columns.put(a.columns.fmt, at, at.own + q, x);
+            }
+        }
+        if (a.hidden.values != nullptr) {
+            if constexpr (GATED) hidden.put(a.hidden.fmt, at, at.own / 2 + k, h[0]);
+            else {
+                hidden.put(a.hidden.fmt, at, at.own + 2 * k, h[0]);
+                hidden.put(a.hidden.fmt, at, at.own + 2 * k + 1, h[1]);
+            }
+        }
+    }
+}
+
+template <typename T, typename P, bool GATED>
+__global__ __launch_bounds__(kThreads) void gradient_kernel(Gradient a) {
+    constexpr int W = GATED ? 4 : 8;
+    __shared__ __attribute__((aligned(16))) Columns<kTile> columns;
+    __shared__ __attribute__((aligned(16))) Columns<GATED ? kTile / 2 : kTile> hidden;
+    __shared__ float sums[GATED ? 1 : 4][kTile];
+    const int64_t tile_row = blockIdx.x / a.across, c0 = (blockIdx.x - tile_row * a.across) * kTile;
+    const Place at(tile_row * kTile, c0);
+    const int64_t own_col = GATED ? at.col / 2 : at.col;
+    Raw<P, 8> p;
+    Raw<T, W> dy;
+    float d[8][8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) dy.load(r, static_cast<const T*>(a.dy) + (at.row + r) * a.dy_pitch + own_col, at.row + r < a.rows ? a.cols - own_col : 0);
+    load_kept(a, at, p);
+    if (a.activation == SSGD_ACT_RELU) differentiate<SSGD_ACT_RELU, GATED>(a, at, p, dy, d, columns, hidden);
+    else if (a.activation == SSGD_ACT_GELU) differentiate<SSGD_ACT_GELU, GATED>(a, at, p, dy, d, columns, hidden);
+    else if (a.activation == SSGD_ACT_SILU) differentiate<SSGD_ACT_SILU, GATED>(a, at, p, dy, d, columns, hidden);
+    else differentiate<SSGD_ACT_NONE, GATED>(a, at, p, dy, d, columns, hidden);
     if (a.along.values != nullptr) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) store_along(a.along, at.row + r, at.col, at.row + r < a.rows, d[r]);
     }
-    if (a.columns.values != nullptr) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float x[8] = {d[0][q], d[1][q], d[2][q], d[3][q], d[4][q], d[5][q], d[6][q], d[7][q]};
-            store_column(a.columns, at, at.col + q, at.col + q < a.p_cols, x);
-        }
-    }
-    if (a.hidden.values != nullptr) {
-#pragma unroll
-        for (int q = 0; q < W; ++q) {
-            const float x[8] = {h[0][q], h[1][q], h[2][q], h[3][q], h[4][q], h[5][q], h[6][q], h[7][q]};
-            store_column(a.hidden, at, own_col + q, own_col + q < a.cols, x);
-        }
-    }
     if constexpr (!GATED) {
-        if (a.partial == nullptr) return;
-        const int lane = threadIdx.x & 63;
+        if (a.partial != nullptr) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            float sum = 0.0f;
+            for (int q = 0; q < 8; ++q) {
+                float sum = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) sum += d[r][q];
-            sum = sum_of_turns(sum);
-            if (at.turn == 0) sums[threadIdx.x >> 6][(lane >> 4) * 32 + (lane & 3) * 8 + q] = sum;
+                for (int r = 0; r < 8; ++r) sum += d[r][q];
+                sum = sum_of_rows(sum);
+                if (at.turn == 0) sums[at.wave][at.own + q] = sum;
+            }
         }
-        __syncthreads();
+    }
+    __syncthreads();
+    if (a.columns.values != nullptr) columns.store(a.columns, c0, a.p_cols, tile_row * kTile);
+    if (a.hidden.values != nullptr) hidden.store(a.hidden, GATED ? c0 / 2 : c0, a.cols, tile_row * kTile);
+    if constexpr (!GATED) {
         const int64_t col = c0 + threadIdx.x;
-        if (threadIdx.x < kTile && col < a.cols)
+        if (a.partial != nullptr && threadIdx.x < kTile && col < a.cols)
             a.partial[tile_row * a.cols + col] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
     }
 }
@@ -166,8 +246,9 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Gradient a) {
 template <int FMT>
 __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* values, const uint8_t* scales, int64_t row_bytes, int64_t scale_bytes, int64_t rows, int64_t cols, Target t,
                                                              int64_t across) {
-    const int64_t tile_row = blockIdx.x / across;
-    const Place at(tile_row * kTile, (blockIdx.x - tile_row * across) * kTile);
+    __shared__ __attribute__((aligned(16))) Columns<kTile> columns;
+    const int64_t tile_row = blockIdx.x / across, c0 = (blockIdx.x - tile_row * across) * kTile;
+    const Place at(tile_row * kTile, c0);
     float x[8][8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -185,8 +266,10 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* valu
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         const float y[8] = {x[0][q], x[1][q], x[2][q], x[3][q], x[4][q], x[5][q], x[6][q], x[7][q]};
-        store_column(t, at, at.col + q, at.col + q < cols, y);
+        columns.put(t.fmt, at, at.own + q, y);
     }
+    __syncthreads();
+    columns.store(t, c0, cols, tile_row * kTile);
 }
 
 bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
@@ -231,13 +314,14 @@ ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t d
             Gradient a{};
             a.dy = dy; a.p = p; a.p_values = static_cast<const uint8_t*>(p_values); a.p_scales = static_cast<const uint8_t*>(p_scales);
             a.rows = rows; a.cols = cols; a.p_cols = p_cols; a.dy_pitch = dy_pitch; a.p_pitch = p_pitch; a.p_bytes = mx_row_bytes(SSGD_MX_FP8, p_cols); a.p_scale_bytes = mx_padded(p_cols) / kMxBlock;
-            a.across = tiles_of(p_cols); a.p_bf16 = p_dtype == SSGD_BF16; a.activation = activation;
+            a.across = tiles_of(p_cols); a.p_bf16 = p == nullptr || p_dtype == SSGD_BF16; a.activation = activation;
             a.along = target_of(values, scales, fmt, p_cols); a.columns = target_of(values_t, scales_t, fmt_t, rows); a.hidden = target_of(values_h, scales_h, fmt_h, rows);
             a.partial = dbias != nullptr ? work : nullptr;
             const dim3 grid((unsigned)(tiles_of(rows) * a.across));
-#define SSGD_GRADIENT(T, G) hipLaunchKernelGGL((gradient_kernel<T, G>), grid, dim3(kThreads), 0, stream, a)
-            if (dtype == SSGD_F32) { if (gated) SSGD_GRADIENT(float, true); else SSGD_GRADIENT(float, false); }
-            else { if (gated) SSGD_GRADIENT(bf16_t, true); else SSGD_GRADIENT(bf16_t, false); }
+#define SSGD_GRADIENT(T, P) do { if (gated) hipLaunchKernelGGL((gradient_kernel<T, P, true>), grid, dim3(kThreads), 0, stream, a); \
+                                  else hipLaunchKernelGGL((gradient_kernel<T, P, false>), grid, dim3(kThreads), 0, stream, a); } while (0)
+            if (dtype == SSGD_F32) { if (p_values) SSGD_GRADIENT(float, Fp8); else if (a.p_bf16) SSGD_GRADIENT(float, bf16_t); else SSGD_GRADIENT(float, float); }
+            else { if (p_values) SSGD_GRADIENT(bf16_t, Fp8); else if (a.p_bf16) SSGD_GRADIENT(bf16_t, bf16_t); else SSGD_GRADIENT(bf16_t, float); }
 #undef SSGD_GRADIENT
         }
         if (dbias != nullptr) launch_column_sums(work, tiles_of(rows), cols, dbias, stream);

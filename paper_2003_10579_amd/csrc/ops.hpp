@@ -134,6 +134,15 @@ __device__ __forceinline__ uint32_t max_of_rows(uint32_t x) {
     const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return umax(b[0], b[1]);
 }
+// (a bit cast of a vector's element reads its first one: copies are taken)
+__device__ __forceinline__ float sum_of_two(uint32_t a, uint32_t b) { return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b); }
+__device__ __forceinline__ float sum_of_rows(float x) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t v = __builtin_bit_cast(uint32_t, sum_of_two(a[0], a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return sum_of_two(b[0], b[1]);
+}
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
 __device__ __forceinline__ float wave_sum(float x) {
