@@ -318,7 +318,7 @@ ssgd_status ssgd_mx_dense(const void *x, int32_t dtype, int64_t pitch, const voi
  *   dp = dy act'(p)      gated:   dp[m][2 c] = dy u act'(g),  dp[m][2 c + 1] = dy act(g),   g = p[m][2 c], u = p[m][2 c + 1]      (relu'(0) = 0)
  * Outputs, each nullable but one: dp quantised along its rows (values, scales in fmt) and along its columns (values_t, scales_t in fmt_t), for the products with the transposed
  * weight and with the layer's input; act(p), or the gated block's output, along its columns (values_h, scales_h in fmt_h), for the next weight's gradient; dbias
- * (fp32, not gated), the sum of dp over its rows.  work: ssgd_mx_activation_backward_work_floats floats, 16-byte aligned, used when dbias is given. */
+ * (fp32, not gated), the sum of dp over its rows.  rows < 2^31, columns of p up to 2^24 - 128.  work: ssgd_mx_activation_backward_work_floats floats, 16-byte aligned, used when dbias is given. */
 int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols);
 ssgd_status ssgd_mx_activation_backward(const void *dy, int32_t dtype, int64_t dy_pitch, int64_t rows, int64_t cols, int32_t gated, int32_t activation,
                                         const void *p, int32_t p_dtype, int64_t p_pitch, const void *p_values, const void *p_scales, int32_t fmt,

@@ -38,19 +38,25 @@ struct Place {
     }
 };
 
-// Eight columns of a row of the matrix that is quantised along its rows.
-__device__ __forceinline__ void store_along(const Target& t, int64_t row, int64_t col, bool live, const float (&x)[8]) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-    most = max_of_4(most);
-    const uint32_t byte = t.fmt == SSGD_MX_FP4 ? mx_scale_byte<SSGD_MX_FP4>(most) : mx_scale_byte<SSGD_MX_FP8>(most);
-    if (!live) return;
-    uint8_t* to = t.values + row * t.row_bytes;
-    if (t.fmt == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(to + col / 2) = mx_pack_fp4(x, byte);
-    else *reinterpret_cast<words2*>(to + col) = mx_pack_fp8(x, byte);
-    if ((threadIdx.x & 3) == 0) t.scales[row * t.scale_bytes + col / kMxBlock] = (uint8_t)byte;
-}
+// Eight columns of rows of the matrix that is quantised along its rows; `to`: the tile's first row (128 rows are less than 2^31 bytes).
+struct Along {
+    uint8_t *values, *scales;
+    uint32_t at, scale_at;
+    __device__ __forceinline__ Along(const Target& t, const Place& p, int64_t tile_row)
+        : values(t.values + tile_row * kTile * t.row_bytes), scales(t.scales + tile_row * kTile * t.scale_bytes),
+          at((uint32_t)(p.wave * 32 + p.turn * 8) * (uint32_t)t.row_bytes + (uint32_t)(t.fmt == SSGD_MX_FP4 ? p.col / 2 : p.col)),
+          scale_at((uint32_t)(p.wave * 32 + p.turn * 8) * (uint32_t)t.scale_bytes + (uint32_t)(p.col / kMxBlock)) {}
+    __device__ __forceinline__ void store(const Target& t, int r, bool live, const float (&x)[8]) const {
+        const uint32_t most = max_of_4(largest_of(x));
+        const uint32_t byte = t.fmt == SSGD_MX_FP4 ? mx_scale_byte<SSGD_MX_FP4>(most) : mx_scale_byte<SSGD_MX_FP8>(most);
+        if (!live) return;
+        const uint32_t to = at + (uint32_t)r * (uint32_t)t.row_bytes;
+        if (t.fmt == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(values + to) = mx_pack_fp4(x, byte);
+        else *reinterpret_cast<words2*>(values + to) = mx_pack_fp8_as_it_is(x, byte);
+        if ((threadIdx.x & 3) == 0) scales[scale_at + (uint32_t)r * (uint32_t)t.scale_bytes] = (uint8_t)byte;
+    }
+};
+
 // The columns of a tile, quantised, on their way to the transposed matrix: 128 rows of one are 128 or 64 bytes side by side there, of which a lane has eight or four
 // (stored by the lanes themselves, in pieces of 32 bytes: 8192 x 8192 pairs in 8 bits 227 us instead of 158).  The 16-byte parts of a column, and columns next to each
 // other, change places by the column's number, so that the lanes that write at a time, and those that read, meet in no bank.
@@ -61,17 +67,14 @@ template <int COLS> struct Columns {
     static __device__ __forceinline__ int part4(int col, int part) { return ((col ^ ((col >> 5) & 3)) * 4 + (part ^ ((col >> 3) & 3))) * 4; }
     // Eight rows of column `col` of the tile.
     __device__ __forceinline__ void put(int32_t fmt, const Place& at, int col, const float (&x)[8]) {
-        uint32_t most = 0;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-        most = max_of_rows(most);
+        const uint32_t most = max_of_rows(largest_of(x));
         uint32_t byte;
         if (fmt == SSGD_MX_FP4) {
             byte = mx_scale_byte<SSGD_MX_FP4>(most);
             values[part4(col, at.wave) + at.turn] = mx_pack_fp4(x, byte);
         } else {
             byte = mx_scale_byte<SSGD_MX_FP8>(most);
-            *reinterpret_cast<words2*>(&values[part8(col, at.wave * 2 + (at.turn >> 1)) + (at.turn & 1) * 2]) = mx_pack_fp8(x, byte);
+            *reinterpret_cast<words2*>(&values[part8(col, at.wave * 2 + (at.turn >> 1)) + (at.turn & 1) * 2]) = mx_pack_fp8_as_it_is(x, byte);
         }
         if (at.turn == 0) scales[col * 4 + at.wave] = (uint8_t)byte;
     }
@@ -96,6 +99,7 @@ struct Fp8 {};       // with scales
 template <typename T, int W> struct Raw;
 template <int W> struct Raw<float, W> {
     float x[8][W];
+    __device__ __forceinline__ void load_all(int r, const float* row) { load_vec<W>(row, W, x[r]); }
     __device__ __forceinline__ void load(int r, const float* row, int64_t left) { load_vec<W>(row, left, x[r]); }
     __device__ __forceinline__ void clear(int r) {
 #pragma unroll
@@ -105,16 +109,18 @@ template <int W> struct Raw<float, W> {
 };
 template <int W> struct Raw<bf16_t, W> {
     uint32_t x[8][W / 2];
-    __device__ __forceinline__ void load(int r, const bf16_t* row, int64_t left) {
-        if (left >= W) {
-            if constexpr (W == 8) {
-                const words4 v = *reinterpret_cast<const words4_any*>(row);
-                x[r][0] = v.x; x[r][1] = v.y; x[r][2] = v.z; x[r][3] = v.w;
-            } else {
-                const words2 v = *reinterpret_cast<const words2_any*>(row);
-                x[r][0] = v.x; x[r][1] = v.y;
-            }
+    __device__ __forceinline__ void load_all(int r, const bf16_t* row) {
+        if constexpr (W == 8) {
+            const words4 v = *reinterpret_cast<const words4_any*>(row);
+            x[r][0] = v.x; x[r][1] = v.y; x[r][2] = v.z; x[r][3] = v.w;
         } else {
+            const words2 v = *reinterpret_cast<const words2_any*>(row);
+            x[r][0] = v.x; x[r][1] = v.y;
+        }
+    }
+    __device__ __forceinline__ void load(int r, const bf16_t* row, int64_t left) {
+        if (left >= W) load_all(r, row);
+        else {
 #pragma unroll
             for (int k = 0; k < W / 2; ++k) x[r][k] = (2 * k < left ? (uint32_t)row[2 * k] : 0u) | (2 * k + 1 < left ? (uint32_t)row[2 * k + 1] << 16 : 0u);
         }
@@ -134,22 +140,45 @@ template <> struct Raw<Fp8, 8> {
         return f32x2{v.x * scale[r], v.y * scale[r]};
     }
 };
+// `whole`: all of the tile's rows and columns are there (a load that may be left out waits for those before it).
 template <typename P>
-__device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, Raw<P, 8>& p) {
+__device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, bool whole, Raw<P, 8>& p) {
+    if constexpr (std::is_same_v<P, Fp8>) {
+        uint32_t byte[8];
+        // (from the tile's first row on: 128 rows are less than 2^31 bytes)
+        const int64_t r0 = at.row - (at.wave * 32 + at.turn * 8);
+        const uint8_t *values = a.p_values + r0 * a.p_bytes, *scales = a.p_scales + r0 * a.p_scale_bytes;
+        const uint32_t pitch = (uint32_t)a.p_bytes, scale_pitch = (uint32_t)a.p_scale_bytes, row = (uint32_t)(at.wave * 32 + at.turn * 8);
+        const uint32_t from = row * pitch + (uint32_t)at.col, scale_from = row * scale_pitch + (uint32_t)(at.col / kMxBlock);
+        auto load = [&](int r) { byte[r] = scales[scale_from + r * scale_pitch]; p.x[r] = *reinterpret_cast<const words2*>(values + (from + r * pitch)); };
+        if (whole) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int64_t row = at.row + r;
-        if constexpr (std::is_same_v<P, Fp8>) {
-            p.x[r] = words2{0u, 0u};
-            uint32_t byte = 0;
-            if (row < a.rows) {
-                p.x[r] = *reinterpret_cast<const words2*>(a.p_values + row * a.p_bytes + at.col);
-                byte = a.p_scales[row * a.p_scale_bytes + at.col / kMxBlock];
+            for (int r = 0; r < 8; ++r) load(r);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                p.x[r] = words2{0u, 0u};
+                byte[r] = 0u;
+                if (at.row + r < a.rows) load(r);
             }
-            // (columns past the last one in a block that is NaN are NaN too: what the formulas make of them is what they make of the block's others)
-            p.scale[r] = mx_scale_value(byte);
-        } else if (a.p == nullptr) p.clear(r);
-        else p.load(r, static_cast<const P*>(a.p) + row * a.p_pitch + at.col, row < a.rows ? a.p_cols - at.col : 0);
+        }
+        // (columns past the last one in a block that is NaN are NaN too: what the formulas make of them is what they make of the block's others)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p.scale[r] = mx_scale_value(byte[r]);
+    } else {
+        if (a.p == nullptr) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) p.clear(r);
+            return;
+        }
+        const P* from = static_cast<const P*>(a.p) + at.row * a.p_pitch + at.col;
+        if (whole) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) p.load_all(r, from + r * a.p_pitch);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) p.load(r, from + r * a.p_pitch, at.row + r < a.rows ? a.p_cols - at.col : 0);
+        }
     }
 }
 
@@ -207,19 +236,28 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Gradient a) {
     const int64_t tile_row = blockIdx.x / a.across, c0 = (blockIdx.x - tile_row * a.across) * kTile;
     const Place at(tile_row * kTile, c0);
     const int64_t own_col = GATED ? at.col / 2 : at.col;
+    conversions_saturate();
     Raw<P, 8> p;
     Raw<T, W> dy;
     float d[8][8];
+    const bool whole = (tile_row + 1) * kTile <= a.rows && c0 + kTile <= a.p_cols;
+    const T* from = static_cast<const T*>(a.dy) + at.row * a.dy_pitch + own_col;
+    if (whole) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) dy.load(r, static_cast<const T*>(a.dy) + (at.row + r) * a.dy_pitch + own_col, at.row + r < a.rows ? a.cols - own_col : 0);
-    load_kept(a, at, p);
+        for (int r = 0; r < 8; ++r) dy.load_all(r, from + r * a.dy_pitch);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) dy.load(r, from + r * a.dy_pitch, at.row + r < a.rows ? a.cols - own_col : 0);
+    }
+    load_kept(a, at, whole, p);
     if (a.activation == SSGD_ACT_RELU) differentiate<SSGD_ACT_RELU, GATED>(a, at, p, dy, d, columns, hidden);
     else if (a.activation == SSGD_ACT_GELU) differentiate<SSGD_ACT_GELU, GATED>(a, at, p, dy, d, columns, hidden);
     else if (a.activation == SSGD_ACT_SILU) differentiate<SSGD_ACT_SILU, GATED>(a, at, p, dy, d, columns, hidden);
     else differentiate<SSGD_ACT_NONE, GATED>(a, at, p, dy, d, columns, hidden);
     if (a.along.values != nullptr) {
+        const Along to(a.along, at, tile_row);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) store_along(a.along, at.row + r, at.col, at.row + r < a.rows, d[r]);
+        for (int r = 0; r < 8; ++r) to.store(a.along, r, whole || at.row + r < a.rows, d[r]);
     }
     if constexpr (!GATED) {
         if (a.partial != nullptr) {
@@ -249,19 +287,27 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* valu
     __shared__ __attribute__((aligned(16))) Columns<kTile> columns;
     const int64_t tile_row = blockIdx.x / across, c0 = (blockIdx.x - tile_row * across) * kTile;
     const Place at(tile_row * kTile, c0);
+    conversions_saturate();
     float x[8][8];
+    uint32_t byte[8];
+    words2 w[8];
+    const uint8_t *from = values + at.row * row_bytes + (FMT == SSGD_MX_FP8 ? at.col : at.col / 2), *scale = scales + at.row * scale_bytes + at.col / kMxBlock;
+    auto load = [&](int r) {
+        byte[r] = scale[r * scale_bytes];
+        if constexpr (FMT == SSGD_MX_FP8) w[r] = *reinterpret_cast<const words2*>(from + r * row_bytes);
+        else w[r] = words2{*reinterpret_cast<const uint32_t*>(from + r * row_bytes), 0u};
+    };
+    if ((tile_row + 1) * kTile <= rows) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) load(r);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) { byte[r] = 0u; w[r] = words2{0u, 0u}; if (at.row + r < rows) load(r); }
+    }
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const int64_t row = at.row + r;
-        uint32_t byte = 0;
-        words2 w = {0u, 0u};
-        if (row < rows) {
-            byte = scales[row * scale_bytes + at.col / kMxBlock];
-            if constexpr (FMT == SSGD_MX_FP8) w = *reinterpret_cast<const words2*>(values + row * row_bytes + at.col);
-            else w.x = *reinterpret_cast<const uint32_t*>(values + row * row_bytes + at.col / 2);
-        }
-        if constexpr (FMT == SSGD_MX_FP8) mx_unpack_fp8(w, mx_scale_value(byte), x[r]);
-        else mx_unpack_fp4(w.x, mx_scale_value(byte), x[r]);
+        if constexpr (FMT == SSGD_MX_FP8) mx_unpack_fp8(w[r], mx_scale_value(byte[r]), x[r]);
+        else mx_unpack_fp4(w[r].x, mx_scale_value(byte[r]), x[r]);
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
@@ -273,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* valu
 }
 
 bool format_ok(int32_t f) { return f == SSGD_MX_FP4 || f == SSGD_MX_FP8; }
-constexpr int64_t kMost = int64_t(1) << 31, kMostSums = int64_t(1) << 25;
+constexpr int64_t kMost = int64_t(1) << 31, kMostColumns = (int64_t(1) << 24) - kMxPad;      // of p: what a product contracts
 bool target_ok(const void* values, const void* scales, int32_t fmt) {
     return (values != nullptr) == (scales != nullptr) && (values == nullptr || (format_ok(fmt) && aligned(values, 16) && aligned(scales, 16)));
 }
@@ -287,7 +333,7 @@ int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
 #pragma GCC visibility push(default)
 extern "C" {
 
-int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows >= kMost || cols >= kMostSums ? -1 : tiles_of(rows) * cols; }
+int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows >= kMost || cols > kMostColumns ? -1 : tiles_of(rows) * cols; }
 
 ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t dy_pitch, int64_t rows, int64_t cols, int32_t gated, int32_t activation, const void* p, int32_t p_dtype,
                                         int64_t p_pitch, const void* p_values, const void* p_scales, int32_t fmt, void* values, void* scales, int32_t fmt_t, void* values_t,
@@ -295,10 +341,10 @@ ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t d
     return op_entry([&]() -> ssgd_status {
         const char* name = "mx activation backward: ";
         auto no = [&](const char* what) { return op_fail(SSGD_EINVAL, (std::string(name) + what).c_str()); };
-        if (!dtype_ok(dtype) || rows < 0 || cols < 0 || rows >= kMost || cols >= kMost / 2) return no("a type of the enumeration, rows from zero to 2^31, columns to 2^30");
+        if (!dtype_ok(dtype) || rows < 0 || cols < 0 || rows >= kMost || cols > kMostColumns || (gated == 1 && 2 * cols > kMostColumns)) return no("a type of the enumeration, rows from zero to 2^31, columns of p to 2^24 - 128");
         if ((gated != 0 && gated != 1) || activation < SSGD_ACT_NONE || activation > SSGD_ACT_SILU) return no("an activation of the enumeration, gated or not");
         if (gated && dbias != nullptr) return no("a gated block has no bias");
-        if (dbias != nullptr && (cols >= kMostSums || !aligned(dbias, 4) || (rows > 0 && cols > 0 && (!work || !aligned(work, 16))))) return no("dbias needs less than 2^25 columns and a 16-byte aligned work area");
+        if (dbias != nullptr && (!aligned(dbias, 4) || (rows > 0 && cols > 0 && (!work || !aligned(work, 16))))) return no("dbias, a gradient of a bias, needs a 16-byte aligned work area");
         if (!target_ok(values, scales, fmt) || !target_ok(values_t, scales_t, fmt_t) || !target_ok(values_h, scales_h, fmt_h)) return no("outputs are 16-byte aligned arrays of values and scales, formats of the enumeration");
         const int64_t p_cols = gated ? 2 * cols : cols;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -145,6 +145,14 @@ __device__ __forceinline__ float sum_of_rows(float x) {
 }
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
+// Largest magnitude of eight numbers, as bits: two at a time, NaN carries.
+__device__ __forceinline__ uint32_t largest_of(const float (&x)[8]) {
+    float m = __builtin_elementwise_maximum(__builtin_fabsf(x[0]), __builtin_fabsf(x[1]));
+#pragma unroll
+    for (int q = 2; q < 8; q += 2) m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, __builtin_fabsf(x[q])), __builtin_fabsf(x[q + 1]));
+    return __builtin_bit_cast(uint32_t, m);
+}
+
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
@@ -189,6 +197,18 @@ __device__ __forceinline__ words2 mx_pack_fp8(const float (&x)[8], uint32_t byte
     shorts2 lo = {0, 0}, hi = {0, 0};
     lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[0], y[1], s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, y[2], y[3], s, true);
     hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[4], y[5], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[6], y[7], s, true);
+    return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+// The same by conversions that saturate by themselves, as they do with the mode's bit for it (FP16_OVFL) set: one instruction to a value less.
+__device__ __forceinline__ void conversions_saturate() {
+    __builtin_amdgcn_s_setreg(1 | 23 << 6, 1);          // one bit, at place 23, of register MODE
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ words2 mx_pack_fp8_as_it_is(const float (&x)[8], uint32_t byte) {
+    const float s = mx_scale_of(byte);
+    shorts2 lo = {0, 0}, hi = {0, 0};
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[0], x[1], s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[2], x[3], s, true);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, x[4], x[5], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, x[6], x[7], s, true);
     return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 __device__ __forceinline__ uint32_t mx_pack_fp8(float a, float b, float c, float d, uint32_t byte) {

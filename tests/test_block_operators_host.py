@@ -83,10 +83,10 @@ def test_mx_dense_work_bytes(L):
 
 @pytest.mark.parametrize("gated", [0, 1])
 @pytest.mark.parametrize("bad", [
-    dict(dy=None), dict(dy=A + 2), dict(dtype=2), dict(pitch=39), dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 30, pitch=1 << 30), dict(gated=2), dict(act=4), dict(act=-1), dict(p=None),
+    dict(dy=None), dict(dy=A + 2), dict(dtype=2), dict(pitch=39), dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 30, pitch=1 << 30), dict(cols=1 << 24, pitch=1 << 24, p_pitch=1 << 25), dict(gated=2), dict(act=4), dict(act=-1), dict(p=None),
     dict(p=A + 2), dict(p_dtype=3), dict(p_pitch=39), dict(p_values=A, p_scales=A), dict(p=None, p_values=A), dict(p=None, p_values=A + 8, p_scales=A), dict(p=None, p_values=A, p_scales=A + 8), dict(fmt=2),
     dict(fmt_t=-1), dict(fmt_h=2), dict(values=None), dict(scales=None), dict(values=A + 8), dict(scales=A + 8), dict(values_t=None), dict(scales_t=A + 4), dict(values_h=A + 4), dict(scales_h=None),
-    dict(values=None, scales=None, values_t=None, scales_t=None, values_h=None, scales_h=None), dict(rows=(1 << 31) - 1, cols=1 << 29, pitch=1 << 29, p_pitch=1 << 30),
+    dict(values=None, scales=None, values_t=None, scales_t=None, values_h=None, scales_h=None), dict(rows=(1 << 31) - 1, cols=1 << 22, pitch=1 << 22, p_pitch=1 << 23),
 ])
 def test_mx_activation_backward_refuses(L, bad, gated):
     g = lambda k, d: bad.get(k, d)  # noqa: E731
@@ -97,7 +97,7 @@ def test_mx_activation_backward_refuses(L, bad, gated):
 
 def test_mx_activation_backward_bias(L):
     call = lambda gated, cols, db, work: L.ssgd_mx_activation_backward(A, 0, cols, 10, cols, gated, 3, A, 0, 2 * cols, None, None, 1, A, A, 1, A, A, 0, None, None, db, work, None)  # noqa: E731
-    for args in ((1, 40, A, A), (0, 40, A, None), (0, 40, A, A + 8), (0, 40, A + 2, A), (0, 1 << 25, A, A)):
+    for args in ((1, 40, A, A), (0, 40, A, None), (0, 40, A, A + 8), (0, 40, A + 2, A)):
         _refused(L, call(*args), b"bias")
     floats = L.ssgd_mx_activation_backward_work_floats
     assert floats(0, 40) == 0 and floats(1, 40) == 40 and floats(129, 40) == 80 and floats(-1, 40) == -1 and floats(10, 1 << 25) == -1
