@@ -27,7 +27,7 @@ struct Forward {
     float *rstd_o, *rstd;
     int64_t rows, per_gate, chunk, o_pitch, s_pitch, sum_pitch, y_pitch, gate_pitch, row_bytes, scale_bytes;
     int32_t d, post_bf16, w_bf16, gate_bf16;
-    double scale, eps;
+    double scale, eps, per_column;        // per_column: 1 / d
 };
 
 struct Backward {
@@ -38,8 +38,10 @@ struct Backward {
     int64_t rows, per_gate, chunk, chunks, dy_pitch, o_pitch, sum_pitch, gate_pitch, dsum_pitch, grad_o_pitch, grad_s_pitch;
     int32_t d, post_bf16, w_bf16, gate_bf16;
     float scale;
+    double per_column;                    // 1 / d
 };
 
+// Sum over the threads of a row, in fp64.  A row has two of them with an array each, and all waves have read one when they meet for the other: one meeting to a sum.
 template <int LANES>
 __device__ __forceinline__ double team_sum(double x, double* part) {
     x = wave_sum(x);
@@ -49,7 +51,6 @@ __device__ __forceinline__ double team_sum(double x, double* part) {
         x = 0.0;
 #pragma unroll
         for (int q = 0; q < LANES / 64; ++q) x += part[q];
-        __syncthreads();
     }
     return x;
 }
@@ -64,7 +65,26 @@ __device__ __forceinline__ void load_row(const void* rows, int64_t row, int64_t 
 __device__ __forceinline__ float as_stored(const float*, float x) { return x; }
 __device__ __forceinline__ float as_stored(const bf16_t*, float x) { return bf16_to_f32(f32_to_bf16(x)); }
 
-__device__ __forceinline__ double inverse_root(double squares, int d, double eps) { return 1.0 / sqrt(squares / d + eps); }
+// (mean + eps)^(-1/2) from the sum of squares: an estimate of 2^-26 or so, and one step of Newton's that doubles its digits (a root and a quotient in fp64 are a hundred
+// instructions for every thread of a row).
+__device__ __forceinline__ double inverse_root(double squares, double per_column, double eps) {
+    const double x = __builtin_fma(squares, per_column, eps), r = __builtin_amdgcn_rsq(x);
+    const double better = __builtin_fma(r, __builtin_fma(-0.5 * x * r, r, 0.5), r);
+    return x > 0.0 && x < __builtin_inf() ? better : r;
+}
+
+// Eight columns of a row up to `end`, read and, when they have arrived, as numbers; SHORT: rows of less than eight columns are among them.
+template <bool SHORT, typename T>
+__device__ __forceinline__ void read(Eight<T>& to, const void* rows, int64_t row, int64_t pitch, int col, int end, int d) {
+    const T* from = static_cast<const T*>(rows) + row * pitch;
+    if (!SHORT || d >= 8) to.load(from, col, end);
+    else to.load_few(from, col, end);
+}
+template <bool SHORT, typename T>
+__device__ __forceinline__ void numbers(Eight<T>& x, int col, int end, int d, float (&to)[8]) {
+    if (!SHORT || d >= 8) x.settle(col, end);
+    x.numbers(to);
+}
 
 // w_post times the gate of a row: what the normalised output is multiplied by.
 __device__ __forceinline__ void factor_of(const Forward& a, int64_t gate, int col, double (&f)[8]) {
@@ -102,48 +122,74 @@ __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int 
     }
 }
 
+// (The weights and the gate stay in registers, and the next row is on its way while a row's sums are taken; sixteen columns to each of 1024 threads leave no registers
+// for either: they read both again for every row, from L2.)
 template <typename T, bool FP8, int LANES, int NV>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forward a) {
     constexpr int kRows = LANES == 64 ? 4 : 1;         // teams of a workgroup
-    __shared__ double part[LANES / 64];
+    constexpr bool kKept = LANES < 1024 || NV == 1, kShort = LANES == 64 && NV == 1;
+    __shared__ double part[2][LANES / 64];
     const int lane = threadIdx.x & (LANES - 1);
     const int64_t team = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES, first = team * a.chunk, end = first + a.chunk < a.rows ? first + a.chunk : a.rows;
     const int wide = FP8 ? (int)mx_padded(a.d) : a.d;
-    int64_t gate = -1;
+    int64_t gate = first / a.per_gate, next_gate = (gate + 1) * a.per_gate;
     double f[NV][8];
     float w[NV][8];
     auto col_of = [&](int v) { return (v * LANES + lane) * 8; };
+    auto end_of = [&](int v) { return v < NV - 1 ? col_of(v) + 8 : a.d; };          // (kernels with NV > 1 have rows that long)
+    Eight<T> next_o[NV], next_s[NV];
+    auto load = [&](int64_t row) {
+        if (row >= end) return;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_side(a.w, a.w_bf16, col_of(v), a.d - col_of(v), w[v]);
-    for (int64_t row = first; row < end; ++row) {
-        if (row / a.per_gate != gate) {
-            gate = row / a.per_gate;
+        for (int v = 0; v < NV; ++v) read<kShort>(next_o[v], a.o, row, a.o_pitch, col_of(v), end_of(v), a.d);
 #pragma unroll
-            for (int v = 0; v < NV; ++v) factor_of(a, gate, col_of(v), f[v]);
+        for (int v = 0; v < NV; ++v) read<kShort>(next_s[v], a.s, row, a.s_pitch, col_of(v), end_of(v), a.d);
+    };
+    if (first >= end) return;              // (the whole team; teams of several waves have their workgroup to themselves)
+    if constexpr (kKept) {
+        load(first);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+            factor_of(a, gate, col_of(v), f[v]);
         }
+    }
+    for (int64_t row = first; row < end; ++row) {
+        if (row == next_gate) {
+            ++gate;
+            next_gate += a.per_gate;
+            if constexpr (kKept) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) factor_of(a, gate, col_of(v), f[v]);
+            }
+        }
+        if constexpr (!kKept) load(row);
         float o[NV][8], s[NV][8];
         double squares = 0.0;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            load_row<T>(a.o, row, a.o_pitch, col_of(v), a.d, o[v]);
-            load_row<T>(a.s, row, a.s_pitch, col_of(v), a.d, s[v]);
+            numbers<kShort>(next_o[v], col_of(v), end_of(v), a.d, o[v]);
+            numbers<kShort>(next_s[v], col_of(v), end_of(v), a.d, s[v]);
         }
+        if constexpr (kKept) load(row + 1);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int q = 0; q < 8; ++q) squares += (double)o[v][q] * (double)o[v][q];
-        const double rstd_o = inverse_root(team_sum<LANES>(squares, part), a.d, a.eps);
+        const double rstd_o = inverse_root(team_sum<LANES>(squares, part[0]), a.per_column, a.eps);
         squares = 0.0;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            if constexpr (!kKept) factor_of(a, gate, col_of(v), f[v]);
             join<T>(a, o[v], s[v], f[v], rstd_o, o[v], squares);
-            store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col_of(v), a.d - col_of(v), o[v]);
+            store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col_of(v), end_of(v) - col_of(v), o[v]);
         }
-        const float rstd = (float)inverse_root(team_sum<LANES>(squares, part), a.d, a.eps);
+        const float rstd = (float)inverse_root(team_sum<LANES>(squares, part[1]), a.per_column, a.eps);
         if (lane == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (col_of(v) < wide) store_normed<T, FP8>(a, row, col_of(v), o[v], rstd, w[v]);
+            if constexpr (!kKept) load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+            if (v < NV - 1 || col_of(v) < wide) store_normed<T, FP8>(a, row, col_of(v), o[v], rstd, w[v]);
         }
     }
 }
@@ -151,7 +197,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
 // Rows that registers do not hold: o a second time, and the sum, which its own threads have written.
 template <typename T, bool FP8>
 __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
-    __shared__ double part[16];
+    __shared__ double part[2][16];
     const int wide = FP8 ? (int)mx_padded(a.d) : a.d;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t gate = row / a.per_gate;
@@ -162,7 +208,7 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) squares += (double)o[q] * (double)o[q];
         }
-        const double rstd_o = inverse_root(team_sum<1024>(squares, part), a.d, a.eps);
+        const double rstd_o = inverse_root(team_sum<1024>(squares, part[0]), a.per_column, a.eps);
         squares = 0.0;
         for (int col = threadIdx.x * 8; col < a.d; col += 8192) {
             float o[8], s[8];
@@ -173,7 +219,7 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
             join<T>(a, o, s, f, rstd_o, s, squares);
             store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
         }
-        const float rstd = (float)inverse_root(team_sum<1024>(squares, part), a.d, a.eps);
+        const float rstd = (float)inverse_root(team_sum<1024>(squares, part[1]), a.per_column, a.eps);
         if (threadIdx.x == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
         for (int col = threadIdx.x * 8; col < wide; col += 8192) {
             float s[8], w[8];
@@ -205,33 +251,61 @@ __device__ __forceinline__ void load_dsum(const Backward& a, int64_t row, int co
 template <typename T, int LANES, int NV>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Backward a) {
     constexpr int kRows = LANES == 64 ? 4 : 1;
-    __shared__ double part[LANES / 64];
+    constexpr bool kKept = LANES < 1024 || NV == 1, kShort = LANES == 64 && NV == 1;
+    __shared__ double part[2][LANES / 64];
     __shared__ float others[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? LANES * NV * 16 : 1];
     const int lane = threadIdx.x & (LANES - 1), team = threadIdx.x / LANES;
     const int64_t gate = blockIdx.x / a.chunks, begin = (blockIdx.x - gate * a.chunks) * a.chunk, rows = a.per_gate - begin < a.chunk ? a.per_gate - begin : a.chunk;
-    const int64_t first = gate * a.per_gate + begin;
+    const int64_t first = gate * a.per_gate + begin, end = first + rows;
     auto col_of = [&](int v) { return (v * LANES + lane) * 8; };
+    auto end_of = [&](int v) { return v < NV - 1 ? col_of(v) + 8 : a.d; };
     float w[NV][8], f[NV][8], dw[NV][8], S[NV][8];
+    auto load_sides = [&](int v) {
+        load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+        factor_of(a, gate, col_of(v), f[v]);
+    };
+    Eight<T> next_dy[NV], next_sum[NV], next_o[NV], next_more[NV];
+    float next_rstd = 0.0f, next_rstd_o = 0.0f;
+    auto load = [&](int64_t row) {
+        if (row >= end) return;
+        next_rstd = a.rstd[row];
+        next_rstd_o = a.rstd_o[row];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            read<kShort>(next_dy[v], a.dy, row, a.dy_pitch, col_of(v), end_of(v), a.d);
+            read<kShort>(next_sum[v], a.sum, row, a.sum_pitch, col_of(v), end_of(v), a.d);
+            read<kShort>(next_o[v], a.o, row, a.o_pitch, col_of(v), end_of(v), a.d);
+        }
+        if (a.dsum != nullptr) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) read<kShort>(next_more[v], a.dsum, row, a.dsum_pitch, col_of(v), end_of(v), a.d);
+        }
+    };
+    if constexpr (kKept) load(first + team);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_side(a.w, a.w_bf16, col_of(v), a.d - col_of(v), w[v]);
-        factor_of(a, gate, col_of(v), f[v]);
+        if constexpr (kKept) load_sides(v);
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[v][q] = S[v][q] = 0.0f;
     }
-    for (int64_t row = first + team; row < first + rows; row += kRows) {
-        const float rstd = a.rstd[row], rstd_o = a.rstd_o[row];
-        float g[NV][8], x[NV][8], more[NV][8], oh[NV][8];
+    for (int64_t row = first + team; row < end; row += kRows) {
+        if constexpr (!kKept) load(row);
+        const float rstd = next_rstd, rstd_o = next_rstd_o;
+        float g[NV][8], x[NV][8];
+        // (o and what is added past the sum stay as they came until they are used)
+        Eight<T> raw_o[NV], raw_more[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            load_row<T>(a.dy, row, a.dy_pitch, col_of(v), a.d, g[v]);
-            load_row<T>(a.sum, row, a.sum_pitch, col_of(v), a.d, x[v]);
-            load_row<T>(a.o, row, a.o_pitch, col_of(v), a.d, oh[v]);
-            load_dsum<T>(a, row, col_of(v), more[v]);
+            numbers<kShort>(next_dy[v], col_of(v), end_of(v), a.d, g[v]);
+            numbers<kShort>(next_sum[v], col_of(v), end_of(v), a.d, x[v]);
+            raw_o[v] = next_o[v];
+            if (a.dsum != nullptr) raw_more[v] = next_more[v];
         }
+        if constexpr (kKept) load(row + kRows);
         float sum = 0.0f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (!kKept) load_sides(v);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 x[v][q] *= rstd;
@@ -239,25 +313,36 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
                 g[v][q] *= w[v][q];
                 sum += g[v][q] * x[v][q];
             }
-        const float c = (float)(team_sum<LANES>((double)sum, part) / a.d);
+        }
+        const float c = (float)(team_sum<LANES>((double)sum, part[0]) * a.per_column);
         sum = 0.0f;
+        float oh[NV][8];
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            numbers<kShort>(raw_o[v], col_of(v), end_of(v), a.d, oh[v]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) g[v][q] = rstd * (g[v][q] - x[v][q] * c);
+            if (a.dsum != nullptr) {
+                numbers<kShort>(raw_more[v], col_of(v), end_of(v), a.d, x[v]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) g[v][q] += x[v][q];
+            }
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                g[v][q] = rstd * (g[v][q] - x[v][q] * c) + more[v][q];
                 oh[v][q] *= rstd_o;
                 S[v][q] += g[v][q] * oh[v][q];
                 x[v][q] = g[v][q] * f[v][q];
                 sum += x[v][q] * oh[v][q];
             }
-        const float c_o = (float)(team_sum<LANES>((double)sum, part) / a.d);
+        }
+        const float c_o = (float)(team_sum<LANES>((double)sum, part[1]) * a.per_column);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            if (v == NV - 1 && col_of(v) >= a.d) break;
 #pragma unroll
             for (int q = 0; q < 8; ++q) { oh[v][q] = rstd_o * (x[v][q] - oh[v][q] * c_o); g[v][q] *= a.scale; }
-            store_vec<8>(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col_of(v), a.d - col_of(v), oh[v]);
-            store_vec<8>(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col_of(v), a.d - col_of(v), g[v]);
+            store_vec<8>(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col_of(v), end_of(v) - col_of(v), oh[v]);
+            store_vec<8>(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col_of(v), end_of(v) - col_of(v), g[v]);
         }
     }
     if (a.dw_parts == nullptr) return;
@@ -285,15 +370,15 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        store_vec<8>(a.dw_parts + (int64_t)blockIdx.x * a.d + col_of(v), a.d - col_of(v), dw[v]);
-        store_vec<8>(a.s_parts + (int64_t)blockIdx.x * a.d + col_of(v), a.d - col_of(v), S[v]);
+        store_vec<8>(a.dw_parts + (int64_t)blockIdx.x * a.d + col_of(v), end_of(v) - col_of(v), dw[v]);
+        store_vec<8>(a.s_parts + (int64_t)blockIdx.x * a.d + col_of(v), end_of(v) - col_of(v), S[v]);
     }
 }
 
 // The same for rows that registers do not hold: what is read is read again for each sum, and the unit's sums are read and written for every row.
 template <typename T>
 __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
-    __shared__ double part[16];
+    __shared__ double part[2][16];
     const int64_t gate = blockIdx.x / a.chunks, begin = (blockIdx.x - gate * a.chunks) * a.chunk, rows = a.per_gate - begin < a.chunk ? a.per_gate - begin : a.chunk;
     const int64_t first = gate * a.per_gate + begin;
     for (int64_t row = first; row < first + rows; ++row) {
@@ -309,7 +394,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             for (int q = 0; q < 8; ++q) few += g[q] * w[q] * (x[q] * rstd);
             sum += few;
         }
-        const float c = (float)(team_sum<1024>(sum, part) / a.d);
+        const float c = (float)(team_sum<1024>(sum, part[0]) * a.per_column);
         // G and what is multiplied with it, of eight columns
         auto gradient = [&](int col, float (&g)[8], float (&oh)[8], float (&f)[8], float (&dw)[8]) {
             float x[8], w[8], more[8];
@@ -336,7 +421,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             for (int q = 0; q < 8; ++q) few += g[q] * f[q] * oh[q];
             sum += few;
         }
-        const float c_o = (float)(team_sum<1024>(sum, part) / a.d);
+        const float c_o = (float)(team_sum<1024>(sum, part[1]) * a.per_column);
         for (int col = threadIdx.x * 8; col < a.d; col += 8192) {
             float g[8], oh[8], f[8], dw[8], S[8], x[8];
             gradient(col, g, oh, f, dw);
@@ -499,7 +584,7 @@ ssgd_status ssgd_block_norm(const void* o, int64_t o_pitch, const void* s, int64
         a.values = static_cast<uint8_t*>(values); a.scales = static_cast<uint8_t*>(scales); a.rstd_o = rstd_o; a.rstd = rstd;
         a.rows = rows; a.per_gate = gate != nullptr ? rows / gates : rows; a.o_pitch = o_pitch; a.s_pitch = s_pitch; a.sum_pitch = sum_pitch; a.y_pitch = y_pitch; a.gate_pitch = gate_pitch;
         a.row_bytes = mx_row_bytes(SSGD_MX_FP8, d); a.scale_bytes = mx_padded(d) / kMxBlock;
-        a.d = (int32_t)d; a.post_bf16 = post_dtype == SSGD_BF16; a.w_bf16 = weight_dtype == SSGD_BF16; a.gate_bf16 = gate_dtype == SSGD_BF16; a.scale = scale; a.eps = eps;
+        a.d = (int32_t)d; a.post_bf16 = post_dtype == SSGD_BF16; a.w_bf16 = weight_dtype == SSGD_BF16; a.gate_bf16 = gate_dtype == SSGD_BF16; a.scale = scale; a.eps = eps; a.per_column = 1.0 / (double)d;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
         if (dtype == SSGD_F32) { if (values) launch_forward<float, true>(a, stream); else launch_forward<float, false>(a, stream); }
         else { if (values) launch_forward<bf16_t, true>(a, stream); else launch_forward<bf16_t, false>(a, stream); }
@@ -538,7 +623,7 @@ ssgd_status ssgd_block_norm_backward(const void* dy, int64_t dy_pitch, const voi
             a.dw_parts = dpost ? work : nullptr; a.s_parts = dpost ? work + units * d : nullptr;
             a.rows = rows; a.per_gate = per_gate; a.chunk = chunk; a.chunks = (per_gate + chunk - 1) / chunk;
             a.dy_pitch = dy_pitch; a.o_pitch = o_pitch; a.sum_pitch = sum_pitch; a.gate_pitch = gate_pitch; a.dsum_pitch = dsum_pitch; a.grad_o_pitch = grad_o_pitch; a.grad_s_pitch = grad_s_pitch;
-            a.d = (int32_t)d; a.post_bf16 = post_dtype == SSGD_BF16; a.w_bf16 = weight_dtype == SSGD_BF16; a.gate_bf16 = gate_dtype == SSGD_BF16; a.scale = (float)scale;
+            a.d = (int32_t)d; a.post_bf16 = post_dtype == SSGD_BF16; a.w_bf16 = weight_dtype == SSGD_BF16; a.gate_bf16 = gate_dtype == SSGD_BF16; a.scale = (float)scale; a.per_column = 1.0 / (double)d;
             if (dtype == SSGD_F32) launch_backward<float>(a, units, stream); else launch_backward<bf16_t>(a, units, stream);
         }
         ssgd_status st = op_hip(hipGetLastError(), "block norm backward");
