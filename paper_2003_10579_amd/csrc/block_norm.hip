@@ -41,10 +41,28 @@ struct Backward {
     double per_column;                    // 1 / d
 };
 
-// Sum over the threads of a row, in fp64.  A row has two of them with an array each, and all waves have read one when they meet for the other: one meeting to a sum.
+// Sum over the threads of a row, in fp64, by moves between lanes that do not go through LDS.  A row has two of them with an array each, and all waves have read one when
+// they meet for the other: one meeting to a sum.
+template <int CTRL>
+__device__ __forceinline__ double plus_moved(double x) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, x);
+    const uint64_t v = (uint64_t)dpp<CTRL>((uint32_t)(w >> 32)) << 32 | dpp<CTRL>((uint32_t)w);
+    return x + __builtin_bit_cast(double, v);
+}
+__device__ __forceinline__ double sum_of_pair(uint32_t lo0, uint32_t hi0, uint32_t lo1, uint32_t hi1) {
+    return __builtin_bit_cast(double, (uint64_t)hi0 << 32 | lo0) + __builtin_bit_cast(double, (uint64_t)hi1 << 32 | lo1);
+}
+__device__ __forceinline__ double sum_of_wave(double x) {
+    x = plus_moved<kMirror>(plus_moved<kHalfMirror>(plus_moved<kXor2>(plus_moved<kXor1>(x))));
+    uint64_t w = __builtin_bit_cast(uint64_t, x);
+    const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)w, (uint32_t)w, false, false), hi = __builtin_amdgcn_permlane16_swap((uint32_t)(w >> 32), (uint32_t)(w >> 32), false, false);
+    w = __builtin_bit_cast(uint64_t, sum_of_pair(lo[0], hi[0], lo[1], hi[1]));
+    const auto lo2 = __builtin_amdgcn_permlane32_swap((uint32_t)w, (uint32_t)w, false, false), hi2 = __builtin_amdgcn_permlane32_swap((uint32_t)(w >> 32), (uint32_t)(w >> 32), false, false);
+    return sum_of_pair(lo2[0], hi2[0], lo2[1], hi2[1]);
+}
 template <int LANES>
 __device__ __forceinline__ double team_sum(double x, double* part) {
-    x = wave_sum(x);
+    x = sum_of_wave(x);
     if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
         __syncthreads();
@@ -53,6 +71,16 @@ __device__ __forceinline__ double team_sum(double x, double* part) {
         for (int q = 0; q < LANES / 64; ++q) x += part[q];
     }
     return x;
+}
+// The sum of squares of a row's numbers.  (In fp64 from the squares on: what is a unit of 2^-24 off in rstd_o is one in the sum that is rounded.)
+template <int LANES, int NV>
+__device__ __forceinline__ double sum_of_squares(const float (&x)[NV][8], double* part) {
+    double sum = 0.0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum += (double)x[v][q] * (double)x[v][q];
+    return team_sum<LANES>(sum, part);
 }
 
 __device__ __forceinline__ void load_side(const void* w, int bf16, int64_t at, int64_t left, float (&x)[8]) {
@@ -98,12 +126,9 @@ __device__ __forceinline__ void factor_of(const Forward& a, int64_t gate, int co
     for (int q = 0; q < 8; ++q) f[q] *= x[q];
 }
 template <typename T>
-__device__ __forceinline__ void join(const Forward& a, const float (&o)[8], const float (&s)[8], const double (&f)[8], double rstd_o, float (&sum)[8], double& squares) {
+__device__ __forceinline__ void join(const Forward& a, const float (&o)[8], const float (&s)[8], const double (&f)[8], double rstd_o, float (&sum)[8]) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        sum[q] = as_stored(static_cast<const T*>(nullptr), (float)((double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q]));
-        squares += (double)sum[q] * (double)sum[q];
-    }
+    for (int q = 0; q < 8; ++q) sum[q] = as_stored(static_cast<const T*>(nullptr), (float)((double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q]));
 }
 template <typename T, bool FP8>
 __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, const float (&s)[8], float rstd, const float (&w)[8]) {
@@ -165,26 +190,20 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
         }
         if constexpr (!kKept) load(row);
         float o[NV][8], s[NV][8];
-        double squares = 0.0;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             numbers<kShort>(next_o[v], col_of(v), end_of(v), a.d, o[v]);
             numbers<kShort>(next_s[v], col_of(v), end_of(v), a.d, s[v]);
         }
         if constexpr (kKept) load(row + 1);
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) squares += (double)o[v][q] * (double)o[v][q];
-        const double rstd_o = inverse_root(team_sum<LANES>(squares, part[0]), a.per_column, a.eps);
-        squares = 0.0;
+        const double rstd_o = inverse_root(sum_of_squares<LANES, NV>(o, part[0]), a.per_column, a.eps);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if constexpr (!kKept) factor_of(a, gate, col_of(v), f[v]);
-            join<T>(a, o[v], s[v], f[v], rstd_o, o[v], squares);
+            join<T>(a, o[v], s[v], f[v], rstd_o, o[v]);
             store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col_of(v), end_of(v) - col_of(v), o[v]);
         }
-        const float rstd = (float)inverse_root(team_sum<LANES>(squares, part[1]), a.per_column, a.eps);
+        const float rstd = (float)inverse_root(sum_of_squares<LANES, NV>(o, part[1]), a.per_column, a.eps);
         if (lane == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -216,7 +235,9 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
             load_row<T>(a.o, row, a.o_pitch, col, a.d, o);
             load_row<T>(a.s, row, a.s_pitch, col, a.d, s);
             factor_of(a, gate, col, f);
-            join<T>(a, o, s, f, rstd_o, s, squares);
+            join<T>(a, o, s, f, rstd_o, s);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) squares += (double)s[q] * (double)s[q];
             store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
         }
         const float rstd = (float)inverse_root(team_sum<1024>(squares, part[1]), a.per_column, a.eps);
