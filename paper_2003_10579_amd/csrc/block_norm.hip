@@ -521,7 +521,10 @@ __global__ __launch_bounds__(1024) void sums_kernel(Sums a) {
     a.dw_post[col] = (float)sum;
 }
 
-int lanes_for(int64_t d) { return d <= 1024 ? 64 : (d <= 2048 ? 256 : (d <= 4096 ? 512 : 1024)); }
+// Threads of a row.  (16384 x 4096 in bf16, forward: 256 with sixteen columns each 97 us, 512 with eight 106; backward, which has more to keep: 173 and 171.  4000 x 8192,
+// 512 and 1024: 50 us either way, 96 and 104.)
+int lanes_for(int64_t d) { return d <= 1024 ? 64 : (d <= 4096 ? 256 : (d <= 8192 ? 512 : 1024)); }
+int lanes_backward(int64_t d) { return d <= 1024 ? 64 : (d <= 2048 ? 256 : (d <= 8192 ? 512 : 1024)); }
 
 template <typename T, bool FP8>
 void launch_forward(Forward a, hipStream_t s) {
@@ -538,16 +541,16 @@ void launch_forward(Forward a, hipStream_t s) {
     if (a.d <= 512) hipLaunchKernelGGL((forward_kernel<T, FP8, 64, 1>), grid, group, 0, s, a);
     else if (a.d <= 1024) hipLaunchKernelGGL((forward_kernel<T, FP8, 64, 2>), grid, group, 0, s, a);
     else if (a.d <= 2048) hipLaunchKernelGGL((forward_kernel<T, FP8, 256, 1>), grid, group, 0, s, a);
-    else if (a.d <= 4096) hipLaunchKernelGGL((forward_kernel<T, FP8, 512, 1>), grid, group, 0, s, a);
-    else if (a.d <= 8192) hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 1>), grid, group, 0, s, a);
+    else if (a.d <= 4096) hipLaunchKernelGGL((forward_kernel<T, FP8, 256, 2>), grid, group, 0, s, a);
+    else if (a.d <= 8192) hipLaunchKernelGGL((forward_kernel<T, FP8, 512, 2>), grid, group, 0, s, a);
     else hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 2>), grid, group, 0, s, a);
 }
 
 // Rows of a unit: as many units as are resident, at most 64 rows to a team, whose sums are in fp32.
 constexpr int64_t kChain = 64;
 int64_t chunk_for(int64_t rows, int64_t per_gate, int64_t d) {
-    const int lanes = lanes_for(d);
-    const int64_t teams = lanes == 64 ? 4 : 1, most = lanes == 1024 ? 256 : (lanes == 512 ? 512 : 1024);
+    const int lanes = lanes_backward(d);
+    const int64_t teams = lanes == 64 ? 4 : 1, most = d > 4096 ? 256 : (d > 2048 ? 512 : 1024);
     int64_t chunk = (rows + most - 1) / most;
     if (chunk < teams) chunk = teams;
     if (chunk > kChain * teams) chunk = kChain * teams;
@@ -561,14 +564,14 @@ int64_t units_for(int64_t rows, int64_t per_gate, int64_t d) {
 
 template <typename T>
 void launch_backward(const Backward& a, int64_t units, hipStream_t s) {
-    const int lanes = lanes_for(a.d);
+    const int lanes = lanes_backward(a.d);
     const dim3 grid((unsigned)units), group(lanes == 64 ? 256 : lanes);
     if (a.d > kMostKept) hipLaunchKernelGGL((backward_long_kernel<T>), grid, dim3(1024), 0, s, a);
     else if (a.d <= 512) hipLaunchKernelGGL((backward_kernel<T, 64, 1>), grid, group, 0, s, a);
     else if (a.d <= 1024) hipLaunchKernelGGL((backward_kernel<T, 64, 2>), grid, group, 0, s, a);
     else if (a.d <= 2048) hipLaunchKernelGGL((backward_kernel<T, 256, 1>), grid, group, 0, s, a);
     else if (a.d <= 4096) hipLaunchKernelGGL((backward_kernel<T, 512, 1>), grid, group, 0, s, a);
-    else if (a.d <= 8192) hipLaunchKernelGGL((backward_kernel<T, 1024, 1>), grid, group, 0, s, a);
+    else if (a.d <= 8192) hipLaunchKernelGGL((backward_kernel<T, 512, 2>), grid, group, 0, s, a);
     else hipLaunchKernelGGL((backward_kernel<T, 1024, 2>), grid, group, 0, s, a);
 }
 

@@ -833,6 +833,10 @@ def _gate(gate, rows, d, dev, what):
     """(pointer, type, number, pitch) of a gate per column (d), or of one for each of several runs of rows (gates x d)."""
     if gate is None:
         return None, 0, 1, 0
+    if gate.dim() == 1 and gate.numel() == d and gate.is_contiguous() and gate.device == dev:
+        if gate.requires_grad and _torch.is_grad_enabled():
+            _unrecorded(what)
+        return gate.data_ptr(), _dtype(gate.dtype), 1, d
     if not (gate.shape == (d,) or (gate.dim() == 2 and gate.shape[1] == d and gate.shape[0] > 0 and rows % gate.shape[0] == 0)) or gate.device != dev:
         _refuse(f"{what}: a gate per column, or one for each of several equal runs of rows, is wanted")
     _, kind, gates, _, pitch = _matrix(gate if gate.dim() == 2 else gate.unsqueeze(0), what)
@@ -850,17 +854,16 @@ def block_norm(o, s, post_weight, weight, gate=None, scale=1.0, eps=1e-6, output
     post, post_kind = _weight(post_weight, o, "block_norm")
     w, w_kind = _weight(weight, o, "block_norm")
     gate_at, gate_kind, gates, gate_pitch = _gate(gate, rows, d, dev, "block_norm")
-    total, stds = _torch.empty(rows, d, dtype=o.dtype, device=dev), _torch.empty(2, rows, dtype=_torch.float32, device=dev)
+    total, rstd_o, rstd = _torch.empty(rows, d, dtype=o.dtype, device=dev), _torch.empty(rows, dtype=_torch.float32, device=dev), _torch.empty(rows, dtype=_torch.float32, device=dev)
     if output is None:
         y = _torch.empty(rows, d, dtype=o.dtype, device=dev)
         to = (y.data_ptr(), d, None, None)
     else:
         y = MxTensor.empty(rows, d, "fp8", dev)
         to = (None, 0, *y._at)
-    at = stds.data_ptr()
     _call(_lib.ssgd_block_norm, dev, o.data_ptr(), pitch, s_at, s_pitch, post, post_kind, w, w_kind, gate_at, gate_kind, gates, gate_pitch, scale, eps, kind, rows, d,
-          total.data_ptr(), d, *to, at, at + 4 * rows)
-    return y, total, stds[0], stds[1]
+          total.data_ptr(), d, *to, rstd_o.data_ptr(), rstd.data_ptr())
+    return y, total, rstd_o, rstd
 
 
 def block_norm_backward(dy, o, sum, post_weight, weight, rstd_o, rstd, gate=None, scale=1.0, dsum=None):
@@ -877,14 +880,13 @@ def block_norm_backward(dy, o, sum, post_weight, weight, rstd_o, rstd, gate=None
             _refuse("block_norm_backward: one float32 rstd per row of both norms is wanted")
     gate_at, gate_kind, gates, gate_pitch = _gate(gate, rows, d, dev, "block_norm_backward")
     grad_o, grad_s = _torch.empty(rows, d, dtype=dy.dtype, device=dev), _torch.empty(rows, d, dtype=dy.dtype, device=dev)
-    sides = _torch.empty(2, d, dtype=_torch.float32, device=dev)
+    dpost, dw = _torch.empty(d, dtype=_torch.float32, device=dev), _torch.empty(d, dtype=_torch.float32, device=dev)
     dgate = None if gate is None else _torch.empty(gate.shape, dtype=_torch.float32, device=dev)
     floats = _lib.ssgd_block_norm_work_floats(rows, d, gates)
     if floats < 0:
         _refuse("block_norm_backward: rows < 2^31, 1 <= columns < 2^24")
     work = _torch.empty(floats, dtype=_torch.float32, device=dev)
-    at = sides.data_ptr()
     _call(_lib.ssgd_block_norm_backward, dev, dy.data_ptr(), pitch, o_at, o_pitch, sum_at, sum_pitch, post, post_kind, w, w_kind, gate_at, gate_kind, gates, gate_pitch, scale,
-          rstd_o.data_ptr(), rstd.data_ptr(), more, more_pitch, kind, rows, d, grad_o.data_ptr(), d, grad_s.data_ptr(), d, at, at + 4 * d, None if dgate is None else dgate.data_ptr(),
+          rstd_o.data_ptr(), rstd.data_ptr(), more, more_pitch, kind, rows, d, grad_o.data_ptr(), d, grad_s.data_ptr(), d, dpost.data_ptr(), dw.data_ptr(), None if dgate is None else dgate.data_ptr(),
           work.data_ptr())
-    return grad_o, grad_s, sides[0], sides[1], dgate
+    return grad_o, grad_s, dpost, dw, dgate
