@@ -140,10 +140,10 @@ __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int 
 #pragma unroll
         for (int q = 0; q < 8; ++q) most = umax(most, magnitude(y[q]));
         const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
-        *reinterpret_cast<words2*>(a.values + row * a.row_bytes + col) = mx_pack_fp8(y, byte);
+        __builtin_nontemporal_store(mx_pack_fp8(y, byte), reinterpret_cast<words2*>(a.values + row * a.row_bytes + col));
         if ((threadIdx.x & 3) == 0) a.scales[row * a.scale_bytes + col / kMxBlock] = (uint8_t)byte;
     } else {
-        store_vec<8>(static_cast<T*>(a.y) + row * a.y_pitch + col, a.d - col, y);
+        stream_vec(static_cast<T*>(a.y) + row * a.y_pitch + col, a.d - col, y);
     }
 }
 
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
         for (int v = 0; v < NV; ++v) {
             if constexpr (!kKept) factor_of(a, gate, col_of(v), f[v]);
             join<T>(a, o[v], s[v], f[v], rstd_o, o[v]);
-            store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col_of(v), end_of(v) - col_of(v), o[v]);
+            stream_vec(static_cast<T*>(a.sum) + row * a.sum_pitch + col_of(v), end_of(v) - col_of(v), o[v]);
         }
         const float rstd = (float)inverse_root(sum_of_squares<LANES, NV>(o, part[1]), a.per_column, a.eps);
         if (lane == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
             join<T>(a, o, s, f, rstd_o, s);
 #pragma unroll
             for (int q = 0; q < 8; ++q) squares += (double)s[q] * (double)s[q];
-            store_vec<8>(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
+            stream_vec(static_cast<T*>(a.sum) + row * a.sum_pitch + col, a.d - col, s);
         }
         const float rstd = (float)inverse_root(team_sum<1024>(squares, part[1]), a.per_column, a.eps);
         if (threadIdx.x == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
@@ -362,8 +362,8 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
             if (v == NV - 1 && col_of(v) >= a.d) break;
 #pragma unroll
             for (int q = 0; q < 8; ++q) { oh[v][q] = rstd_o * (x[v][q] - oh[v][q] * c_o); g[v][q] *= a.scale; }
-            store_vec<8>(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col_of(v), end_of(v) - col_of(v), oh[v]);
-            store_vec<8>(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col_of(v), end_of(v) - col_of(v), g[v]);
+            stream_vec(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col_of(v), end_of(v) - col_of(v), oh[v]);
+            stream_vec(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col_of(v), end_of(v) - col_of(v), g[v]);
         }
     }
     if (a.dw_parts == nullptr) return;
@@ -448,8 +448,8 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             gradient(col, g, oh, f, dw);
 #pragma unroll
             for (int q = 0; q < 8; ++q) { S[q] = g[q] * oh[q]; x[q] = rstd_o * (g[q] * f[q] - oh[q] * c_o); g[q] *= a.scale; }
-            store_vec<8>(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col, a.d - col, x);
-            store_vec<8>(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col, a.d - col, g);
+            stream_vec(static_cast<T*>(a.grad_o) + row * a.grad_o_pitch + col, a.d - col, x);
+            stream_vec(static_cast<T*>(a.grad_s) + row * a.grad_s_pitch + col, a.d - col, g);
             if (a.dw_parts == nullptr) continue;
             float *dw_to = a.dw_parts + (int64_t)blockIdx.x * a.d + col, *s_to = a.s_parts + (int64_t)blockIdx.x * a.d + col;
             if (row > first) {

@@ -52,7 +52,7 @@ struct Along {
         if (!live) return;
         const uint32_t to = at + (uint32_t)r * (uint32_t)t.row_bytes;
         if (t.fmt == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(values + to) = mx_pack_fp4(x, byte);
-        else *reinterpret_cast<words2*>(values + to) = mx_pack_fp8_as_it_is(x, byte);
+        else __builtin_nontemporal_store(mx_pack_fp8_as_it_is(x, byte), reinterpret_cast<words2*>(values + to));
         if ((threadIdx.x & 3) == 0) scales[scale_at + (uint32_t)r * (uint32_t)t.scale_bytes] = (uint8_t)byte;
     }
 };
@@ -86,7 +86,7 @@ template <int COLS> struct Columns {
             const int col = u >> shift, part = u & (parts - 1);
             if (first + col >= rows) continue;
             const words4 w = *reinterpret_cast<const words4*>(&values[t.fmt == SSGD_MX_FP4 ? part4(col, part) : part8(col, part)]);
-            *reinterpret_cast<words4*>(t.values + (first + col) * t.row_bytes + at + part * 16) = w;
+            __builtin_nontemporal_store(w, reinterpret_cast<words4*>(t.values + (first + col) * t.row_bytes + at + part * 16));
         }
         if ((int)threadIdx.x < COLS && first + threadIdx.x < rows)
             *reinterpret_cast<uint32_t*>(t.scales + (first + threadIdx.x) * t.scale_bytes + r0 / kMxBlock) = *reinterpret_cast<const uint32_t*>(&scales[threadIdx.x * 4]);
@@ -333,7 +333,7 @@ int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
 #pragma GCC visibility push(default)
 extern "C" {
 
-int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows >= kMost || cols > kMostColumns ? -1 : tiles_of(rows) * cols; }
+int64_t ssgd_mx_activation_backward_work_floats(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows >= kMost || cols > kMostColumns ? -1 : (rows <= kTile && rows > 0 ? 0 : tiles_of(rows) * cols); }      // (one tile of rows leaves its sums where they belong)
 
 ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t dy_pitch, int64_t rows, int64_t cols, int32_t gated, int32_t activation, const void* p, int32_t p_dtype,
                                         int64_t p_pitch, const void* p_values, const void* p_scales, int32_t fmt, void* values, void* scales, int32_t fmt_t, void* values_t,
@@ -344,7 +344,7 @@ ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t d
         if (!dtype_ok(dtype) || rows < 0 || cols < 0 || rows >= kMost || cols > kMostColumns || (gated == 1 && 2 * cols > kMostColumns)) return no("a type of the enumeration, rows from zero to 2^31, columns of p to 2^24 - 128");
         if ((gated != 0 && gated != 1) || activation < SSGD_ACT_NONE || activation > SSGD_ACT_SILU) return no("an activation of the enumeration, gated or not");
         if (gated && dbias != nullptr) return no("a gated block has no bias");
-        if (dbias != nullptr && (!aligned(dbias, 4) || (rows > 0 && cols > 0 && (!work || !aligned(work, 16))))) return no("dbias, a gradient of a bias, needs a 16-byte aligned work area");
+        if (dbias != nullptr && (!aligned(dbias, 4) || (rows > kTile && cols > 0 && (!work || !aligned(work, 16))))) return no("dbias, a gradient of a bias, needs a 16-byte aligned work area");
         if (!target_ok(values, scales, fmt) || !target_ok(values_t, scales_t, fmt_t) || !target_ok(values_h, scales_h, fmt_h)) return no("outputs are 16-byte aligned arrays of values and scales, formats of the enumeration");
         const int64_t p_cols = gated ? 2 * cols : cols;
         const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -362,7 +362,7 @@ ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t d
             a.rows = rows; a.cols = cols; a.p_cols = p_cols; a.dy_pitch = dy_pitch; a.p_pitch = p_pitch; a.p_bytes = mx_row_bytes(SSGD_MX_FP8, p_cols); a.p_scale_bytes = mx_padded(p_cols) / kMxBlock;
             a.across = tiles_of(p_cols); a.p_bf16 = p == nullptr || p_dtype == SSGD_BF16; a.activation = activation;
             a.along = target_of(values, scales, fmt, p_cols); a.columns = target_of(values_t, scales_t, fmt_t, rows); a.hidden = target_of(values_h, scales_h, fmt_h, rows);
-            a.partial = dbias != nullptr ? work : nullptr;
+            a.partial = dbias != nullptr && rows > kTile ? work : dbias;
             const dim3 grid((unsigned)(tiles_of(rows) * a.across));
 #define SSGD_GRADIENT(T, P) do { if (gated) hipLaunchKernelGGL((gradient_kernel<T, P, true>), grid, dim3(kThreads), 0, stream, a); \
                                   else hipLaunchKernelGGL((gradient_kernel<T, P, false>), grid, dim3(kThreads), 0, stream, a); } while (0)
@@ -370,7 +370,7 @@ ssgd_status ssgd_mx_activation_backward(const void* dy, int32_t dtype, int64_t d
             else { if (p_values) SSGD_GRADIENT(bf16_t, Fp8); else if (a.p_bf16) SSGD_GRADIENT(bf16_t, bf16_t); else SSGD_GRADIENT(bf16_t, float); }
 #undef SSGD_GRADIENT
         }
-        if (dbias != nullptr) launch_column_sums(work, tiles_of(rows), cols, dbias, stream);
+        if (dbias != nullptr && (rows > kTile || rows == 0)) launch_column_sums(work, tiles_of(rows), cols, dbias, stream);
         return op_hip(hipGetLastError(), "mx activation backward");
     });
 }

@@ -54,10 +54,13 @@ struct Common {
             for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
             const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
             if (live && n < h.value_bytes) {
-                *reinterpret_cast<words2*>(h.values + m * h.value_bytes + n) = mx_pack_fp8(x, byte);
+                __builtin_nontemporal_store(mx_pack_fp8(x, byte), reinterpret_cast<words2*>(h.values + m * h.value_bytes + n));
                 if ((threadIdx.x & 3) == 0) h.scales[m * h.scale_bytes + n / kMxBlock] = (uint8_t)byte;
             }
-        } else if (h.to != nullptr && live) store<8>(h, m, n, width - n, x);
+        } else if (h.to != nullptr && live && n < width) {
+            if (h.bf16) stream_vec(static_cast<bf16_t*>(h.to) + m * h.pitch + n, width - n, x);
+            else stream_vec(static_cast<float*>(h.to) + m * h.pitch + n, width - n, x);
+        }
     }
     // Four results of eight columns.
     __device__ __forceinline__ void gate(const float (&p)[8], float (&h)[4]) const {

@@ -114,6 +114,18 @@ __device__ __forceinline__ void store_vec(bf16_t* p, int64_t left, const float (
     }
 }
 
+// Eight numbers of a large output, which is read again only after much else: stores that do not push other data out of the caches.
+__device__ __forceinline__ void stream_vec(float* p, int64_t left, const float (&x)[8]) {
+    if (left >= 8) {
+        __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4_any*>(p));
+        __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, reinterpret_cast<f32x4_any*>(p + 4));
+    } else store_vec<8>(p, left, x);
+}
+__device__ __forceinline__ void stream_vec(bf16_t* p, int64_t left, const float (&x)[8]) {
+    if (left >= 8) __builtin_nontemporal_store(words4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}, reinterpret_cast<words4_any*>(p));
+    else store_vec<8>(p, left, x);
+}
+
 // Moves within rows of 16 lanes, without LDS.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }

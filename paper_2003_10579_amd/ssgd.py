@@ -799,9 +799,10 @@ def _activation_backward(what, dy, p, gated, activation, hidden, format, format_
         floats = _lib.ssgd_mx_activation_backward_work_floats(rows, cols)
         if floats < 0:
             _refuse(f"{what}: rows < 2^31, columns up to 2^24 - 128")
-        db, work = _torch.empty(cols, dtype=_torch.float32, device=dev), _torch.empty(floats, dtype=_torch.float32, device=dev)
+        db = _torch.empty(cols, dtype=_torch.float32, device=dev)
+        work = _torch.empty(floats, dtype=_torch.float32, device=dev) if floats else None
     _call(_lib.ssgd_mx_activation_backward, dev, dy.data_ptr(), kind, pitch, rows, cols, gated, act, *kept, _FORMATS[format], *q._at, _FORMATS[format_transposed], *t._at,
-          *((0, None, None) if h is None else (_FORMATS[hidden], *h._at)), *((None, None) if db is None else (db.data_ptr(), work.data_ptr())))
+          *((0, None, None) if h is None else (_FORMATS[hidden], *h._at)), None if db is None else db.data_ptr(), None if work is None else work.data_ptr())
     return q, t, h, db
 
 

@@ -96,11 +96,11 @@ def test_mx_activation_backward_refuses(L, bad, gated):
 
 
 def test_mx_activation_backward_bias(L):
-    call = lambda gated, cols, db, work: L.ssgd_mx_activation_backward(A, 0, cols, 10, cols, gated, 3, A, 0, 2 * cols, None, None, 1, A, A, 1, A, A, 0, None, None, db, work, None)  # noqa: E731
+    call = lambda gated, cols, db, work: L.ssgd_mx_activation_backward(A, 0, cols, 200, cols, gated, 3, A, 0, 2 * cols, None, None, 1, A, A, 1, A, A, 0, None, None, db, work, None)  # noqa: E731
     for args in ((1, 40, A, A), (0, 40, A, None), (0, 40, A, A + 8), (0, 40, A + 2, A)):
         _refused(L, call(*args), b"bias")
     floats = L.ssgd_mx_activation_backward_work_floats
-    assert floats(0, 40) == 0 and floats(1, 40) == 40 and floats(129, 40) == 80 and floats(-1, 40) == -1 and floats(10, 1 << 25) == -1
+    assert floats(0, 40) == 0 and floats(128, 40) == 0 and floats(129, 40) == 80 and floats(-1, 40) == -1 and floats(10, 1 << 25) == -1
     assert L.ssgd_mx_activation_backward(None, 0, 0, 10, 0, 0, 3, None, 0, 0, None, None, 1, None, None, 1, None, None, 0, None, None, None, None, None) == ssgd.OK
 
 
