@@ -535,7 +535,9 @@ void launch_forward(Forward a, hipStream_t s) {
         return;
     }
     // rows next to each other to a team: they share a gate as a rule
-    const int64_t most = (lanes == 64 ? 2048 : 524288 / lanes) * (int64_t)teams;
+    // as many workgroups as are resident, or twice or nearly three times as many where rows are short or two to four thousand columns (65536 x 512: 41 us with 2048, 45 with 1024;
+    // 16384 x 4096: 87 with 2048, 96 with 768; 4000 x 8192: 40 with 256, 47 with 1024; 30000 x 2000: 73 with 1024, 75 with 2048)
+    const int64_t most = (a.d <= 512 ? 2048 : (a.d <= 1024 ? 768 : (a.d <= 2048 ? 1024 : (a.d <= 4096 ? 2048 : 256)))) * (int64_t)teams;
     a.chunk = (a.rows + most - 1) / most;
     const int64_t blocks = ((a.rows + a.chunk - 1) / a.chunk + teams - 1) / teams;
     const dim3 grid((unsigned)blocks), group(lanes == 64 ? 256 : lanes);
@@ -547,11 +549,11 @@ void launch_forward(Forward a, hipStream_t s) {
     else hipLaunchKernelGGL((forward_kernel<T, FP8, 1024, 2>), grid, group, 0, s, a);
 }
 
-// Rows of a unit: as many units as are resident, at most 64 rows to a team, whose sums are in fp32.
+// Rows of a unit: as many units as are resident (16384 x 4096: 162 us with 256, 166 with 512), at most 64 rows to a team, whose sums are in fp32.
 constexpr int64_t kChain = 64;
 int64_t chunk_for(int64_t rows, int64_t per_gate, int64_t d) {
     const int lanes = lanes_backward(d);
-    const int64_t teams = lanes == 64 ? 4 : 1, most = d > 4096 ? 256 : (d > 2048 ? 512 : 1024);
+    const int64_t teams = lanes == 64 ? 4 : 1, most = d > 4096 ? 256 : (d > 2048 ? 256 : (d > 1024 ? 768 : (d > 512 ? 512 : 1024)));
     int64_t chunk = (rows + most - 1) / most;
     if (chunk < teams) chunk = teams;
     if (chunk > kChain * teams) chunk = kChain * teams;

@@ -105,6 +105,17 @@ template <typename T, int W> struct Raw;
 template <int W> struct Raw<float, W> {
     float x[8][W];
     __device__ __forceinline__ void load_all(int r, const float* row) { load_vec<W>(row, W, x[r]); }
+    __device__ __forceinline__ void settle(int r, int gone) {
+        if (gone == 0) return;
+#pragma unroll
+        for (int step = W / 2; step > 0; step /= 2) {
+            if (gone & step) {
+#pragma unroll
+                for (int q = 0; q < W; ++q) x[r][q] = q + step < W ? x[r][q + step] : 0.0f;
+            }
+        }
+        if (gone >= W) clear(r);
+    }
     __device__ __forceinline__ void load(int r, const float* row, int64_t left) { load_vec<W>(row, left, x[r]); }
     __device__ __forceinline__ void clear(int r) {
 #pragma unroll
@@ -122,6 +133,21 @@ template <int W> struct Raw<bf16_t, W> {
             const words2 v = *reinterpret_cast<const words2_any*>(row);
             x[r][0] = v.x; x[r][1] = v.y;
         }
+    }
+    __device__ __forceinline__ void settle(int r, int gone) {
+        if (gone == 0) return;
+#pragma unroll
+        for (int step = W / 4; step > 0; step /= 2) {
+            if (gone & (2 * step)) {
+#pragma unroll
+                for (int k = 0; k < W / 2; ++k) x[r][k] = k + step < W / 2 ? x[r][k + step] : 0u;
+            }
+        }
+        if (gone & 1) {
+#pragma unroll
+            for (int k = 0; k < W / 2; ++k) x[r][k] = x[r][k] >> 16 | (k + 1 < W / 2 ? x[r][k + 1] << 16 : 0u);
+        }
+        if (gone >= W) clear(r);
     }
     __device__ __forceinline__ void load(int r, const bf16_t* row, int64_t left) {
         if (left >= W) load_all(r, row);
@@ -145,7 +171,28 @@ template <> struct Raw<Fp8, 8> {
         return f32x2{v.x * scale[r], v.y * scale[r]};
     }
 };
-// `whole`: all of the tile's rows and columns are there (a load that may be left out waits for those before it).
+// Rows of a matrix in a tile: `whole`: all of the tile's rows and columns are there.  Where they are not, rows past the last one read that one and columns past the end
+// the row's last ones, which move to the front or are cleared when all have arrived: a load that may be left out waits for those before it (129 x 777: 15 us).
+template <typename T, int W>
+__device__ __forceinline__ void load_rows(Raw<T, W>& to, const void* matrix, int64_t pitch, int64_t rows, int64_t cols, int64_t row, int64_t col, bool whole) {
+    const T* from = static_cast<const T*>(matrix);
+    if (whole) {
+        from += row * pitch + col;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) to.load_all(r, from + r * pitch);
+    } else if (cols >= W) {
+        const int64_t at = col <= cols - W ? col : cols - W;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) to.load_all(r, from + (row + r < rows ? row + r : rows - 1) * pitch + at);
+        const int gone = col - at < W ? (int)(col - at) : W;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) to.settle(r, row + r < rows ? gone : W);
+    } else {
+        from += row * pitch + col;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) to.load(r, from + r * pitch, row + r < rows ? cols - col : 0);
+    }
+}
 template <typename P>
 __device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, bool whole, Raw<P, 8>& p) {
     if constexpr (std::is_same_v<P, Fp8>) {
@@ -154,18 +201,17 @@ __device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, bo
         const int64_t r0 = at.row - (at.wave * 32 + at.turn * 8);
         const uint8_t *values = a.p_values + r0 * a.p_bytes, *scales = a.p_scales + r0 * a.p_scale_bytes;
         const uint32_t pitch = (uint32_t)a.p_bytes, scale_pitch = (uint32_t)a.p_scale_bytes, row = (uint32_t)(at.wave * 32 + at.turn * 8);
-        const uint32_t from = row * pitch + (uint32_t)at.col, scale_from = row * scale_pitch + (uint32_t)(at.col / kMxBlock);
-        auto load = [&](int r) { byte[r] = scales[scale_from + r * scale_pitch]; p.x[r] = *reinterpret_cast<const words2*>(values + (from + r * pitch)); };
-        if (whole) {
+        // (rows past the last one read that one, and are cleared)
+        const uint32_t last = (uint32_t)(a.rows - 1 - r0 < kTile ? a.rows - 1 - r0 : kTile), cols_at = (uint32_t)at.col, block_at = (uint32_t)(at.col / kMxBlock);
 #pragma unroll
-            for (int r = 0; r < 8; ++r) load(r);
-        } else {
+        for (int r = 0; r < 8; ++r) {
+            const uint32_t own = row + r < last ? row + r : last;
+            byte[r] = scales[own * scale_pitch + block_at];
+            p.x[r] = *reinterpret_cast<const words2*>(values + (own * pitch + cols_at));
+        }
+        if (!whole) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                p.x[r] = words2{0u, 0u};
-                byte[r] = 0u;
-                if (at.row + r < a.rows) load(r);
-            }
+            for (int r = 0; r < 8; ++r) if (row + r > last) { byte[r] = 0u; p.x[r] = words2{0u, 0u}; }
         }
         // (columns past the last one in a block that is NaN are NaN too: what the formulas make of them is what they make of the block's others)
 #pragma unroll
@@ -176,14 +222,7 @@ __device__ __forceinline__ void load_kept(const Gradient& a, const Place& at, bo
             for (int r = 0; r < 8; ++r) p.clear(r);
             return;
         }
-        const P* from = static_cast<const P*>(a.p) + at.row * a.p_pitch + at.col;
-        if (whole) {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) p.load_all(r, from + r * a.p_pitch);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) p.load(r, from + r * a.p_pitch, at.row + r < a.rows ? a.p_cols - at.col : 0);
-        }
+        load_rows<P, 8>(p, a.p, a.p_pitch, a.rows, a.p_cols, at.row, at.col, whole);
     }
 }
 
@@ -246,14 +285,7 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Gradient a) {
     Raw<T, W> dy;
     float d[8][8];
     const bool whole = (tile_row + 1) * kTile <= a.rows && c0 + kTile <= a.p_cols;
-    const T* from = static_cast<const T*>(a.dy) + at.row * a.dy_pitch + own_col;
-    if (whole) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) dy.load_all(r, from + r * a.dy_pitch);
-    } else {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) dy.load(r, from + r * a.dy_pitch, at.row + r < a.rows ? a.cols - own_col : 0);
-    }
+    load_rows<T, W>(dy, a.dy, a.dy_pitch, a.rows, a.cols, at.row, own_col, whole);
     load_kept(a, at, whole, p);
     if (a.activation == SSGD_ACT_RELU) differentiate<SSGD_ACT_RELU, GATED>(a, at, p, dy, d, columns, hidden);
     else if (a.activation == SSGD_ACT_GELU) differentiate<SSGD_ACT_GELU, GATED>(a, at, p, dy, d, columns, hidden);
@@ -296,18 +328,19 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* valu
     float x[8][8];
     uint32_t byte[8];
     words2 w[8];
-    const uint8_t *from = values + at.row * row_bytes + (FMT == SSGD_MX_FP8 ? at.col : at.col / 2), *scale = scales + at.row * scale_bytes + at.col / kMxBlock;
+    // (rows past the last one read that one, and are cleared)
     auto load = [&](int r) {
-        byte[r] = scale[r * scale_bytes];
-        if constexpr (FMT == SSGD_MX_FP8) w[r] = *reinterpret_cast<const words2*>(from + r * row_bytes);
-        else w[r] = words2{*reinterpret_cast<const uint32_t*>(from + r * row_bytes), 0u};
+        const int64_t row = at.row + r < rows ? at.row + r : rows - 1;
+        const uint8_t* from = values + row * row_bytes + (FMT == SSGD_MX_FP8 ? at.col : at.col / 2);
+        byte[r] = scales[row * scale_bytes + at.col / kMxBlock];
+        if constexpr (FMT == SSGD_MX_FP8) w[r] = *reinterpret_cast<const words2*>(from);
+        else w[r] = words2{*reinterpret_cast<const uint32_t*>(from), 0u};
     };
-    if ((tile_row + 1) * kTile <= rows) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) load(r);
-    } else {
+    for (int r = 0; r < 8; ++r) load(r);
+    if ((tile_row + 1) * kTile > rows) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) { byte[r] = 0u; w[r] = words2{0u, 0u}; if (at.row + r < rows) load(r); }
+        for (int r = 0; r < 8; ++r) if (at.row + r >= rows) { byte[r] = 0u; w[r] = words2{0u, 0u}; }
     }
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
