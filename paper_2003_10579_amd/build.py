@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libssgd.so")
 SOURCES = ["linear_tile.hip", "linear_tile_lsq.hip", "api.hip", "schedule.hip", "linear.hip", "linear_defer.hip", "full_loss.hip", "full_grad.hip", "mlp.hip", "mc.hip",
            "adamw.hip", "mx_quantize.hip", "rmsnorm.hip", "mx_matmul.hip",
            "mx_dense.hip", "mx_backward.hip", "block_norm.hip"]
-HEADERS = ["common.hpp", "limits.hpp", "rng.hpp", "mlp.hpp", "ops.hpp", "mx_product.hpp", "activations.hpp", "column_sums.hpp", os.path.join("..", "..", "include", "ssgd.h")]
+HEADERS = ["common.hpp", "limits.hpp", "rng.hpp", "mlp.hpp", "ops.hpp", "mx_product.hpp", "activations.hpp", "column_sums.hpp", "rows.hpp", os.path.join("..", "..", "include", "ssgd.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # event-process arithmetic (clock sums, AdaSync rule) must round like plain IEEE operations

@@ -12,7 +12,7 @@
 // rounded once: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before it is rounded.
 #include <cmath>
 
-#include "ops.hpp"
+#include "rows.hpp"
 
 using namespace ssgd;
 
@@ -84,15 +84,8 @@ __device__ __forceinline__ double sum_of_squares(const float (&x)[NV][8], double
     return team_sum<LANES>(sum, part);
 }
 
-__device__ __forceinline__ void load_side(const void* w, int bf16, int64_t at, int64_t left, float (&x)[8]) {
-    if (bf16) load_vec<8>(static_cast<const bf16_t*>(w) + at, left, x);
-    else load_vec<8>(static_cast<const float*>(w) + at, left, x);
-}
 template <typename T>
 __device__ __forceinline__ void load_row(const void* rows, int64_t row, int64_t pitch, int col, int d, float (&x)[8]) { load_vec<8>(static_cast<const T*>(rows) + row * pitch + col, d - col, x); }
-
-__device__ __forceinline__ float as_stored(const float*, float x) { return x; }
-__device__ __forceinline__ float as_stored(const bf16_t*, float x) { return bf16_to_f32(f32_to_bf16(x)); }
 
 // (mean + eps)^(-1/2) from the sum of squares: an estimate of 2^-26 or so, and one step of Newton's that doubles its digits (a root and a quotient in fp64 are a hundred
 // instructions for every thread of a row).
@@ -102,27 +95,14 @@ __device__ __forceinline__ double inverse_root(double squares, double per_column
     return x > 0.0 && x < __builtin_inf() ? better : r;
 }
 
-// Eight columns of a row up to `end`, read and, when they have arrived, as numbers; SHORT: rows of less than eight columns are among them.
-template <bool SHORT, typename T>
-__device__ __forceinline__ void read(Eight<T>& to, const void* rows, int64_t row, int64_t pitch, int col, int end, int d) {
-    const T* from = static_cast<const T*>(rows) + row * pitch;
-    if (!SHORT || d >= 8) to.load(from, col, end);
-    else to.load_few(from, col, end);
-}
-template <bool SHORT, typename T>
-__device__ __forceinline__ void numbers(Eight<T>& x, int col, int end, int d, float (&to)[8]) {
-    if (!SHORT || d >= 8) x.settle(col, end);
-    x.numbers(to);
-}
-
 // w_post times the gate of a row: what the normalised output is multiplied by.
 __device__ __forceinline__ void factor_of(const Forward& a, int64_t gate, int col, double (&f)[8]) {
     float x[8];
-    load_side(a.post, a.post_bf16, col, a.d - col, x);
+    load_weight(a.post, a.post_bf16, col, a.d - col, x);
 #pragma unroll
     for (int q = 0; q < 8; ++q) f[q] = x[q];
     if (a.gate == nullptr) return;
-    load_side(a.gate, a.gate_bf16, gate * a.gate_pitch + col, a.d - col, x);
+    load_weight(a.gate, a.gate_bf16, gate * a.gate_pitch + col, a.d - col, x);
 #pragma unroll
     for (int q = 0; q < 8; ++q) f[q] *= x[q];
 }
@@ -176,7 +156,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
         load(first);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+            load_weight(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
             factor_of(a, gate, col_of(v), f[v]);
         }
     }
@@ -208,7 +188,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void forward_kernel(Forw
         if (lane == 0) { a.rstd_o[row] = (float)rstd_o; a.rstd[row] = rstd; }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if constexpr (!kKept) load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+            if constexpr (!kKept) load_weight(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
             if (v < NV - 1 || col_of(v) < wide) store_normed<T, FP8>(a, row, col_of(v), o[v], rstd, w[v]);
         }
     }
@@ -246,17 +226,17 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
         for (int col = threadIdx.x * 8; col < wide; col += 8192) {
             float s[8], w[8];
             load_row<T>(a.sum, row, a.sum_pitch, col, a.d, s);
-            load_side(a.w, a.w_bf16, col, a.d - col, w);
+            load_weight(a.w, a.w_bf16, col, a.d - col, w);
             store_normed<T, FP8>(a, row, col, s, rstd, w);
         }
     }
 }
 
 __device__ __forceinline__ void factor_of(const Backward& a, int64_t gate, int col, float (&f)[8]) {
-    load_side(a.post, a.post_bf16, col, a.d - col, f);
+    load_weight(a.post, a.post_bf16, col, a.d - col, f);
     if (a.gate == nullptr) return;
     float x[8];
-    load_side(a.gate, a.gate_bf16, gate * a.gate_pitch + col, a.d - col, x);
+    load_weight(a.gate, a.gate_bf16, gate * a.gate_pitch + col, a.d - col, x);
 #pragma unroll
     for (int q = 0; q < 8; ++q) f[q] *= x[q];
 }
@@ -283,7 +263,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     auto end_of = [&](int v) { return v < NV - 1 ? col_of(v) + 8 : a.d; };
     float w[NV][8], f[NV][8], dw[NV][8], S[NV][8];
     auto load_sides = [&](int v) {
-        load_side(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
+        load_weight(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
         factor_of(a, gate, col_of(v), f[v]);
     };
     Eight<T> next_dy[NV], next_sum[NV], next_o[NV], next_more[NV];
@@ -410,7 +390,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             float g[8], x[8], w[8];
             load_row<T>(a.dy, row, a.dy_pitch, col, a.d, g);
             load_row<T>(a.sum, row, a.sum_pitch, col, a.d, x);
-            load_side(a.w, a.w_bf16, col, a.d - col, w);
+            load_weight(a.w, a.w_bf16, col, a.d - col, w);
             float few = 0.0f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) few += g[q] * w[q] * (x[q] * rstd);
@@ -424,7 +404,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             load_row<T>(a.sum, row, a.sum_pitch, col, a.d, x);
             load_row<T>(a.o, row, a.o_pitch, col, a.d, oh);
             load_dsum<T>(a, row, col, more);
-            load_side(a.w, a.w_bf16, col, a.d - col, w);
+            load_weight(a.w, a.w_bf16, col, a.d - col, w);
             factor_of(a, gate, col, f);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {

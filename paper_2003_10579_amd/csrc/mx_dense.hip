@@ -195,13 +195,15 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* parts, int32_t
     e.ahead(row, col, r);
     e.bias_of(col, b);
     const float* at = parts + row * e.cols + col;
+    float x[8][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k < n) load_vec<8>(at + k * stride, e.cols - col, x[k]);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         if (k >= n) break;
-        float x[8];
-        load_vec<8>(at + k * stride, e.cols - col, x);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) p[q] += x[q];
+        for (int q = 0; q < 8; ++q) p[q] += x[k][q];
     }
     e.add_bias(col, b, p);
     e.keep(row, col, p);

@@ -11,6 +11,7 @@
 #include <cmath>
 
 #include "column_sums.hpp"
+#include "rows.hpp"
 
 using namespace ssgd;
 
@@ -52,14 +53,6 @@ __device__ __forceinline__ double team_sum(double x, double* part) {
     }
     return x;
 }
-
-__device__ __forceinline__ void load_weight(const void* w, int bf16, int col, int d, float (&x)[8]) {
-    if (bf16) load_vec<8>(static_cast<const bf16_t*>(w) + col, d - col, x);
-    else load_vec<8>(static_cast<const float*>(w) + col, d - col, x);
-}
-
-__device__ __forceinline__ float as_stored(const float*, float x) { return x; }
-__device__ __forceinline__ float as_stored(const bf16_t*, float x) { return bf16_to_f32(f32_to_bf16(x)); }
 
 // Eight columns of the stream: the sum, rounded as it is stored, and stored.
 template <typename T>
@@ -106,19 +99,6 @@ __device__ __forceinline__ float inverse_root(double squares, const Forward& a) 
     return (float)(1.0 / sqrt(all));
 }
 
-// Eight columns of a row up to `end`, read and, when they have arrived, as numbers; SHORT: rows of less than eight columns are among them.
-template <bool SHORT, typename T>
-__device__ __forceinline__ void read(Eight<T>& to, const void* rows, int64_t row, int64_t pitch, int col, int end, int d) {
-    const T* from = static_cast<const T*>(rows) + row * pitch;
-    if (!SHORT || d >= 8) to.load(from, col, end);
-    else to.load_few(from, col, end);
-}
-template <bool SHORT, typename T>
-__device__ __forceinline__ void numbers(Eight<T>& x, int col, int end, int d, float (&to)[8]) {
-    if (!SHORT || d >= 8) x.settle(col, end);
-    x.numbers(to);
-}
-
 // (four waves to a SIMD: sixteen fp32 columns a thread with 8-bit output are two registers above what that leaves)
 template <typename T, bool FP8, int LANES, int NV>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, 4) void forward_kernel(Forward a) {
@@ -146,7 +126,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, 4) void forward_kernel(F
     if constexpr (kAhead) load(team);
     float w[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, col_of(v), end_of(v), w[v]);
+    for (int v = 0; v < NV; ++v) load_weight(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
     for (int64_t row = team; row < a.rows; row += teams) {
         if constexpr (!kAhead) load(row);
         float s[NV][8];
@@ -223,7 +203,7 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Forward a) {
         for (int64_t col = threadIdx.x * 8; col < end; col += 8192) {
             float s[8], w[8];
             again(col, s);
-            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
+            load_weight(a.w, a.w_bf16, (int)col, a.d - (int)col, w);
             store_normed<T, FP8>(a, row, (int)col, a.d, s, rstd, w);
         }
     }
@@ -267,7 +247,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void backward_kernel(Bac
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_weight(a.w, a.w_bf16, col_of(v), end_of(v), w[v]);
+        load_weight(a.w, a.w_bf16, col_of(v), end_of(v) - col_of(v), w[v]);
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[v][q] = 0.0f;
     }
@@ -382,7 +362,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             float dy[8], s[8], w[8];
             load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy);
             load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, s);
-            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
+            load_weight(a.w, a.w_bf16, (int)col, a.d - (int)col, w);
             float few = 0.0f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) few += dy[q] * w[q] * (s[q] * rstd);
@@ -393,7 +373,7 @@ __global__ __launch_bounds__(1024) void backward_long_kernel(Backward a) {
             float dy[8], s[8], w[8];
             load_vec<8>(static_cast<const T*>(a.dy) + row * a.dy_pitch + col, a.d - col, dy);
             load_vec<8>(static_cast<const T*>(a.s) + row * a.s_pitch + col, a.d - col, s);
-            load_weight(a.w, a.w_bf16, (int)col, a.d, w);
+            load_weight(a.w, a.w_bf16, (int)col, a.d - (int)col, w);
 #pragma unroll
             for (int q = 0; q < 8; ++q) s[q] *= rstd;
             store_dx<T, false>(a, row, col, a.d, dy, s, w, rstd, c);

@@ -120,3 +120,32 @@ def test_two_streams_at_once(env):
                 got[k] = model.answer(x[:n])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("rows", [1, 2, 12, 40, 70])
+def test_answers_captured_and_replayed(env, rows):
+    """A serving step as a graph: the same bits as without one, with new rows in every replay."""
+    torch, ssgd, lowbit_block = env
+    model = lowbit_block.GatedBlocks(640, 900, 2, seed=6)
+    model.quantize_weights()
+    x = torch.randn(rows, 640, device="cuda").to(torch.bfloat16)
+    # what a program takes that goes on from 8-bit rows, or from rows as they are
+    def step():
+        out = model.answer(x)
+        h = ssgd.mx_gated(out, model.q_up[0][0], output="fp8")
+        return out, ssgd.mx_dense(h, model.q_down[0][0], bias=model.bias[0], activation="gelu", residual=out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, 640, device="cuda"))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
