@@ -52,12 +52,16 @@ struct Along {
           at((uint32_t)(p.wave * 32 + p.turn * 8) * (uint32_t)t.row_bytes + (uint32_t)(t.fmt == SSGD_MX_FP4 ? p.col / 2 : p.col)),
           scale_at((uint32_t)(p.wave * 32 + p.turn * 8) * (uint32_t)t.scale_bytes + (uint32_t)(p.col / kMxBlock)) {}
     __device__ __forceinline__ void store(const Target& t, int r, bool live, const float (&x)[8]) const {
-        const uint32_t most = max_of_4(largest_of(x));
-        const uint32_t byte = t.fmt == SSGD_MX_FP4 ? mx_scale_byte<SSGD_MX_FP4>(most) : mx_scale_byte<SSGD_MX_FP8>(most);
+        const uint32_t most = max_of_4(largest_of(x)), to = at + (uint32_t)r * (uint32_t)t.row_bytes;
+        uint32_t byte;
+        if (t.fmt == SSGD_MX_FP4) {
+            byte = mx_scale_byte<SSGD_MX_FP4>(most);
+            if (live) *reinterpret_cast<uint32_t*>(values + to) = mx_pack_fp4(x, byte);
+        } else {
+            const words2 w = mx_quantize_fp8(x, most, byte);
+            if (live) __builtin_nontemporal_store(w, reinterpret_cast<words2*>(values + to));
+        }
         if (!live) return;
-        const uint32_t to = at + (uint32_t)r * (uint32_t)t.row_bytes;
-        if (t.fmt == SSGD_MX_FP4) *reinterpret_cast<uint32_t*>(values + to) = mx_pack_fp4(x, byte);
-        else __builtin_nontemporal_store(mx_pack_fp8_as_it_is(x, byte), reinterpret_cast<words2*>(values + to));
         if ((threadIdx.x & 3) == 0) scales[scale_at + (uint32_t)r * (uint32_t)t.scale_bytes] = (uint8_t)byte;
     }
 };
@@ -70,19 +74,23 @@ template <int COLS> struct Columns {
     uint8_t scales[COLS * 4];
     static __device__ __forceinline__ int part8(int col, int part) { return ((col ^ ((col >> 6) & 1)) * 8 + (part ^ ((col >> 3) & 7))) * 4; }
     static __device__ __forceinline__ int part4(int col, int part) { return ((col ^ ((col >> 5) & 3)) * 4 + (part ^ ((col >> 3) & 3))) * 4; }
-    // Eight rows of column `col` of the tile.
-    __device__ __forceinline__ void put(int32_t fmt, const Place& at, int col, const float (&x)[8]) {
+    // Eight rows of column `own + q` of the tile, q < 8 and own a multiple of eight.  (All that depends on the lane is the same for all q but which of two neighbours it is,
+    // so the compiler has two addresses and constants.)
+    __device__ __forceinline__ void put(int32_t fmt, const Place& at, int own, int q, const float (&x)[8]) {
         const uint32_t most = max_of_rows(largest_of(x));
         uint32_t byte;
         if (fmt == SSGD_MX_FP4) {
             byte = mx_scale_byte<SSGD_MX_FP4>(most);
-            values[part4(col, at.wave) + at.turn] = mx_pack_fp4(x, byte);
+            values[part4(own + q, at.wave) + at.turn] = mx_pack_fp4(x, byte);
         } else {
-            byte = mx_scale_byte<SSGD_MX_FP8>(most);
-            *reinterpret_cast<words2*>(&values[part8(col, at.wave * 2 + (at.turn >> 1)) + (at.turn & 1) * 2]) = mx_pack_fp8_as_it_is(x, byte);
+            const int flip = (own >> 6) & 1, part = (at.wave * 2 + (at.turn >> 1)) ^ ((own >> 3) & 7);
+            const int first = (own * 8 + part) * 4 + (at.turn & 1) * 2 + (q % 2 ? -flip : flip) * 32;
+            *reinterpret_cast<words2*>(&values[first + q * 32]) = mx_quantize_fp8(x, most, byte);
         }
-        if (at.turn == 0) scales[col * 4 + at.wave] = (uint8_t)byte;
+        if (at.turn == 0) scales[(own + q) * 4 + at.wave] = (uint8_t)byte;
     }
+    // The same for any column.
+    __device__ __forceinline__ void put_at(int32_t fmt, const Place& at, int col, const float (&x)[8]) { put(fmt, at, col & ~7, col & 7, x); }
     // All of them, when all waves have met: column 0 is row `first` of the transposed matrix, of `rows`.
     __device__ __forceinline__ void store(const Target& t, int64_t first, int64_t rows, int64_t r0) const {
         const int parts = t.fmt == SSGD_MX_FP4 ? 4 : 8, shift = t.fmt == SSGD_MX_FP4 ? 2 : 3;
@@ -258,14 +266,14 @@ __device__ __forceinline__ void differentiate(const Gradient& a, const Place& at
 #pragma unroll
             for (int q = 2 * k; q < 2 * k + 2; ++q) {
                 const float x[8] = {d[0][q], d[1][q], d[2][q], d[3][q], d[4][q], d[5][q], d[6][q], d[7][q]};
-                columns.put(a.columns.fmt, at, at.own + q, x);
+                columns.put(a.columns.fmt, at, at.own, q, x);
             }
         }
         if (a.hidden.values != nullptr) {
-            if constexpr (GATED) hidden.put(a.hidden.fmt, at, at.own / 2 + k, h[0]);
+            if constexpr (GATED) hidden.put_at(a.hidden.fmt, at, at.own / 2 + k, h[0]);
             else {
-                hidden.put(a.hidden.fmt, at, at.own + 2 * k, h[0]);
-                hidden.put(a.hidden.fmt, at, at.own + 2 * k + 1, h[1]);
+                hidden.put(a.hidden.fmt, at, at.own, 2 * k, h[0]);
+                hidden.put(a.hidden.fmt, at, at.own, 2 * k + 1, h[1]);
             }
         }
     }
@@ -350,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const uint8_t* valu
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         const float y[8] = {x[0][q], x[1][q], x[2][q], x[3][q], x[4][q], x[5][q], x[6][q], x[7][q]};
-        columns.put(t.fmt, at, at.own + q, y);
+        columns.put(t.fmt, at, at.own, q, y);
     }
     __syncthreads();
     columns.store(t, c0, cols, tile_row * kTile);

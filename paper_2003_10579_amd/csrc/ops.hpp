@@ -185,6 +185,10 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest) {
     const uint32_t e = largest >> 23, top = FMT == SSGD_MX_FP4 ? 2u : 8u;
     return e == 255u ? 255u : (e > top ? e - top : 0u);
 }
+// The same but for 255, which the caller puts in where a wave has such a block at all (`nan_block`, of any lane): a whole difference that stops at zero.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_scale_byte_of_numbers(uint32_t largest) { return __builtin_elementwise_sub_sat(largest >> 23, FMT == SSGD_MX_FP4 ? 2u : 8u); }
+__device__ __forceinline__ bool nan_block(uint32_t largest) { return largest >= 0x7F800000u; }
 // Eight values at a scale -> 4 (E2M1, low nibble first) or 8 bytes, nearest, ties to even, saturating.  The conversions divide by a scale
 // themselves, whose exponent field is the byte; past E4M3's largest value they give NaN, so those values are cut off before: at 448 times the
 // scale, 1.75 x 2^(byte + 8 - 127), which bfloat16 holds as well.  (The byte is 246 at most in 8 bits, and 252 in 4.)
@@ -221,7 +225,16 @@ __device__ __forceinline__ words2 mx_pack_fp8_as_it_is(const float (&x)[8], uint
     shorts2 lo = {0, 0}, hi = {0, 0};
     lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[0], x[1], s, false); lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[2], x[3], s, true);
     hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, x[4], x[5], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, x[6], x[7], s, true);
-    return byte == 255u ? words2{0u, 0u} : words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    return words2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+// Eight values of a block, whose largest magnitude is `most`, in 8 bits, and the block's byte.
+__device__ __forceinline__ words2 mx_quantize_fp8(const float (&x)[8], uint32_t most, uint32_t& byte) {
+    byte = mx_scale_byte_of_numbers<SSGD_MX_FP8>(most);
+    words2 w = mx_pack_fp8_as_it_is(x, byte);
+    if (__builtin_expect(__any(nan_block(most)), 0)) {
+        if (nan_block(most)) { byte = 255u; w = words2{0u, 0u}; }
+    }
+    return w;
 }
 __device__ __forceinline__ uint32_t mx_pack_fp8(float a, float b, float c, float d, uint32_t byte) {
     const float s = mx_scale_of(byte), most = __builtin_bit_cast(float, mx_limit(byte));
