@@ -7,8 +7,8 @@
 //   ds = scale G,   do = rstd_o (G gate w_post - ohat mean(G gate w_post ohat))
 //   dw = sum dy shat,   S = sum over a gate's rows of G ohat:   dgate = w_post S,   dw_post = sum over gates of gate S
 //
-// Bound by memory (16384 x 4096 in bf16, a gate for each of 8 runs: forward with 8-bit output 87 us, 5.4 TB/s; backward 158 us and its sums 9, 4.9 TB/s; 4000 x 8192: 47 and 80 us;
-// 65536 x 512: 41 and 71; rows of 16000, of which 1024 threads hold no more than the row itself, 3.5 and 2.7 TB/s).  A row stays in the registers of its threads, eight or sixteen columns each, through both sums.  The sum s' is taken in fp64 and
+// Bound by memory (16384 x 4096 in bf16, a gate for each of 8 runs: forward with 8-bit output 86 us, 5.5 TB/s; backward 157 us and its sums 7, 5.0 TB/s; 4000 x 8192: 40 and 80 us;
+// 65536 x 512: 41 and 71; rows of 16000, of which 1024 threads hold no more than the row itself, 3.6 and 2.8 TB/s).  A row stays in the registers of its threads, eight or sixteen columns each, through both sums.  The sum s' is taken in fp64 and
 // rounded once: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before it is rounded.
 #include <cmath>
 

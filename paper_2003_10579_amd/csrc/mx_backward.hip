@@ -3,10 +3,10 @@
 //
 //   dp = dy act'(p),   h = act(p)          gated, in pairs of columns g, u:   dg = dy u act'(g),   du = dy act(g),   h = act(g) u
 //
-// Per pair from 8-bit checkpoints 4 bytes are read and 4.1 or 4.6 written (8192 x 8192 pairs, dy in bf16, h in 8 bits: 145 us, 4.3 TB/s; p in bf16 172 us, 4.4 TB/s; not gated 88 us;
-// a bias alone 54 us).  A wave has some 1500 instructions for 64 values of dp, which take 85 of the 145 us: of their two quantisations most.  Large outputs go past the
-// caches' replacement (151 us otherwise).  Measured and not kept: four rows to a lane, for twice the waves (190 us: rows in pieces of 64 bytes), registers for three waves
-// by force (173), workgroups of an XCD side by side (185), four or eight tiles of a column in turn (151 to 160), loads past the replacement (transposition 31 instead of 22).
+// Per pair from 8-bit checkpoints 4.1 bytes are read and 2.1 to 3.1 written (8192 x 8192 pairs, dy in bf16, h in 8 bits: 141 us, 4.4 TB/s; p in bf16 172 us, 4.4 TB/s; not gated 85 us;
+// a bias alone 53 us).  A wave has 1370 vector instructions for 64 values of dp, most of them of their two quantisations: 54 % of the time.  Large outputs go past the caches'
+// replacement (7 us more otherwise).  Measured and not kept: four rows to a lane, for twice the waves (190 us: rows in pieces of 64 bytes), registers for three waves by force (173),
+// workgroups of an XCD side by side (185), two, four or eight tiles of a column in turn (151 to 160 against 151), loads past the replacement (transposition 31 us instead of 22).
 #include <type_traits>
 
 #include "activations.hpp"
@@ -180,7 +180,8 @@ template <> struct Raw<Fp8, 8> {
     }
 };
 // Rows of a matrix in a tile: `whole`: all of the tile's rows and columns are there.  Where they are not, rows past the last one read that one and columns past the end
-// the row's last ones, which move to the front or are cleared when all have arrived: a load that may be left out waits for those before it (129 x 777: 15 us).
+// the row's last ones, which move to the front or are cleared when all have arrived: a load that may be left out waits for those before it (129 x 777: 14.7 us instead of 13.2, of which most is the code's
+// first way through the instruction cache).
 template <typename T, int W>
 __device__ __forceinline__ void load_rows(Raw<T, W>& to, const void* matrix, int64_t pitch, int64_t rows, int64_t cols, int64_t row, int64_t col, bool whole) {
     const T* from = static_cast<const T*>(matrix);
