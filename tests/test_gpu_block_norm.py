@@ -87,7 +87,7 @@ def _check(env, rows, d, dtype, gates, scale, with_dsum=True):
 
 
 # every form: 64 to 1024 threads a row with eight and sixteen columns each, a row that is read again; one row and more than are at work at a time
-SHAPES = [(1, 1, 0), (1, 3072, 1), (3, 7, 1), (4, 64, 2), (2, 511, 0), (9, 512, 3), (7, 513, 7), (4, 1024, 1), (3, 1025, 0), (6, 2048, 2), (2, 2049, 1), (3, 4096, 3), (2, 4097, 1), (3, 8192, 0),
+SHAPES = [(1, 1, 0), (1, 3001, 1), (3, 7, 1), (4, 64, 2), (2, 511, 0), (9, 512, 3), (7, 513, 7), (4, 1024, 1), (3, 1025, 0), (6, 2048, 2), (2, 2049, 1), (3, 4096, 3), (2, 4097, 1), (3, 8192, 0),
           (2, 8193, 2), (2, 16384, 1), (3, 16385, 3), (2, 20000, 1), (5000, 40, 1), (3000, 1030, 50), (1100, 5000, 1), (600, 9000, 4), (300, 16400, 2), (2000, 100, 2000), (20000, 24, 1), (1000, 600, 8)]
 
 
