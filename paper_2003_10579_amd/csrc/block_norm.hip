@@ -117,10 +117,7 @@ __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int 
 #pragma unroll
     for (int q = 0; q < 8; ++q) y[q] = (s[q] * rstd) * w[q];
     if constexpr (FP8) {
-        uint32_t most = 0;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) most = umax(most, magnitude(y[q]));
-        const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
+        const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(largest_of(y)));
         __builtin_nontemporal_store(mx_pack_fp8(y, byte), reinterpret_cast<words2*>(a.values + row * a.row_bytes + col));
         if ((threadIdx.x & 3) == 0) a.scales[row * a.scale_bytes + col / kMxBlock] = (uint8_t)byte;
     } else {

@@ -7,8 +7,8 @@
 // without a rounding in between.  Where a workgroup does not have the whole sum (contractions in parts) or a block of 32 columns (few rows), fp32
 // sums go to a work area and a second launch finishes them.
 //
-// Bound by the product: 8192^3 in 8 by 4 bits takes 379 us without an epilogue, 383 with a bias, 385 with relu, 393 with silu, 407 with gelu or with a residual and 426 with
-// bias, gelu and residual; gated 380 without an activation, 385 with silu, 399 with 8-bit output and p kept in 8 bits (8192 x 16384 x 4096, with twice the results: 410, 453).
+// Bound by the product: 8192^3 in 8 by 4 bits takes 379 us without an epilogue, 388 with a bias, 387 with relu, 396 with silu, 409 with gelu, 398 with a residual and 416
+// with bias, gelu and residual; gated 382 without an activation, 389 with silu, 401 with 8-bit output and p kept in 8 bits (8192 x 16384 x 4096, with twice the results: 406 and 452).
 // What an epilogue adds is memory that waits (all CUs come to it at the same time) and gelu's 26 instructions a value, two of them at a quarter of the rate.
 #include "activations.hpp"
 #include "mx_product.hpp"
@@ -50,19 +50,21 @@ struct Common {
             for (int q = 0; q < 8; ++q) p[q] = n + q < cols ? p[q] : 0.0f;
         }
     }
-    // Eight columns from n on, of `width` that there are; four lanes side by side have a block.
+    // Eight columns from n on, of `width` that there are; four lanes side by side have a block.  STREAM: past the caches' replacement (with bias, gelu
+    // and residual 8192^3 takes 416 us instead of 428, 8192 x 16384 x 4096 takes 495 instead of 514; gated products take the same time either way).
+    template <bool STREAM>
     static __device__ __forceinline__ void store8(const Held& h, int64_t m, int64_t n, int64_t width, bool live, const float (&x)[8]) {
         if (h.values != nullptr) {
-            uint32_t most = 0;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) most = umax(most, magnitude(x[q]));
-            const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(most));
+            const uint32_t byte = mx_scale_byte<SSGD_MX_FP8>(max_of_4(largest_of(x)));
             if (live && n < h.value_bytes) {
-                __builtin_nontemporal_store(mx_pack_fp8(x, byte), reinterpret_cast<words2*>(h.values + m * h.value_bytes + n));
+                words2* to = reinterpret_cast<words2*>(h.values + m * h.value_bytes + n);
+                if constexpr (STREAM) __builtin_nontemporal_store(mx_pack_fp8(x, byte), to);
+                else *to = mx_pack_fp8(x, byte);
                 if ((threadIdx.x & 3) == 0) h.scales[m * h.scale_bytes + n / kMxBlock] = (uint8_t)byte;
             }
         } else if (h.to != nullptr && live && n < width) {
-            if (h.bf16) stream_vec(static_cast<bf16_t*>(h.to) + m * h.pitch + n, width - n, x);
+            if constexpr (!STREAM) store<8>(h, m, n, width - n, x);
+            else if (h.bf16) stream_vec(static_cast<bf16_t*>(h.to) + m * h.pitch + n, width - n, x);
             else stream_vec(static_cast<float*>(h.to) + m * h.pitch + n, width - n, x);
         }
     }
@@ -162,7 +164,7 @@ struct Epilogue : Common {
     }
     __device__ __forceinline__ void store_results(int64_t m, int64_t n, const float (&p)[8]) const {
         const bool live = m < rows;
-        if constexpr (!GATED) store8(out, m, n, cols, live, p);
+        if constexpr (!GATED) store8<true>(out, m, n, cols, live, p);
         else {
             const float h[4] = {p[0], p[1], p[2], p[3]};
             const int64_t c = n / 2;
@@ -179,7 +181,7 @@ struct Epilogue : Common {
         }
     }
     __device__ __forceinline__ bool keeps() const { return kept.to != nullptr || kept.values != nullptr; }
-    __device__ __forceinline__ void keep(int64_t m, int64_t n, const float (&p)[8]) const { store8(kept, m, n, cols, m < rows, p); }
+    __device__ __forceinline__ void keep(int64_t m, int64_t n, const float (&p)[8]) const { store8<!GATED>(kept, m, n, cols, m < rows, p); }
 };
 
 // The parts of a contraction (none: a contraction of no columns), added in order, and the epilogue: eight columns a thread.
