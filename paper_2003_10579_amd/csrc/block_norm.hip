@@ -9,7 +9,7 @@
 //
 // Bound by memory (16384 x 4096 in bf16, a gate for each of 8 runs: forward with 8-bit output 86 us, 5.5 TB/s; backward 157 us and its sums 7, 5.0 TB/s; 4000 x 8192: 40 and 80 us;
 // 65536 x 512: 41 and 71; rows of 16000, of which 1024 threads hold no more than the row itself, 3.6 and 2.8 TB/s).  A row stays in the registers of its threads, eight or sixteen columns each, through both sums.  The sum s' is taken in fp64 and
-// rounded once: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before it is rounded.
+// rounded once, for bfloat16 too: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before it is rounded.
 #include <cmath>
 
 #include "rows.hpp"
@@ -109,7 +109,7 @@ __device__ __forceinline__ void factor_of(const Forward& a, int64_t gate, int co
 template <typename T>
 __device__ __forceinline__ void join(const Forward& a, const float (&o)[8], const float (&s)[8], const double (&f)[8], double rstd_o, float (&sum)[8]) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum[q] = as_stored(static_cast<const T*>(nullptr), (float)((double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q]));
+    for (int q = 0; q < 8; ++q) sum[q] = as_stored(static_cast<const T*>(nullptr), (double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q]);
 }
 template <typename T, bool FP8>
 __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, const float (&s)[8], float rstd, const float (&w)[8]) {
