@@ -315,7 +315,9 @@ ssgd_status ssgd_mx_dense(const void *x, int32_t dtype, int64_t pitch, const voi
                           void *hip_stream);
 /* What lies between the products of its backward pass.  dy (rows x cols) is the gradient of act(p), or of the gated block's output, and p what the forward pass has
  * kept (rows x cols, gated rows x 2 cols): a matrix in p_dtype, or p_values and p_scales (SSGD_MX_FP8); neither is needed with SSGD_ACT_NONE, not gated.
- *   dp = dy act'(p)      gated:   dp[m][2 c] = dy u act'(g),  dp[m][2 c + 1] = dy act(g),   g = p[m][2 c], u = p[m][2 c + 1]      (relu'(0) = 0)
+ *   dp = dy act'(p)      gated:   dp[m][2 c] = dy u act'(g),  dp[m][2 c + 1] = dy act(g),   g = p[m][2 c], u = p[m][2 c + 1]
+ * relu' is 1 where p (g) > 0 and 0 elsewhere, and selects: where it is 0, dp (dg) is zero whatever dy and u are, infinities and NaN among them.  All else are products in fp32,
+ * from left to right.
  * Outputs, each nullable but one: dp quantised along its rows (values, scales in fmt) and along its columns (values_t, scales_t in fmt_t), for the products with the transposed
  * weight and with the layer's input; act(p), or the gated block's output, along its columns (values_h, scales_h in fmt_h), for the next weight's gradient; dbias
  * (fp32, not gated), the sum of dp over its rows.  rows < 2^31, columns of p up to 2^24 - 128.  work: ssgd_mx_activation_backward_work_floats floats, 16-byte aligned, used when dbias is given. */

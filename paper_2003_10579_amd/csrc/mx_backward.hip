@@ -250,7 +250,8 @@ __device__ __forceinline__ void differentiate(const Gradient& a, const Place& at
                 const f32x2 both = dy.pair(r, k / 2);
                 const float g = k % 2 ? both.y : both.x;
                 activation_and_slope(ACT, x.x, y, slope);
-                d[r][2 * k] = g * x.y * slope;
+                // (relu selects, here as below: where its slope is zero, a product past fp32's range is no part of the gradient)
+                d[r][2 * k] = ACT == SSGD_ACT_RELU ? (slope > 0.0f ? g * x.y : 0.0f) : g * x.y * slope;
                 d[r][2 * k + 1] = g * y;
                 h[0][r] = y * x.y;
             } else {

@@ -63,3 +63,32 @@ def test_sums_of_the_stream_in_bfloat16_are_rounded_once(env):
     wide = o.double()
     want = scale * s.double() + wide * (wide.square().mean(1, keepdim=True) + 1e-6).rsqrt() * (gate.double() * post.double()).repeat_interleave(rows // gates, 0)
     assert torch.equal(total, _to_bf16(torch, want))
+
+
+# ---- relu: a closed gate lets nothing through -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kept", ["float32", "fp8"])
+def test_a_closed_relu_selects(env, kept):
+    """At p <= 0 the gradient is zero whatever dy is, for a gated block whatever dy u is: a product past fp32's range, an infinity, NaN."""
+    torch, ssgd = env
+    some = lambda values: bool((values & 0x7F).any())          # (a zero may have a sign)  # noqa: E731
+    rows, cols = 40, 70
+    g = torch.Generator().manual_seed(1)
+    gate = -torch.rand(rows, cols, generator=g)
+    gate[:, ::5] = 0.0
+    up = torch.randn(rows, cols, generator=g).sign() * 2.0 ** 90
+    dy = torch.randn(rows, cols, generator=g).sign() * 2.0 ** 60
+    both = torch.stack((gate, up), 2).flatten(1).cuda()
+    both = ssgd.mx_quantize(both, "fp8") if kept == "fp8" else both
+    q, t, h = ssgd.mx_gated_backward(dy.cuda(), both, "relu", hidden="fp8")
+    for m in (q, t, h):
+        assert not some(m.values) and not (m.scales == 255).any()
+    alone = ssgd.mx_quantize(gate.cuda(), "fp8") if kept == "fp8" else gate.cuda()
+    for bad in (float("inf"), float("nan")):
+        dy[3, 4] = bad
+        q, t, _ = ssgd.mx_gated_backward(dy.cuda(), both, "relu")
+        # the gate's gradient is zero, that of what it multiplies dy times zero
+        assert not some(t.values[0::2]) and not (t.scales[0::2] == 255).any() and t.scales[9, 0] == 255 and int((t.scales == 255).sum()) == 1
+        assert q.scales[3, 0] == 255 and int((q.scales == 255).sum()) == 1
+        q, t, _, db = ssgd.mx_dense_backward(dy.cuda(), alone, "relu")
+        assert not some(q.values) and not some(t.values) and not (q.scales == 255).any() and not (t.scales == 255).any() and not db.any()
