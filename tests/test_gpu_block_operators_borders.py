@@ -92,3 +92,42 @@ def test_a_closed_relu_selects(env, kept):
         assert q.scales[3, 0] == 255 and int((q.scales == 255).sum()) == 1
         q, t, _, db = ssgd.mx_dense_backward(dy.cuda(), alone, "relu")
         assert not some(q.values) and not some(t.values) and not (q.scales == 255).any() and not (t.scales == 255).any() and not db.any()
+
+
+# ---- gelu and silu in fp32, wherever their values are normal numbers ----------------------------------------------------------
+
+def _gelu(x):
+    from scipy.special import ndtr
+    return x * ndtr(x)
+
+
+def _of_bias(torch, ssgd, x, rows, act):
+    """act(x) in fp32 by the product's epilogue: weights of zero, values through the bias."""
+    b = ssgd.MxTensor.empty(x.numel(), 600, "fp4", x.device)
+    b.values.zero_(), b.scales.zero_()
+    return ssgd.mx_dense(torch.ones(rows, 600, device="cuda"), b, bias=x, activation=act)
+
+
+# one row, few rows, tiles
+@pytest.mark.parametrize("rows", [1, 3, 100])
+def test_gelu_over_its_whole_range(env, rows):
+    """Of Phi(-|x|), in units of 2^-24 of itself: the fit's 1 + 2 x^2, the exponent's two roundings x^2 in all, and of its constant 0.11 x^2 that the fit has made good; the exponential two,
+    1 + 0.3425 |x| and its reciprocal three, which are seven in a polynomial that grows as its argument to the power of 2.35 at most, four roundings of that, and two products: 16 + 3.1 x^2.  x Phi(x) is one more."""
+    torch, ssgd = env
+    x = torch.cat([torch.linspace(-12.9, 9, 20001), -torch.logspace(-30, 1, 300), torch.logspace(-30, 30, 300)]).cuda()
+    xh = _host(x)
+    want = _gelu(xh)
+    got = _host(_of_bias(torch, ssgd, x, rows, "gelu"))
+    assert np.all(np.abs(got - want) <= np.where(xh < 0, 17 + 3.2 * xh ** 2, 17) * U * np.abs(want) + 2.0 ** -126)
+
+
+def test_the_slope_of_gelu(env):
+    """Phi + x phi: Phi as above without the exponent's roundings, phi two units of its exponential, one of what is made good, 0.11 x^2 of its constant, two of its factor, and one for the sum."""
+    torch, ssgd = env
+    x = torch.linspace(-12.9, 9, 20001).cuda()[None]
+    xh = _host(x)[0]
+    at = xh != 0
+    phi, cdf = np.exp(-xh * xh / 2) / np.sqrt(2 * np.pi), _gelu(xh) / np.where(at, xh, 1)
+    db = _host(ssgd.mx_dense_backward(torch.ones_like(x), x, "gelu")[3])
+    bound = U * (np.where(xh < 0, 17 + 2.2 * xh ** 2, 17) * cdf + (7 + 0.2 * xh ** 2) * np.abs(xh) * phi) + 2.0 ** -126
+    assert np.all((np.abs(db - cdf - xh * phi) <= bound)[at])
