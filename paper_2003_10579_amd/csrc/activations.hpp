@@ -4,7 +4,9 @@
 
 namespace ssgd {
 
-// 2^x and 1 / x by one instruction each, an error of 2^-23 of the result or less.
+// 2^x and 1 / x by one instruction each, within 2^-23 of the result.  e^x rounds its exponent: |x| units of 2^-24 of the result, and 0.23 |x| for its constant, so that silu is
+// 7 + 1.3 |x| units of itself off at most for x < 0 (1.4e-6 at -12), 8 for x >= 0; below -87.3
+// the quotient is below fp32's normal numbers and may count as zero.  (The exponent made good is five instructions more for a value.)
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
 

@@ -131,3 +131,40 @@ def test_the_slope_of_gelu(env):
     db = _host(ssgd.mx_dense_backward(torch.ones_like(x), x, "gelu")[3])
     bound = U * (np.where(xh < 0, 17 + 2.2 * xh ** 2, 17) * cdf + (7 + 0.2 * xh ** 2) * np.abs(xh) * phi) + 2.0 ** -126
     assert np.all((np.abs(db - cdf - xh * phi) <= bound)[at])
+
+
+def _silu(x):
+    from scipy.special import expit
+    return x * expit(x)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 100])
+def test_silu_over_its_whole_range(env, rows):
+    """In units of 2^-24: the exponent's rounding |x|, its constant 0.23 |x|, the exponential two, the sum one, the quotient two, the product with x one."""
+    torch, ssgd = env
+    x = torch.cat([torch.linspace(-87, 20, 20001), -torch.logspace(-30, 1, 300), torch.logspace(-30, 38, 300)]).cuda()
+    xh = _host(x)
+    want = _silu(xh)
+    got = _host(_of_bias(torch, ssgd, x, rows, "silu"))
+    assert np.all(np.abs(got - want) <= np.where(xh < 0, 7 + 1.3 * np.abs(xh), 7 + 1.3 * np.abs(xh) * np.exp(-np.abs(xh))) * U * np.abs(want) + 2.0 ** -126)
+
+
+def test_the_slope_of_silu(env):
+    """s (1 + x (1 - s)): s is six units off and 1.3 |x| (1 - s) of the exponent's, 1 - s as much of s, and three roundings follow."""
+    torch, ssgd = env
+    x = torch.linspace(-80, 20, 20001).cuda()[None]
+    xh = _host(x)[0]
+    s = 1 / (1 + np.exp(-xh))
+    off = 6 + 1.3 * np.abs(xh) * (1 - s)
+    db = _host(ssgd.mx_dense_backward(torch.ones_like(x), x, "silu")[3])
+    assert np.all(np.abs(db - s * (1 + xh * (1 - s))) <= U * ((off + 4) * s * (1 + np.abs(xh) * (1 - s)) + (off + 1) * np.abs(xh) * s * s) + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("rows", [1, 100])
+def test_the_ends_of_the_range(env, rows, act):
+    """What the formulas give there: the number itself above, zero below, NaN for -inf (times zero) and NaN."""
+    torch, ssgd = env
+    x = torch.tensor([float("inf"), 3.4e38, 1e30, 500.0, -500.0, -1e30, -3.4e38, float("-inf"), float("nan")]).cuda()
+    got = _of_bias(torch, ssgd, x, rows, act)
+    assert torch.equal(got[:, :4], x[:4].expand(rows, 4)) and not got[:, 4:7].any() and got[:, 7:].isnan().all()
