@@ -168,3 +168,67 @@ def test_the_ends_of_the_range(env, rows, act):
     x = torch.tensor([float("inf"), 3.4e38, 1e30, 500.0, -500.0, -1e30, -3.4e38, float("-inf"), float("nan")]).cuda()
     got = _of_bias(torch, ssgd, x, rows, act)
     assert torch.equal(got[:, :4], x[:4].expand(rows, 4)) and not got[:, 4:7].any() and got[:, 7:].isnan().all()
+
+
+# ---- what earlier tests of these operators could not see ------------------------------------------------------------------------
+
+def test_slopes_far_out(env):
+    """A column of the transposed gradient has blocks of its own, so each value is within half a step of E4M3 (2^-4) however large its neighbours are, or, as the
+    largest of its block and with more than 1.75 in front of its power of two, cut off at 1.75: off by (2 - 1.75) / 2 = 2^-3 at most."""
+    torch, ssgd = env
+    far = torch.tensor([0.0, -0.0, 1e4, -1e4, 88.0, -88.0, 300.0, -300.0, 1e38, -1e38, 1e-30, -1e-30]).cuda()
+    fh = _host(far)
+    for act in ("relu", "gelu", "silu"):
+        tiny = np.abs(fh) < 1e-20
+        slope = np.where(fh > 50, 1.0, np.where(fh < -50, 0.0, 0.5))
+        y = np.where(fh > 50, fh, np.where(fh < -50, 0.0, fh / 2))
+        if act == "relu":
+            slope, y = (fh > 0).astype(float), np.maximum(fh, 0)
+        for rows in (32, 100):
+            p, dy = far.repeat(rows, 1), torch.full((rows, far.numel()), 0.75, device="cuda")
+            q, t, _, db = ssgd.mx_dense_backward(dy, p, act)
+            got = _host(ssgd.mx_dequantize(t))
+            assert np.all(np.abs(got - 0.75 * slope[:, None]) <= 2.0 ** -3 * 0.75 * slope[:, None] + 1e-12)
+            assert np.all(np.abs(_host(db) - 0.75 * rows * slope) <= 1e-5 * rows)
+            # gated, with what the gate multiplies moderate
+            p = torch.stack((p, torch.full_like(p, -1.25)), 2).flatten(1)
+            _, t, ht = ssgd.mx_gated_backward(dy, p, act, hidden="fp8")
+            got, h = _host(ssgd.mx_dequantize(t)), _host(ssgd.mx_dequantize(ht))
+            for of, want in ((got[0::2], -0.75 * 1.25 * slope), (got[1::2], 0.75 * y), (h, -1.25 * y)):
+                assert np.all(np.abs(of - want[:, None]) <= 2.0 ** -3 * np.abs(want[:, None]) + (1e-12 if tiny.any() else 0))
+
+
+@pytest.mark.parametrize("act", [None, "relu", "gelu", "silu"])
+@pytest.mark.parametrize("rows", [1, 3, 100])
+def test_a_block_with_nan_leaves_its_neighbours_alone(env, rows, act):
+    torch, ssgd = env
+    N, K = 100, 600
+    x, b = torch.randn(rows, K, device="cuda"), ssgd.mx_quantize(torch.randn(N, K, device="cuda") / 25)
+    bias = torch.randn(N, device="cuda")
+    want, want_kept = ssgd.mx_dense(x, b, bias=bias, activation=act, output="fp8", keep="fp8")
+    for bad in (float("nan"), float("inf")):
+        bias[40] = bad
+        got, kept = ssgd.mx_dense(x, b, bias=bias, activation=act, output="fp8", keep="fp8")
+        for of, to in ((got, want), (kept, want_kept)):
+            assert torch.all(of.scales[:, 1] == 255) and not of.values[:, 32:64].any()
+            others = [0, 2, 3]
+            assert torch.equal(of.scales[:, others], to.scales[:, others]) and torch.equal(of.values[:, :32], to.values[:, :32]) and torch.equal(of.values[:, 64:], to.values[:, 64:])
+
+
+def test_kept_sums_in_8_bits_past_2_to_the_32(env):
+    """The far corner of more than 2^32 results is bit for bit that of the same rows and columns by themselves: they begin at a block of 32 (66000 - 208 = 2056 x 32)."""
+    torch, ssgd = env
+    n, k = 66000, 130
+    a, b = ssgd.mx_quantize(torch.randn(n, k, device="cuda")), ssgd.mx_quantize(torch.randn(n, k, device="cuda"))
+    bias = torch.randn(n, device="cuda")
+    first = n - 208
+    part = lambda q, at: ssgd.MxTensor(q.values[at].contiguous(), q.scales[at].contiguous(), q.format, (208, k))  # noqa: E731
+    cols = slice(first, n)
+    for rows in (slice(0, 208), cols):
+        some, some_kept = ssgd.mx_dense(part(a, rows), part(b, cols), bias=bias[cols].contiguous(), activation="silu", output="fp8", keep="fp8")
+        out, kept = ssgd.mx_dense(a, b, bias=bias, activation="silu", output="fp8", keep="fp8")
+        assert kept.values.numel() > 1 << 32
+        for of, to in ((out, some), (kept, some_kept)):
+            assert torch.equal(of.values[rows, first:n], to.values[:, :208]) and torch.equal(of.scales[rows, first // 32:-(-n // 32)], to.scales[:, :7])
+        del out, kept
+    torch.cuda.empty_cache()
