@@ -3,10 +3,11 @@
 //
 //   dp = dy act'(p),   h = act(p)          gated, in pairs of columns g, u:   dg = dy u act'(g),   du = dy act(g),   h = act(g) u
 //
-// Per pair from 8-bit checkpoints 4.1 bytes are read and 2.1 to 3.1 written (8192 x 8192 pairs, dy in bf16, h in 8 bits: 141 us, 4.4 TB/s; p in bf16 172 us, 4.4 TB/s; not gated 85 us;
+// Per pair from 8-bit checkpoints 4.1 bytes are read and 4.1 written for both quantisations of dp, 0.5 to 1 more for h's (8192 x 8192 pairs, dy in bf16, h in 8 bits: 141 us, 4.4 TB/s; p in bf16 172 us, 4.4 TB/s; not gated 85 us;
 // a bias alone 53 us).  A wave has 1370 vector instructions for 64 values of dp, most of them of their two quantisations: 54 % of the time.  Large outputs go past the caches'
 // replacement (7 us more otherwise).  Measured and not kept: four rows to a lane, for twice the waves (190 us: rows in pieces of 64 bytes), registers for three waves by force (173),
-// workgroups of an XCD side by side (185), two, four or eight tiles of a column in turn (151 to 160 against 151), loads past the replacement (transposition 31 us instead of 22).
+// workgroups of an XCD side by side (185), two, four or eight tiles of a column in turn (151 to 160 against 151), loads past the replacement (transposition of
+// 8192 x 8192 to 4 bits 31 us instead of 22).  Rows in 4 bits leave a lane in four bytes and take the same time past the replacement or not (148 and 152 us).
 #include <type_traits>
 
 #include "activations.hpp"

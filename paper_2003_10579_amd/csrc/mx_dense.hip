@@ -7,8 +7,9 @@
 // without a rounding in between.  Where a workgroup does not have the whole sum (contractions in parts) or a block of 32 columns (few rows), fp32
 // sums go to a work area and a second launch finishes them.
 //
-// Bound by the product: 8192^3 in 8 by 4 bits takes 379 us without an epilogue, 388 with a bias, 387 with relu, 396 with silu, 409 with gelu, 398 with a residual and 416
-// with bias, gelu and residual; gated 382 without an activation, 389 with silu, 401 with 8-bit output and p kept in 8 bits (8192 x 16384 x 4096, with twice the results: 406 and 452).
+// Bound by the product: 8192^3 in 8 by 4 bits, normal numbers, takes 379 us without an epilogue, 388 with a bias, 387 with relu, 396 with silu, 409 with gelu, 398 with a residual and 416
+// with bias, gelu and residual; gated 382 without an activation, 389 with silu, 401 with 8-bit output and p kept in 8 bits (8192 x 16384 x 4096, with twice the results: 406 and 452); another run's clock
+// or inputs make all of them up to 5 % more (421 to 441 for the first with bias, gelu and residual).
 // What an epilogue adds is memory that waits (all CUs come to it at the same time) and gelu's 26 instructions a value, two of them at a quarter of the rate.
 #include "activations.hpp"
 #include "mx_product.hpp"

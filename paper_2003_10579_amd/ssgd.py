@@ -758,7 +758,7 @@ def mx_dense(x, w, bias=None, activation=None, residual=None, format="fp8", dtyp
     """residual + act(x w^T + bias) in one pass, for an MxTensor x or rows (float32 or bfloat16) that are quantised to `format` on the way, and an "fp4"
     MxTensor w (outputs x inputs).  activation: None, "relu", "gelu" or "silu".  The result is a matrix of `dtype` (x's unless it is given, bfloat16 for an
     MxTensor) or, with output="fp8", an MxTensor for the product behind it.  keep="same" (a matrix of dtype) or "fp8" (an MxTensor, a checkpoint in 8 bits)
-    gives (result, x w^T + bias): what mx_dense_backward takes.  Autograd records nothing."""
+    gives (result, x w^T + bias): what mx_dense_backward takes.  The product is as exact as mx_matmul's.  Autograd records nothing."""
     return _epilogue("mx_dense", x, w, 0, activation, bias, residual, format, dtype, output, keep)
 
 
