@@ -357,7 +357,7 @@ ssgd_status ssgd_rmsnorm_backward(const void *dy, int64_t dy_pitch, const void *
  *   y = sum rstd weight,                          rstd = (mean of sum^2 + eps)^(-1/2)
  * o, s, sum and y have `dtype`; the weights are d contiguous elements of their own types.  gate (nullable: 1): `gates` rows of d elements of gate_dtype,
  * gate_pitch apart, each for rows / gates rows of the stream that lie together (one for all: a gate per column; rows % gates == 0).  Output: y, or values and
- * scales (SSGD_MX_FP8, 16-byte aligned).  The sum is taken in fp64 and rounded once.  rstd_o and rstd (fp32, one per row) are for the backward
+ * scales (SSGD_MX_FP8, 16-byte aligned).  The sum is taken in fp64, rounded to fp32 and from there to dtype.  rstd_o and rstd (fp32, one per row) are for the backward
  * pass.  rows < 2^31, 1 <= d < 2^24. */
 ssgd_status ssgd_block_norm(const void *o, int64_t o_pitch, const void *s, int64_t s_pitch, const void *post_weight, int32_t post_dtype,
                             const void *weight, int32_t weight_dtype, const void *gate, int32_t gate_dtype, int64_t gates, int64_t gate_pitch,

@@ -7,13 +7,12 @@
 //   ds = scale G,   do = rstd_o (G gate w_post - ohat mean(G gate w_post ohat))
 //   dw = sum dy shat,   S = sum over a gate's rows of G ohat:   dgate = w_post S,   dw_post = sum over gates of gate S
 //
-// Bound by memory (16384 x 4096 in bf16, a gate for each of 8 runs: forward with 8-bit output 87 us, 5.4 TB/s; backward 157 us and its sums 7, 5.0 TB/s; 4000 x 8192: 46 and 80 us;
-// 65536 x 512: 43 and 71).  Rows of 8193 to 16384
-// columns leave 1024 threads no registers for the next one, and some of their own go to scratch memory (forward 4 to 17 of 128, backward 34 in bf16 and 94 in fp32): 2000 x 16000 in bf16 3.4 and
-// 2.5 TB/s; so do backward rows of 4097 to 8192 in fp32 (31 of 256; 4000 x 8192: 234 us, 3.4 TB/s, forward 86 us, 5.0).  A row stays in the registers of its threads, eight or sixteen columns each, through both sums.  The sum s' is taken in fp64 and
-// rounded once, for bfloat16 too: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before it is rounded.
+// Bound by memory (16384 x 4096 in bf16, a gate for each of 8 runs: forward with 8-bit output 85 us, 5.5 TB/s; backward 159 us and its sums 7, 4.8 TB/s; 4000 x 8192: 43 and 79 us; 65536 x 512:
+// 42 and 76).  Rows of 8193 to 16384 columns leave 1024 threads no registers for the next one, and some of their own go to scratch memory (forward 4 to 17 of 128, backward 34 in bf16 and 94 in
+// fp32): 2000 x 16000 in bf16 3.6 and 2.4 TB/s; so do backward rows of 4097 to 8192 in fp32 (31 of 256; 4000 x 8192: 234 us, 3.4 TB/s, forward 86 us, 5.0).  A row stays in the registers of its threads, eight or sixteen columns each, through both sums.  The sum s' is taken in fp64,
+// rounded to fp32 and from there to the rows' type, as torch brings fp64 to bfloat16: what it is rounded to decides all that follows, and a sum of three products in fp32 is a few units off before
+// it is rounded (of bfloat16 rows three sums in 10^5 are on the other side of a border then; through fp32 seven in 10^6 are not the nearest to the sum in fp64).
 #include <cmath>
-#include <type_traits>
 
 #include "rows.hpp"
 
@@ -111,24 +110,8 @@ __device__ __forceinline__ void factor_of(const Forward& a, int64_t gate, int co
 }
 template <typename T>
 __device__ __forceinline__ void join(const Forward& a, const float (&o)[8], const float (&s)[8], const double (&f)[8], double rstd_o, float (&sum)[8]) {
-    double x[8];
-    float near[8];
-    uint32_t middle = ~0u;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        x[q] = (double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q];
-        near[q] = (float)x[q];
-        if constexpr (std::is_same_v<T, bf16_t>) middle = umin(middle, is_middle(near[q]));
-    }
-    if constexpr (std::is_same_v<T, bf16_t>) {
-        // (one of 65536 values is a middle.  16384 x 4096 with 8-bit output takes 87 us, 90 with selections at every value and 85 with two roundings; 4000 x 8192 46, 47 and 43.)
-        if (__builtin_expect(__any(middle == 0u), 0)) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) near[q] = beside_middle(near[q], x[q]);
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sum[q] = as_stored(static_cast<const T*>(nullptr), near[q]);
+    for (int q = 0; q < 8; ++q) sum[q] = as_stored(static_cast<const T*>(nullptr), (float)((double)s[q] * a.scale + ((double)o[q] * rstd_o) * f[q]));
 }
 template <typename T, bool FP8>
 __device__ __forceinline__ void store_normed(const Forward& a, int64_t row, int col, const float (&s)[8], float rstd, const float (&w)[8]) {
@@ -518,8 +501,8 @@ __global__ __launch_bounds__(1024) void sums_kernel(Sums a) {
     a.dw_post[col] = (float)sum;
 }
 
-// Threads of a row.  (16384 x 4096 in bf16, forward: 256 with sixteen columns each 88 to 92 us, 512 with eight 99; backward with its sums, which has more to keep: 168 and 167.  4000 x 8192,
-// 512 and 1024: 47 and 54 us, 79 and 100.)
+// Threads of a row.  (16384 x 4096 in bf16, forward: 256 with sixteen columns each 85 us, 512 with eight 91 to 95; backward with its sums, which has more to keep: 166 either way.  4000 x 8192,
+// 512 and 1024: 43 and 51 us, 79 and 99.  In fp32 16384 x 4096 takes 223 and 198 us forward, 429 and 399 backward.)
 int lanes_for(int64_t d) { return d <= 1024 ? 64 : (d <= 4096 ? 256 : (d <= 8192 ? 512 : 1024)); }
 int lanes_backward(int64_t d) { return d <= 1024 ? 64 : (d <= 2048 ? 256 : (d <= 8192 ? 512 : 1024)); }
 

@@ -115,8 +115,9 @@ __device__ __forceinline__ void store_vec(bf16_t* p, int64_t left, const float (
 }
 
 // Eight numbers of an output: stores that do not push other data out of the caches, whatever its size.  By themselves the norms between blocks take 2 to 20 % less with them in bf16
-// (16384 x 4096 forward 90 us instead of 99, 4000 x 8192 backward 79 instead of 97), in fp32 8 % less to 20 % more (16384 x 4096 225 instead of 187 us, backward 403 instead of 328); two gated
-// blocks in a row, whose next product reads them, are the same to 3 % either way (one row 50 us, 64 rows 75 instead of 72, 8192 x 4096 trained 4610 us).
+// (16384 x 4096 forward 85 us instead of 94, 4000 x 8192 backward 79 instead of 97), in fp32 15 % less to 23 % more (2047 x 1537 forward 10.6 instead of 12.5 us, 16384 x 4096 backward 400
+// instead of 327); two gated blocks in a row, whose next product reads them, are the same to 3 % either way (one row 50 us, 64 rows 74.5 instead of 72.8, 8192 x 4096 trained 4532
+// instead of 4561, 8192 x 1024 688 instead of 671).
 __device__ __forceinline__ void stream_vec(float* p, int64_t left, const float (&x)[8]) {
     if (left >= 8) {
         __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4_any*>(p));
@@ -133,7 +134,6 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
 // Largest of 4 and of 16 adjacent lanes.  On the bits of magnitudes: infinities and NaN are the largest, so they carry.
 __device__ __forceinline__ uint32_t max_of_4(uint32_t x) { x = umax(x, dpp<kXor1>(x)); return umax(x, dpp<kXor2>(x)); }
 __device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
