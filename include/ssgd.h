@@ -295,7 +295,7 @@ ssgd_status ssgd_mx_linear(const void *x, int32_t dtype, int64_t pitch, int64_t 
 /* The product with a dense layer's epilogue, or with that of a gated feed-forward block:
  *   p = A B^T + bias,   out[m][n] = residual + act(p[m][n])      or, gated (N even, no bias, no residual),   out[m][c] = act(p[m][2 c]) p[m][2 c + 1]
  * so a gated block's B has gate and up rows in turn.  act: none, relu, gelu (x Phi(x), Phi the normal distribution's function to 3.2e-7, below
- * zero to 17 + 3.2 x^2 units of 2^-24 of itself) or silu (x / (1 + e^-x), below zero to 7 + 1.3 |x| units);
+ * zero to 16 + 1.6 x^2 units of 2^-24 of itself) or silu (x / (1 + e^-x), below zero to 7 + 1.3 |x| units);
  * infinities and NaN follow the formulas, and where Phi (x < -13.2) or the quotient (x < -87.3) is below fp32's normal numbers it may count as zero.
  * In fp32 from the product's sums on, rounded once to the output: out (M x N, gated M x N / 2) in out_dtype, or values and
  * scales (16-byte aligned), the rows quantised to SSGD_MX_FP8.  p itself goes, where the backward pass wants it, to kept (kept_dtype) or to kept_values
